@@ -417,6 +417,139 @@ hspmd_status hspmd_attn_block_bwd(const hspmd_attn_plan* plan, const void* q, co
                                   void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * ---- Rotary embedding with positions on several axes ----
+ * hspmd_rope_qk turns a token by its position in its sequence.  Pictures and video have positions in time, height and
+ * width, and a token that is generated has a position that no plan knows: here every token brings its positions, one
+ * per axis, and every pair of columns belongs to one axis.  With x_i the column i < head_dim/2 of a head vector of q or k,
+ * a(i) the pair's axis and p_a the token's position on axis a,
+ *     phi_i = p_{a(i)} theta_i,  theta_i = base^(-2i/head_dim),
+ *     y_i = x_i cos(phi_i) - x_{i+head_dim/2} sin(phi_i),
+ *     y_{i+head_dim/2} = x_{i+head_dim/2} cos(phi_i) + x_i sin(phi_i).
+ * The map is orthogonal: the gradient with respect to x is the rotation by the opposite angles (inverse != 0) of the
+ * gradient with respect to y, in bf16 or fp32 like the gradients of the backward.
+ */
+typedef struct {
+    const float* table;        /* device, from hspmd_rope_table with the tensors' head_dim, 16-byte aligned                       */
+    int32_t table_positions;   /* positions 0 .. table_positions-1 are in the table                                               */
+    int32_t num_axes;          /* 1 .. 4                                                                                          */
+    const int32_t* positions;  /* device: axis a of token t at positions[a * positions_stride + t]                                */
+    int64_t positions_stride;  /* >= the number of tokens where num_axes > 1                                                      */
+    const uint8_t* pair_axis;  /* host, [head_dim / 2], each < num_axes (sections, interleaved, anything); NULL: every pair axis 0 */
+} hspmd_rope_axes;
+
+/*
+ * q_out, k_out = q, k turned (one launch).
+ *   q, q_out   [total_tokens, local_q_heads, head_dim]; k, k_out [total_tokens, local_kv_heads, head_dim]; token strides in
+ *              elements, multiples of 8 and >= heads*head_dim, each tensor its own; in place (q_out == q, k_out == k, with the same
+ *              stride) is allowed, other overlaps are not; 16-byte aligned
+ *   local_kv_heads 0 .. : with 0 only q is turned and k, k_out are not looked at
+ *   dtype      HSPMD_GRAD_BF16 or HSPMD_GRAD_F32, the same for all four.  Arithmetic in fp32 (every product and sum rounded once),
+ *              one rounding to bf16
+ * A position outside the table is not read: the pairs of its axis become NaN for that token.
+ * Errors: INVALID_ARG for NULL / misaligned pointers, bad strides, axes or counts; UNSUPPORTED for a head_dim outside the
+ * supported set or an unknown dtype.  total_tokens == 0 returns OK without launching.
+ */
+hspmd_status hspmd_rope_axes_qk(const hspmd_rope_axes* rope, const void* q, const void* k, int64_t q_token_stride,
+                                int64_t kv_token_stride, void* q_out, void* k_out, int64_t q_out_token_stride,
+                                int64_t kv_out_token_stride, int32_t total_tokens, int32_t local_q_heads, int32_t local_kv_heads,
+                                int32_t head_dim, hspmd_grad_dtype dtype, int32_t inverse, void* stream);
+
+/*
+ * ---- A paged key/value cache, and the attention that reads it ----
+ * For evaluation by generation between training steps: the keys and values of every sequence stay on the device that holds
+ * their heads, in pages of page_size tokens out of one pool, and new tokens (a prompt, a chunk of one, a single token) attend to
+ * all that is cached.  The library owns no part of it: the pool, the page table and the lengths are the caller's.
+ *
+ * The pool.  A page holds page_size consecutive tokens of one sequence, all heads, head by head:
+ *   k, v             [num_pages, local_kv_heads, page_size, row] with row = hspmd_kv_cache_row(head_dim, dtype) elements:
+ *                    head_dim, for e4m3 rounded up to a multiple of 16; the columns past head_dim are the library's and hold zero.
+ *                    Page i starts at i * page_stride elements (a multiple of 16 bytes, >= local_kv_heads*page_size*row), so k and v
+ *                    may lie interleaved in one allocation
+ *   HSPMD_CACHE_BF16 the values
+ *   HSPMD_CACHE_E4M3 8-bit floats (4 exponent, 3 mantissa bits, no infinities) with one power-of-two scale per token and head:
+ *                    value = e4m3 * 2^(scale - 127), scales in k_scale, v_scale, uint8 [num_pages, local_kv_heads, page_size], page i
+ *                    at i * scale_page_stride (a multiple of 4).  A power of two costs a float no precision, makes
+ *                    quantisation and reading back exact but for the one rounding to 8 bits, and every value is a bf16 number.
+ *                    hspmd_kv_cache_write takes e = the smallest integer >= -100 with max |x| <= 448 * 2^e over the row's finite
+ *                    elements, stores scale = e + 127 and round-to-nearest-even(x / 2^e); infinities and NaN become NaN
+ *   page_size        a power of two, 16 .. 1024
+ */
+typedef enum { HSPMD_CACHE_BF16 = 0, HSPMD_CACHE_E4M3 = 1 } hspmd_cache_dtype;
+typedef struct {
+    void* k;                     /* device, 16-byte aligned */
+    void* v;
+    uint8_t* k_scale;            /* device, 4-byte aligned, e4m3 only */
+    uint8_t* v_scale;
+    int64_t page_stride;         /* elements */
+    int64_t scale_page_stride;   /* bytes, e4m3 only */
+    int32_t num_pages, page_size, local_kv_heads, head_dim;
+    hspmd_cache_dtype dtype;
+} hspmd_kv_cache;
+
+/*
+ * The rows of one call.  Sequence s brings the packed rows cu_rows[s] .. cu_rows[s+1]-1 of the call's tensors and has kv_lens[s]
+ * tokens in the cache, these rows' own included: row r of n sits at position kv_lens[s] - n + r.  Token p of the sequence
+ * lies in slot p % page_size of page page_table[s * table_width + p / page_size].
+ * All three arrays are DEVICE memory and are read when the kernels run: a captured graph replays with the lengths and pages
+ * that it finds there.  The host therefore cannot check them; the kernels do, and no value in them leads out of the pool or the
+ * tensors: rows of a sequence are clamped to 0 .. total_rows, its length to table_width * page_size.
+ * A row whose position is negative (n > kv_lens[s]) has no place in the cache: a write skips it, a read gives zeros, the
+ * attention gives O = 0 and LSE = -inf.  A page number outside 0 .. num_pages-1 is not followed: a write skips the row, a read
+ * gives NaN, the attention gives NaN to rows that would see a key of that page.  Rows that belong to no sequence (behind
+ * cu_rows[num_seqs], for a batch that is padded to a fixed size) are left as they were.
+ */
+typedef struct {
+    const int32_t* cu_rows;      /* device, [num_seqs + 1], non-decreasing */
+    const int32_t* kv_lens;      /* device, [num_seqs] */
+    const int32_t* page_table;   /* device, [num_seqs, table_width] */
+    int32_t num_seqs, table_width;
+    int32_t total_rows;          /* rows of the call's tensors, >= cu_rows[num_seqs] */
+    int32_t max_rows;            /* the most rows of a sequence (0: unknown).  Chooses the attention's kernels; a sequence with more is
+                                    computed all the same, slower */
+} hspmd_kv_batch;
+
+int32_t hspmd_kv_cache_row(int32_t head_dim, hspmd_cache_dtype dtype);   /* 0 on bad arguments */
+
+/*
+ * Writes the batch's rows of k and v into their places, turning k on the way (rope != NULL) and quantising.
+ *   k, v     bf16 [total_rows, local_kv_heads, head_dim], strides as in hspmd_attn_varlen_fwd
+ *   rope     NULL: k is written as it is.  Otherwise positions may be NULL: every axis of a row then stands at the row's position
+ *            in its sequence (a row without a place stands at none: its q becomes NaN).  k is turned in fp32 and rounded once, to the cache's type
+ *   q, q_out with rope: bf16 [total_rows, local_q_heads, head_dim], turned in the same launch (in place allowed); both NULL: k only.
+ *            Without rope both have to be NULL
+ * Two rows of one call must not have the same place.
+ */
+hspmd_status hspmd_kv_cache_write(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, const void* k, const void* v,
+                                  int64_t kv_token_stride, const hspmd_rope_axes* rope, const void* q, void* q_out,
+                                  int64_t q_token_stride, int64_t q_out_token_stride, int32_t local_q_heads, void* stream);
+
+/*
+ * Reads the batch's rows back: k, v bf16 [total_rows, local_kv_heads, head_dim] (token stride kv_token_stride), the values exactly.
+ * kv_lens[s] = n gives a sequence's first n tokens, packed as hspmd_attn_varlen_fwd and hspmd_attn_block_fwd take them.
+ */
+hspmd_status hspmd_kv_cache_read(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, void* k, void* v,
+                                 int64_t kv_token_stride, void* stream);
+
+/*
+ * Attention of the batch's rows over the cache (their own keys and values have been written before): the row at position p
+ * sees the keys at positions 0 .. p of its sequence.
+ *   q    bf16 [total_rows, local_q_heads, head_dim], 16-byte aligned, token stride as in hspmd_attn_varlen_fwd; local_q_heads a multiple of
+ *        the cache's heads, grouped as everywhere
+ *   o    bf16 [total_rows, local_q_heads, head_dim], contiguous, written; lse fp32 [local_q_heads, total_rows], written, may be NULL
+ *   workspace  device, at least hspmd_attn_paged_workspace_bytes(cache, batch, local_q_heads) bytes, 16-byte aligned: partial results where
+ *        the keys of a row are shared out.  The size follows from num_seqs, table_width, total_rows and the heads, never less for more of
+ *        any; nothing in it outlives the call.
+ * softmax_scale as in hspmd_attn_varlen_fwd.  No atomics: results are run-to-run bit-identical.
+ * Errors of the calls above: INVALID_ARG for NULL / misaligned pointers, bad strides, counts or page sizes; UNSUPPORTED for a head_dim
+ * outside the supported set or an unknown dtype; WORKSPACE_TOO_SMALL.  Nothing is launched on error; total_rows == 0 or num_seqs == 0
+ * returns OK without launching.
+ */
+size_t hspmd_attn_paged_workspace_bytes(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, int32_t local_q_heads);
+hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, const void* q, int64_t q_token_stride,
+                                  int32_t local_q_heads, float softmax_scale, void* o, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
+/*
  * Per-kernel timing for measurement (the evidence the kernels are tuned against; not part of
  * the paper's method).  While enabled, every kernel launch made by forward / backward on the
  * calling process is bracketed by a pair of HIP events recorded on the launch stream.

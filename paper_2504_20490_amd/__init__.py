@@ -11,4 +11,6 @@ from .binding import (  # noqa: F401
     BlockPlan, block_schedule, attn_block_fwd, attn_merge, attn_block_bwd, estimate_ms,
     rope_table_bytes, rope_table, rope_qk, attn_varlen_bwd_rope, attn_block_bwd_rope,
     attn_varlen_bwd_static_ws, STATIC_WORKSPACE_BYTES, probe_mfma_rate, PROBE_MODES,
+    RopeAxes, rope_axes_qk, CACHE_BF16, CACHE_E4M3, KVCache, KVBatch, kv_cache_row, kv_cache_write, kv_cache_read,
+    attn_paged_workspace_bytes, attn_paged_fwd,
 )

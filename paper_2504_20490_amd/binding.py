@@ -34,6 +34,24 @@ class BlockItem(ctypes.Structure):
                 ("head", ctypes.c_int32), ("q_pos", ctypes.c_int32)]
 
 
+class _RopeAxesArgs(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_positions", ctypes.c_int32), ("num_axes", ctypes.c_int32),
+                ("positions", ctypes.c_void_p), ("positions_stride", ctypes.c_int64), ("pair_axis", ctypes.c_char_p)]
+
+
+class _KVCacheArgs(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("scale_page_stride", ctypes.c_int64), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("local_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int)]
+
+
+class _KVBatchArgs(ctypes.Structure):
+    _fields_ = [("cu_rows", ctypes.c_void_p), ("kv_lens", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("num_seqs", ctypes.c_int32), ("table_width", ctypes.c_int32), ("total_rows", ctypes.c_int32),
+                ("max_rows", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -130,6 +148,20 @@ def load_library():
     lib.hspmd_attn_block_bwd.restype = ctypes.c_int
     lib.hspmd_attn_block_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, ctypes.c_int64, ctypes.c_int64, ctypes.c_float,
                                          vp, ctypes.c_int32, vp, vp, ctypes.c_int32, vp, ctypes.c_size_t, vp]
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    axes_p, cache_p, batch_p = (ctypes.POINTER(c) for c in (_RopeAxesArgs, _KVCacheArgs, _KVBatchArgs))
+    lib.hspmd_rope_axes_qk.restype = ctypes.c_int
+    lib.hspmd_rope_axes_qk.argtypes = [axes_p, vp, vp, i64, i64, vp, vp, i64, i64, i32, i32, i32, i32, ctypes.c_int, i32, vp]
+    lib.hspmd_kv_cache_row.restype = i32
+    lib.hspmd_kv_cache_row.argtypes = [i32, ctypes.c_int]
+    lib.hspmd_kv_cache_write.restype = ctypes.c_int
+    lib.hspmd_kv_cache_write.argtypes = [cache_p, batch_p, vp, vp, i64, axes_p, vp, vp, i64, i64, i32, vp]
+    lib.hspmd_kv_cache_read.restype = ctypes.c_int
+    lib.hspmd_kv_cache_read.argtypes = [cache_p, batch_p, vp, vp, i64, vp]
+    lib.hspmd_attn_paged_workspace_bytes.restype = ctypes.c_size_t
+    lib.hspmd_attn_paged_workspace_bytes.argtypes = [cache_p, batch_p, i32]
+    lib.hspmd_attn_paged_fwd.restype = ctypes.c_int
+    lib.hspmd_attn_paged_fwd.argtypes = [cache_p, batch_p, vp, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
     lib.hspmd_probe_scratch_bytes.restype = ctypes.c_size_t
     lib.hspmd_probe_scratch_bytes.argtypes = []
     lib.hspmd_probe_mfma_tflops.restype = ctypes.c_int
@@ -492,3 +524,204 @@ def estimate_ms(cu_seqlens: Sequence[int], q_heads: int, kv_heads: int, head_dim
     _check(load_library().hspmd_attn_estimate_ms(_ptr32(cu), len(cu) - 1, q_heads, kv_heads, head_dim,
                                                  ctypes.byref(f), ctypes.byref(b)))
     return float(f.value), float(b.value)
+
+
+# ------------------------------------------------- rotary embedding with several axes, paged key/value cache
+CACHE_BF16, CACHE_E4M3 = 0, 1
+
+
+def _bad(what: str):
+    return HspmdError(1, what)
+
+
+def _device_tensors(*tensors) -> None:
+    """All given tensors lie on the current GPU: the calls enqueue on a stream of that device."""
+    import torch
+    here = torch.cuda.current_device() if torch.cuda.is_available() else None
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.get_device() != here):
+            raise _bad("every tensor has to be on the current GPU")
+
+
+def _rows_stride(x, heads: int, head_dim: int, dtype, what: str, tokens: Optional[int] = None) -> int:
+    """The token stride of a [T, heads, head_dim] tensor of the given type whose rows are contiguous."""
+    if x.dtype != dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or (tokens is not None and x.shape[0] != tokens):
+        raise _bad(f"{what} has to be [{'T' if tokens is None else tokens}, {heads}, {head_dim}] of {dtype}")
+    if x.numel() and (x.stride(2) != 1 and head_dim > 1 or x.stride(1) != head_dim and heads > 1):
+        raise _bad(f"{what}: the heads of a token have to be contiguous")
+    return _token_stride(x, heads, head_dim)
+
+
+class RopeAxes:
+    """The rotation of hspmd_rope_axes: a table of rope_table's, and per token one position on each axis.
+
+    positions: device int32 [num_axes, T] or [T]; None where the tokens' own positions are meant (kv_cache_write).
+    pair_axis: for every pair of columns the axis that it belongs to; None: one axis."""
+
+    def __init__(self, table, table_positions: int, positions=None, pair_axis: Optional[Sequence[int]] = None):
+        import torch
+        a = _RopeAxesArgs()
+        if table.dtype != torch.float32 or not table.is_contiguous():
+            raise _bad("the rope table has to be a contiguous fp32 tensor")
+        self.table, self.positions = table, positions              # (kept alive)
+        self.pairs, self.tokens = table.numel() // 2 // max(int(table_positions), 1), None
+        axes = 1
+        if positions is not None:
+            if positions.dtype != torch.int32 or positions.dim() not in (1, 2) or (positions.numel() > 1 and positions.stride(-1) != 1):
+                raise _bad("positions has to be int32 [num_axes, T] with contiguous rows")
+            self.tokens = positions.shape[-1]
+            if positions.dim() == 2:
+                axes, a.positions_stride = positions.shape[0], positions.stride(0) if positions.shape[0] > 1 else positions.shape[1]
+            a.positions = positions.data_ptr() or None
+        if pair_axis is not None:
+            if any(not 0 <= int(x) < 256 for x in pair_axis):
+                raise _bad("pair_axis names an axis that does not exist")
+            self.pair_axis = bytes(int(x) for x in pair_axis)
+            a.pair_axis = self.pair_axis
+            axes = max(axes, 1 + max(self.pair_axis, default=0)) if positions is None else axes
+        self.has_pairs = None if pair_axis is None else len(self.pair_axis)
+        a.table, a.table_positions, a.num_axes = table.data_ptr(), int(table_positions), axes
+        self._args = a
+
+    def _check(self, head_dim: int, tokens: Optional[int]) -> None:
+        if self.pairs < head_dim // 2:
+            raise _bad("rope table tensor is too small")
+        if self.has_pairs is not None and self.has_pairs != head_dim // 2:
+            raise _bad("pair_axis has to have head_dim / 2 entries")
+        if tokens is not None and self.tokens is not None and self.tokens < tokens:
+            raise _bad("positions has fewer tokens than the tensors")
+        _device_tensors(self.table, self.positions)
+
+
+def rope_axes_qk(rope: RopeAxes, q, k, q_out, k_out, inverse: bool = False, stream=None) -> None:
+    """q_out, k_out = q, k turned by each token's positions (inverse: turned back, as gradients are); bf16 or fp32 [T, heads, head_dim],
+    in place where q_out is q and k_out is k.  k and k_out may be None."""
+    import torch
+    T, hq, d = q.shape
+    if q.dtype not in (torch.bfloat16, torch.float32):
+        raise _bad("q has to be bf16 or fp32")
+    if (k is None) != (k_out is None):
+        raise _bad("k and k_out go together")
+    hkv = 0 if k is None else k.shape[1]
+    strides = [_rows_stride(x, h, d, q.dtype, what, T) if x is not None else 0
+               for x, h, what in ((q, hq, "q"), (k, hkv, "k"), (q_out, hq, "q_out"), (k_out, hkv, "k_out"))]
+    rope._check(d, T)
+    _device_tensors(q, k, q_out, k_out)
+    _check(load_library().hspmd_rope_axes_qk(ctypes.byref(rope._args), _dev_ptr(q), _opt_ptr(k), strides[0], strides[1], _dev_ptr(q_out),
+                                             _opt_ptr(k_out), strides[2], strides[3], T, hq, hkv, d,
+                                             GRAD_F32 if q.dtype == torch.float32 else GRAD_BF16, 1 if inverse else 0,
+                                             _stream_handle(stream)))
+
+
+def kv_cache_row(head_dim: int, dtype: int) -> int:
+    """Elements of a cached row: head_dim, for CACHE_E4M3 rounded up to a multiple of 16."""
+    return int(load_library().hspmd_kv_cache_row(int(head_dim), int(dtype)))
+
+
+class KVCache:
+    """The pool of pages: k, v [num_pages, kv_heads, page_size, row], bf16 or float8_e4m3fn (then with k_scale, v_scale uint8
+    [num_pages, kv_heads, page_size]); everything but the pages' stride contiguous.  head_dim: where it is less than row."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None, head_dim: Optional[int] = None):
+        import torch
+        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+            raise _bad("the cache has to be bf16 or float8_e4m3fn")
+        e4m3 = k.dtype == torch.float8_e4m3fn
+        if e4m3 != (k_scale is not None) or e4m3 != (v_scale is not None):
+            raise _bad("an e4m3 cache has scales, a bf16 cache has none")
+        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+            raise _bad("k and v have to be [num_pages, kv_heads, page_size, row], alike")
+        pages, heads, size, row = k.shape
+        for x, inner in ((k, (size * row, row, 1)), (v, (size * row, row, 1)), (k_scale, (size, 1)), (v_scale, (size, 1))):
+            if x is None:
+                continue
+            if len(inner) == 2 and (x.dtype != torch.uint8 or tuple(x.shape) != (pages, heads, size)):
+                raise _bad("scales have to be uint8 [num_pages, kv_heads, page_size]")
+            if any(x.stride(i + 1) != s and x.shape[i + 1] > 1 for i, s in enumerate(inner)):
+                raise _bad("a page's heads, rows and columns have to be contiguous")
+        strides = [x.stride(0) if pages > 1 else heads * size * (row if x.dim() == 4 else 1) for x in (k, v, k_scale, v_scale) if x is not None]
+        if strides[0] != strides[1] or strides[2:3] != strides[3:]:
+            raise _bad("k and v have to have the same page stride")
+        self.tensors = (k, v, k_scale, v_scale)                    # (kept alive)
+        self.head_dim, self.kv_heads, self.row = row if head_dim is None else int(head_dim), heads, row
+        self.dtype = CACHE_E4M3 if e4m3 else CACHE_BF16
+        if row != (self.head_dim if not e4m3 else (self.head_dim + 15) // 16 * 16):
+            raise _bad("the cache's row does not fit head_dim")
+        self._args = _KVCacheArgs(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if e4m3 else None, v_scale.data_ptr() if e4m3 else None,
+                                  strides[0], strides[2] if e4m3 else 0, pages, size, heads, self.head_dim, self.dtype)
+
+
+class KVBatch:
+    """The rows of a call: device int32 cu_rows [num_seqs + 1], kv_lens [num_seqs], page_table [num_seqs, table_width]; max_rows: the
+    most rows of a sequence (0: unknown).  The calls read them when their kernels run."""
+
+    def __init__(self, cu_rows, kv_lens, page_table, max_rows: int = 0):
+        import torch
+        n = kv_lens.numel()
+        if any(x.dtype != torch.int32 or not x.is_contiguous() for x in (cu_rows, kv_lens, page_table)):
+            raise _bad("cu_rows, kv_lens and page_table have to be contiguous int32 tensors")
+        if cu_rows.numel() != n + 1 or page_table.dim() != 2 or page_table.shape[0] != n:
+            raise _bad("cu_rows has to have one entry more than kv_lens, page_table as many rows")
+        self.tensors = (cu_rows, kv_lens, page_table)              # (kept alive)
+        self._args = _KVBatchArgs(cu_rows.data_ptr(), kv_lens.data_ptr() or None, page_table.data_ptr() or None, n, page_table.shape[1],
+                                  0, int(max_rows))
+
+    def _with_rows(self, rows: int) -> _KVBatchArgs:
+        a = _KVBatchArgs.from_buffer_copy(self._args)
+        a.total_rows = rows
+        return a
+
+
+def kv_cache_write(cache: KVCache, batch: KVBatch, k, v, rope: Optional[RopeAxes] = None, q=None, q_out=None, stream=None) -> None:
+    """Writes k, v (bf16 [T, kv_heads, head_dim]) into their places, k turned by `rope` (positions None: the rows' own); q, if given, is
+    turned into q_out in the same launch."""
+    import torch
+    d, bf16 = cache.head_dim, torch.bfloat16
+    T = k.shape[0]
+    stride = _rows_stride(k, cache.kv_heads, d, bf16, "k")
+    if _rows_stride(v, cache.kv_heads, d, bf16, "v", T) != stride:
+        raise _bad("k and v have to have the same token stride")
+    if (q is None) != (q_out is None):
+        raise _bad("q and q_out go together")
+    hq = 0 if q is None else q.shape[1]
+    qs, qos = (0, 0) if q is None else (_rows_stride(q, hq, d, bf16, "q", T), _rows_stride(q_out, hq, d, bf16, "q_out", T))
+    if rope is not None:
+        rope._check(d, T)
+    _device_tensors(*cache.tensors, *batch.tensors, k, v, q, q_out)
+    _check(load_library().hspmd_kv_cache_write(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(T)), _dev_ptr(k), _dev_ptr(v), stride,
+                                               None if rope is None else ctypes.byref(rope._args), _opt_ptr(q), _opt_ptr(q_out), qs, qos, hq,
+                                               _stream_handle(stream)))
+
+
+def kv_cache_read(cache: KVCache, batch: KVBatch, k, v, stream=None) -> None:
+    """Reads the batch's rows back into k, v (bf16 [T, kv_heads, head_dim])."""
+    import torch
+    stride = _rows_stride(k, cache.kv_heads, cache.head_dim, torch.bfloat16, "k")
+    if _rows_stride(v, cache.kv_heads, cache.head_dim, torch.bfloat16, "v", k.shape[0]) != stride:
+        raise _bad("k and v have to have the same token stride")
+    _device_tensors(*cache.tensors, *batch.tensors, k, v)
+    _check(load_library().hspmd_kv_cache_read(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(k.shape[0])), _dev_ptr(k), _dev_ptr(v),
+                                              stride, _stream_handle(stream)))
+
+
+def attn_paged_workspace_bytes(cache: KVCache, batch: KVBatch, total_rows: int, q_heads: int) -> int:
+    return int(load_library().hspmd_attn_paged_workspace_bytes(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(int(total_rows))),
+                                                               int(q_heads)))
+
+
+def attn_paged_fwd(cache: KVCache, batch: KVBatch, q, o, lse, workspace, softmax_scale: float = 0.0, stream=None) -> None:
+    """Attention of the rows q (bf16 [T, q_heads, head_dim]) over their sequences' cached keys and values; o bf16 like q, contiguous, and lse
+    fp32 [q_heads, T] (may be None) are written; workspace: any device tensor of attn_paged_workspace_bytes(...) bytes."""
+    import torch
+    T, hq, d = q.shape
+    stride = _rows_stride(q, hq, cache.head_dim, torch.bfloat16, "q")
+    if o.shape != q.shape or o.dtype != torch.bfloat16 or not o.is_contiguous():
+        raise _bad("o has to be a contiguous bf16 tensor of q's shape")
+    if lse is not None and (tuple(lse.shape) != (hq, T) or lse.dtype != torch.float32 or not lse.is_contiguous()):
+        raise _bad("lse has to be a contiguous fp32 tensor [q_heads, T]")
+    if not workspace.is_contiguous():
+        raise _bad("the workspace has to be contiguous")
+    _device_tensors(*cache.tensors, *batch.tensors, q, o, lse, workspace)
+    _check(load_library().hspmd_attn_paged_fwd(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(T)), _dev_ptr(q), stride, hq,
+                                               float(softmax_scale), _dev_ptr(o), _opt_ptr(lse), _dev_ptr(workspace),
+                                               workspace.numel() * workspace.element_size(), _stream_handle(stream)))

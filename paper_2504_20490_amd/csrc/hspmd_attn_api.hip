@@ -15,6 +15,7 @@
 
 #include "../../include/hspmd_attn.h"
 #include "kernels.hpp"
+#include "paged.hpp"
 #include "schedule.hpp"
 
 namespace hspmd {
@@ -1100,6 +1101,239 @@ hspmd_status hspmd_attn_block_bwd_rope(const hspmd_attn_plan* plan, const void* 
     if (hspmd_status rc = check_rope_table(plan, table, table_positions)) return rc;
     return block_bwd(plan, q, k, v, o, lse, d_o, q_token_stride, kv_token_stride, softmax_scale, dq, dq_accumulate, dk, dv,
                      reuse_statistics, table, workspace, workspace_bytes, stream);
+}
+
+// ---- rotary embedding with several axes, paged cache ------------------------------------------------------------
+
+// Rows of a call: a launch has one wave per row (and head) at most, and a grid holds fewer than 2^32 threads
+static constexpr int64_t kMaxRows = (int64_t)1 << 25, kMaxRowHeads = (int64_t)1 << 25;
+
+static hspmd_status check_stride(int64_t stride, int64_t heads, int32_t head_dim, const char* what) {
+    if (stride < heads * head_dim || stride % 8 != 0)
+        return fail(HSPMD_ERR_INVALID_ARG, std::string(what) + " must be a multiple of 8 and >= heads*head_dim");
+    return HSPMD_OK;
+}
+
+// `own_positions`: positions may be NULL (a row then stands at its position in its sequence)
+static hspmd_status check_axes(const hspmd_rope_axes* rope, int32_t head_dim, int64_t tokens, bool own_positions, hspmd::AxesParams* out) {
+    if (!rope) return fail(HSPMD_ERR_INVALID_ARG, "rope is NULL");
+    if (!rope->table || !aligned16(rope->table)) return fail(HSPMD_ERR_INVALID_ARG, "rope table must be non-NULL and 16-byte aligned");
+    if (rope->table_positions < 0) return fail(HSPMD_ERR_INVALID_ARG, "table_positions is negative");
+    if (rope->num_axes < 1 || rope->num_axes > 4) return fail(HSPMD_ERR_INVALID_ARG, "num_axes must be 1 .. 4");
+    if (!rope->positions && !own_positions) return fail(HSPMD_ERR_INVALID_ARG, "positions is NULL");
+    if (rope->positions && rope->num_axes > 1 && rope->positions_stride < tokens)
+        return fail(HSPMD_ERR_INVALID_ARG, "positions_stride is below the number of tokens");
+    if (reinterpret_cast<uintptr_t>(rope->positions) & 3u) return fail(HSPMD_ERR_INVALID_ARG, "positions must be 4-byte aligned");
+    *out = hspmd::AxesParams{};
+    out->table = rope->table;
+    out->table_positions = rope->table_positions;
+    out->num_axes = rope->num_axes;
+    out->positions = rope->positions;
+    out->positions_stride = rope->positions_stride;
+    for (int i = 0; rope->pair_axis && i < head_dim / 2; ++i) {
+        if (rope->pair_axis[i] >= rope->num_axes) return fail(HSPMD_ERR_INVALID_ARG, "pair_axis names an axis that does not exist");
+        out->axis_of[i / 32] |= (uint64_t)rope->pair_axis[i] << (i % 32 * 2);
+    }
+    return HSPMD_OK;
+}
+
+hspmd_status hspmd_rope_axes_qk(const hspmd_rope_axes* rope, const void* q, const void* k, int64_t q_token_stride,
+                                int64_t kv_token_stride, void* q_out, void* k_out, int64_t q_out_token_stride,
+                                int64_t kv_out_token_stride, int32_t total_tokens, int32_t local_q_heads, int32_t local_kv_heads,
+                                int32_t head_dim, hspmd_grad_dtype dtype, int32_t inverse, void* stream) {
+    if (dtype != HSPMD_GRAD_BF16 && dtype != HSPMD_GRAD_F32) return fail(HSPMD_ERR_UNSUPPORTED, "dtype must be bf16 or fp32");
+    if (!supported_head_dim(head_dim)) return fail(HSPMD_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 between 8 and 128");
+    if (total_tokens < 0 || total_tokens > kMaxRows) return fail(HSPMD_ERR_INVALID_ARG, "total_tokens must be 0 .. 2^25");
+    if (local_q_heads < 1 || local_kv_heads < 0 || local_q_heads > (1 << 16) || local_kv_heads > (1 << 16))
+        return fail(HSPMD_ERR_INVALID_ARG, "local_q_heads must be 1 .. 65536, local_kv_heads 0 .. 65536");
+    if (total_tokens == 0) return HSPMD_OK;
+    hspmd::RopeAxesParams p{};
+    if (hspmd_status rc = check_axes(rope, head_dim, total_tokens, false, &p.rope)) return rc;
+    const bool keys = local_kv_heads > 0;
+    if (!q || !q_out || (keys && (!k || !k_out))) return fail(HSPMD_ERR_INVALID_ARG, "null tensor pointer");
+    if (!aligned16(q) || !aligned16(q_out) || (keys && (!aligned16(k) || !aligned16(k_out))))
+        return fail(HSPMD_ERR_INVALID_ARG, "q, k, q_out, k_out must be 16-byte aligned");
+    if (hspmd_status rc = check_stride(q_token_stride, local_q_heads, head_dim, "q_token_stride")) return rc;
+    if (hspmd_status rc = check_stride(q_out_token_stride, local_q_heads, head_dim, "q_out_token_stride")) return rc;
+    if (keys) {
+        if (hspmd_status rc = check_stride(kv_token_stride, local_kv_heads, head_dim, "kv_token_stride")) return rc;
+        if (hspmd_status rc = check_stride(kv_out_token_stride, local_kv_heads, head_dim, "kv_out_token_stride")) return rc;
+    }
+    p.q = q;
+    p.k = k;
+    p.q_out = q_out;
+    p.k_out = k_out;
+    p.q_stride = q_token_stride;
+    p.kv_stride = kv_token_stride;
+    p.q_out_stride = q_out_token_stride;
+    p.kv_out_stride = kv_out_token_stride;
+    p.tokens = total_tokens;
+    p.q_heads = local_q_heads;
+    p.kv_heads = local_kv_heads;
+    p.head_dim = head_dim;
+    p.sin_sign = inverse ? -1.f : 1.f;
+    const hipError_t e = hspmd::launch_rope_axes(p, dtype == HSPMD_GRAD_F32, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip(e, "rope launch (axes)");
+    return HSPMD_OK;
+}
+
+int32_t hspmd_kv_cache_row(int32_t head_dim, hspmd_cache_dtype dtype) {
+    if (!supported_head_dim(head_dim) || (dtype != HSPMD_CACHE_BF16 && dtype != HSPMD_CACHE_E4M3)) return 0;
+    return dtype == HSPMD_CACHE_BF16 ? head_dim : (head_dim + 15) / 16 * 16;
+}
+
+// what can be checked of the pool and the rows without reading device memory; `idle`: there is nothing to do
+static hspmd_status check_cache(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, hspmd::PagedPool* pool, hspmd::PagedRows* rows,
+                                bool* idle, bool pointers = true) {
+    if (!cache) return fail(HSPMD_ERR_INVALID_ARG, "cache is NULL");
+    if (!batch) return fail(HSPMD_ERR_INVALID_ARG, "batch is NULL");
+    if (cache->dtype != HSPMD_CACHE_BF16 && cache->dtype != HSPMD_CACHE_E4M3) return fail(HSPMD_ERR_UNSUPPORTED, "cache dtype must be bf16 or e4m3");
+    if (!supported_head_dim(cache->head_dim)) return fail(HSPMD_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 between 8 and 128");
+    const bool e4m3 = cache->dtype == HSPMD_CACHE_E4M3;
+    const int bytes = e4m3 ? 1 : 2;
+    if (cache->local_kv_heads < 1 || cache->local_kv_heads > (1 << 16)) return fail(HSPMD_ERR_INVALID_ARG, "local_kv_heads must be 1 .. 65536");
+    if (cache->num_pages < 1) return fail(HSPMD_ERR_INVALID_ARG, "the cache has no page");
+    if (cache->page_size < 16 || cache->page_size > 1024 || (cache->page_size & (cache->page_size - 1)))
+        return fail(HSPMD_ERR_INVALID_ARG, "page_size must be a power of two between 16 and 1024");
+    const int32_t row = hspmd_kv_cache_row(cache->head_dim, cache->dtype);
+    const int64_t tokens = (int64_t)cache->local_kv_heads * cache->page_size;
+    if (cache->page_stride < tokens * row || cache->page_stride * bytes % 16 != 0)
+        return fail(HSPMD_ERR_INVALID_ARG, "page_stride must be a multiple of 16 bytes and hold the heads' page_size rows");
+    if (pointers) {
+        if (!cache->k || !cache->v || !aligned16(cache->k) || !aligned16(cache->v))
+            return fail(HSPMD_ERR_INVALID_ARG, "the cache's k and v must be non-NULL and 16-byte aligned");
+        if (e4m3) {
+            if (!cache->k_scale || !cache->v_scale || ((reinterpret_cast<uintptr_t>(cache->k_scale) | reinterpret_cast<uintptr_t>(cache->v_scale)) & 3u))
+                return fail(HSPMD_ERR_INVALID_ARG, "the cache's k_scale and v_scale must be non-NULL and 4-byte aligned");
+        }
+    }
+    if (e4m3 && (cache->scale_page_stride < tokens || cache->scale_page_stride % 4 != 0))
+        return fail(HSPMD_ERR_INVALID_ARG, "scale_page_stride must be a multiple of 4 and hold the heads' page_size scales");
+    if (batch->num_seqs < 0 || batch->table_width < 0 || batch->max_rows < 0) return fail(HSPMD_ERR_INVALID_ARG, "negative count in the batch");
+    if (batch->total_rows < 0 || batch->total_rows > kMaxRows) return fail(HSPMD_ERR_INVALID_ARG, "total_rows must be 0 .. 2^25");
+    *idle = batch->num_seqs == 0 || batch->total_rows == 0;
+    if (pointers && !*idle) {
+        if (!batch->cu_rows || !batch->kv_lens || (!batch->page_table && batch->table_width > 0))
+            return fail(HSPMD_ERR_INVALID_ARG, "null pointer in the batch");
+        if ((reinterpret_cast<uintptr_t>(batch->cu_rows) | reinterpret_cast<uintptr_t>(batch->kv_lens) | reinterpret_cast<uintptr_t>(batch->page_table)) & 3u)
+            return fail(HSPMD_ERR_INVALID_ARG, "the batch's arrays must be 4-byte aligned");
+    }
+    *pool = hspmd::PagedPool{};
+    pool->k = static_cast<uint8_t*>(cache->k);
+    pool->v = static_cast<uint8_t*>(cache->v);
+    pool->k_scale = cache->k_scale;
+    pool->v_scale = cache->v_scale;
+    pool->page_bytes = cache->page_stride * bytes;
+    pool->scale_page_bytes = cache->scale_page_stride;
+    pool->num_pages = cache->num_pages;
+    while ((1 << pool->page_shift) < cache->page_size) ++pool->page_shift;
+    pool->kv_heads = cache->local_kv_heads;
+    pool->head_dim = cache->head_dim;
+    pool->row_bytes = row * bytes;
+    *rows = hspmd::PagedRows{batch->cu_rows, batch->kv_lens, batch->page_table, batch->num_seqs, batch->table_width, batch->total_rows};
+    return HSPMD_OK;
+}
+
+hspmd_status hspmd_kv_cache_write(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, const void* k, const void* v,
+                                  int64_t kv_token_stride, const hspmd_rope_axes* rope, const void* q, void* q_out,
+                                  int64_t q_token_stride, int64_t q_out_token_stride, int32_t local_q_heads, void* stream) {
+    hspmd::CacheWriteParams p{};
+    bool idle = false;
+    if (hspmd_status rc = check_cache(cache, batch, &p.pool, &p.rows, &idle)) return rc;
+    if ((q == nullptr) != (q_out == nullptr)) return fail(HSPMD_ERR_INVALID_ARG, "q and q_out go together");
+    if (q && !rope) return fail(HSPMD_ERR_INVALID_ARG, "q is given and there is no rope to turn it by");
+    if (q && (local_q_heads < 1 || local_q_heads > (1 << 16))) return fail(HSPMD_ERR_INVALID_ARG, "local_q_heads must be 1 .. 65536");
+    if (idle) return HSPMD_OK;
+    if (!k || !v) return fail(HSPMD_ERR_INVALID_ARG, "null tensor pointer");
+    if (!aligned16(k) || !aligned16(v) || !aligned16(q) || !aligned16(q_out))
+        return fail(HSPMD_ERR_INVALID_ARG, "k, v, q, q_out must be 16-byte aligned");
+    const int32_t hd = cache->head_dim;
+    if (hspmd_status rc = check_stride(kv_token_stride, cache->local_kv_heads, hd, "kv_token_stride")) return rc;
+    if (q) {
+        if (hspmd_status rc = check_stride(q_token_stride, local_q_heads, hd, "q_token_stride")) return rc;
+        if (hspmd_status rc = check_stride(q_out_token_stride, local_q_heads, hd, "q_out_token_stride")) return rc;
+    }
+    if (rope) {
+        if (hspmd_status rc = check_axes(rope, hd, batch->total_rows, true, &p.rope)) return rc;
+    }
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.q = static_cast<const uint16_t*>(q);
+    p.q_out = static_cast<uint16_t*>(q_out);
+    p.kv_stride = kv_token_stride;
+    p.q_stride = q_token_stride;
+    p.q_out_stride = q_out_token_stride;
+    p.q_heads = q ? local_q_heads : 0;
+    const hipError_t e = hspmd::launch_cache_write(p, cache->dtype == HSPMD_CACHE_E4M3, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip(e, "cache write launch");
+    return HSPMD_OK;
+}
+
+hspmd_status hspmd_kv_cache_read(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, void* k, void* v,
+                                 int64_t kv_token_stride, void* stream) {
+    hspmd::CacheReadParams p{};
+    bool idle = false;
+    if (hspmd_status rc = check_cache(cache, batch, &p.pool, &p.rows, &idle)) return rc;
+    if (idle) return HSPMD_OK;
+    if (!k || !v) return fail(HSPMD_ERR_INVALID_ARG, "null tensor pointer");
+    if (!aligned16(k) || !aligned16(v)) return fail(HSPMD_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+    if (hspmd_status rc = check_stride(kv_token_stride, cache->local_kv_heads, cache->head_dim, "kv_token_stride")) return rc;
+    p.k = static_cast<uint16_t*>(k);
+    p.v = static_cast<uint16_t*>(v);
+    p.kv_stride = kv_token_stride;
+    const hipError_t e = hspmd::launch_cache_read(p, cache->dtype == HSPMD_CACHE_E4M3, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip(e, "cache read launch");
+    return HSPMD_OK;
+}
+
+// heads of the attention over the cache
+static hspmd_status check_paged_heads(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, int32_t local_q_heads) {
+    if (local_q_heads < 1 || local_q_heads % cache->local_kv_heads != 0)
+        return fail(HSPMD_ERR_INVALID_ARG, "local_q_heads must be a positive multiple of the cache's heads");
+    if ((int64_t)batch->total_rows * local_q_heads > kMaxRowHeads)
+        return fail(HSPMD_ERR_INVALID_ARG, "total_rows * local_q_heads must not exceed 2^25");
+    return HSPMD_OK;
+}
+
+size_t hspmd_attn_paged_workspace_bytes(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, int32_t local_q_heads) {
+    hspmd::PagedPool pool;
+    hspmd::PagedRows rows;
+    bool idle = false;
+    if (check_cache(cache, batch, &pool, &rows, &idle, /*pointers=*/false) || check_paged_heads(cache, batch, local_q_heads)) return 0;
+    return idle ? 0 : hspmd::paged_sizes(rows, pool.page_shift, local_q_heads, pool.kv_heads, pool.head_dim).total_bytes();
+}
+
+hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, const void* q, int64_t q_token_stride,
+                                  int32_t local_q_heads, float softmax_scale, void* o, float* lse, void* workspace,
+                                  size_t workspace_bytes, void* stream) {
+    hspmd::PagedAttnParams p{};
+    bool idle = false;
+    if (hspmd_status rc = check_cache(cache, batch, &p.pool, &p.rows, &idle)) return rc;
+    if (hspmd_status rc = check_paged_heads(cache, batch, local_q_heads)) return rc;
+    float scale = 0.f;
+    if (hspmd_status rc = resolve_scale(softmax_scale, cache->head_dim, &scale)) return rc;
+    if (idle) return HSPMD_OK;
+    if (!q || !o || !workspace) return fail(HSPMD_ERR_INVALID_ARG, "null tensor or workspace pointer");
+    if (!aligned16(q) || !aligned16(o) || !aligned16(workspace)) return fail(HSPMD_ERR_INVALID_ARG, "q, o, workspace must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(HSPMD_ERR_INVALID_ARG, "lse must be 4-byte aligned");
+    if (hspmd_status rc = check_stride(q_token_stride, local_q_heads, cache->head_dim, "q_token_stride")) return rc;
+    const hspmd::PagedSizes sizes = hspmd::paged_sizes(p.rows, p.pool.page_shift, local_q_heads, p.pool.kv_heads, p.pool.head_dim);
+    if (workspace_bytes < sizes.total_bytes()) return fail(HSPMD_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than hspmd_attn_paged_workspace_bytes");
+    p.q = static_cast<const uint16_t*>(q);
+    p.o = static_cast<uint16_t*>(o);
+    p.lse = lse;
+    p.q_stride = q_token_stride;
+    p.q_heads = local_q_heads;
+    p.group = local_q_heads / cache->local_kv_heads;
+    p.scale_log2 = scale * 1.4426950408889634f;
+    char* const ws = static_cast<char*>(workspace);
+    p.where = reinterpret_cast<int2*>(ws);
+    p.part_stats = reinterpret_cast<float2*>(ws + sizes.where_bytes);
+    p.part_o = reinterpret_cast<float*>(ws + sizes.where_bytes + sizes.stats_bytes);
+    p.part_rows = (int32_t)sizes.part_rows;
+    const hipError_t e = hspmd::launch_paged_attn(p, sizes, cache->dtype == HSPMD_CACHE_E4M3, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip(e, "paged attention launch");
+    return HSPMD_OK;
 }
 
 hspmd_status hspmd_profile_enable(int32_t on) {

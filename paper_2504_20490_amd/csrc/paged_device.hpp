@@ -1,0 +1,142 @@
+// Device code shared by the kernels around the paged cache: where a row is, rotation by a token's own positions,
+// 8-bit conversions.
+#pragma once
+#include "attn_device.hpp"
+#include "paged.hpp"
+
+namespace hspmd {
+
+// A row's sequence and position, and its place in the pool.  All values come from device arrays that nobody has checked: every
+// index that follows from them is bounded here.
+struct RowPlace {
+    int seq;        // -1: the row belongs to no sequence
+    int pos;        // position in the sequence; negative: no place
+    int page;       // page number, -1 where the table holds none that exists
+    int slot;       // slot in the page
+};
+
+// by a whole wave, the same row in every lane: the sequence s with cu_rows[s] <= row < cu_rows[s + 1]
+__device__ __forceinline__ int sequence_of(const PagedRows& b, int row) {
+    const int lane = threadIdx.x & 63;
+    for (int s0 = 0; s0 < b.num_seqs; s0 += 64) {
+        const int s = s0 + lane;
+        const bool ends_behind = s < b.num_seqs && b.cu_rows[s + 1] > row;
+        const uint64_t m = __ballot(ends_behind);
+        if (m != 0) {
+            const int found = s0 + __builtin_ctzll(m);
+            return b.cu_rows[found] <= row ? found : -1;
+        }
+    }
+    return -1;
+}
+
+__device__ __forceinline__ int kv_length(const PagedRows& b, int page_shift, int seq) {
+    const int64_t most = (int64_t)b.table_width << page_shift;
+    return (int)min((int64_t)max(b.kv_lens[seq], 0), min(most, (int64_t)0x7fffff00));
+}
+
+__device__ __forceinline__ int page_at(const PagedPool& pool, const PagedRows& b, int seq, int index) {
+    const int page = b.page_table[(int64_t)seq * b.table_width + index];
+    return (unsigned)page < (unsigned)pool.num_pages ? page : -1;
+}
+
+__device__ __forceinline__ RowPlace place_of(const PagedPool& pool, const PagedRows& b, int row) {
+    RowPlace r{sequence_of(b, row), -1, -1, 0};
+    if (r.seq < 0) return r;
+    const int kv = kv_length(b, pool.page_shift, r.seq);
+    const int pos = kv - (b.cu_rows[r.seq + 1] - row);   // (cu_rows[seq + 1] > row)
+    if (pos < 0) return r;
+    r.pos = pos;
+    r.page = page_at(pool, b, r.seq, pos >> pool.page_shift);
+    r.slot = pos & ((1 << pool.page_shift) - 1);
+    return r;
+}
+
+// (cos, sin) of VEC consecutive pairs from pair `first` on; `pos`: a token's position on each axis
+template <int VEC>
+__device__ __forceinline__ void load_turn(const AxesParams& a, const int (&pos)[4], int first, int half, float (&c)[VEC], float (&s)[VEC]) {
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+        const int i = first + j;
+        const int axis = (int)(a.axis_of[i >> 5] >> ((i & 31) * 2)) & 3;
+        const int at = axis == 0 ? pos[0] : axis == 1 ? pos[1] : axis == 2 ? pos[2] : pos[3];
+        float2 cs = make_float2(__builtin_nanf(""), __builtin_nanf(""));
+        if ((unsigned)at < (unsigned)a.table_positions) cs = *reinterpret_cast<const float2*>(a.table + ((int64_t)at * half + i) * 2);
+        c[j] = cs.x;
+        s[j] = cs.y;
+    }
+}
+
+// One pair turned.  Products and sums are rounded one by one (no fused multiply-add): the result then does not depend on how a
+// compiler contracts the expression, which matters where it is quantised next: a value at a rounding border, or a row maximum
+// at a power of two, comes out the same from any fp32 evaluation of the formula.
+__device__ __forceinline__ void turn_pair(float lo, float hi, float c, float s, float& out_lo, float& out_hi) {
+#pragma clang fp contract(off)
+    const float a = lo * c, b = hi * s, d = hi * c, e = lo * s;
+    out_lo = a - b;
+    out_hi = d + e;
+}
+
+// VEC consecutive elements, 2 or 4 bytes each, as floats and back
+template <int VEC, bool F32>
+__device__ __forceinline__ void load_floats(const void* base, int64_t elem, float (&x)[VEC]) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int j = 0; j < VEC; j += 4) {
+            const f32x4 t = *reinterpret_cast<const f32x4*>(static_cast<const float*>(base) + elem + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[j + e] = t[e];
+        }
+    } else {
+        using Raw = typename std::conditional<VEC == 8, u32x4, u32x2>::type;
+        const Raw t = *reinterpret_cast<const Raw*>(static_cast<const uint16_t*>(base) + elem);
+#pragma unroll
+        for (int j = 0; j < VEC / 2; ++j) {
+            x[2 * j] = __uint_as_float(t[j] << 16);
+            x[2 * j + 1] = __uint_as_float(t[j] & 0xffff0000u);
+        }
+    }
+}
+template <int VEC, bool F32>
+__device__ __forceinline__ void store_floats(void* base, int64_t elem, const float (&x)[VEC]) {
+    if constexpr (F32) {
+#pragma unroll
+        for (int j = 0; j < VEC; j += 4)
+            *reinterpret_cast<f32x4*>(static_cast<float*>(base) + elem + j) = f32x4{x[j], x[j + 1], x[j + 2], x[j + 3]};
+    } else {
+        using Raw = typename std::conditional<VEC == 8, u32x4, u32x2>::type;
+        Raw t;
+#pragma unroll
+        for (int j = 0; j < VEC / 2; ++j) t[j] = pack_bf16(x[2 * j], x[2 * j + 1]);
+        *reinterpret_cast<Raw*>(static_cast<uint16_t*>(base) + elem) = t;
+    }
+}
+
+// 2^e for -126 <= e <= 127
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// the scale that a stored byte stands for (bytes that the library writes: 27 .. 247)
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// smallest e >= -100 with amax <= 448 * 2^e (448 = 1.75 * 2^8, the largest e4m3 number); amax finite, >= 0
+__device__ __forceinline__ int e4m3_exponent(float amax) {
+    const uint32_t u = __float_as_uint(amax);
+    return max((int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u ? 1 : 0), -100);
+}
+
+__device__ __forceinline__ bool is_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) != 0x7f800000u; }
+
+// four floats, already in units of the scale, as e4m3 (round to nearest even)
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
+}
+
+// four e4m3 numbers times `scale` (a power of two) as bf16, exactly
+__device__ __forceinline__ u32x2 e4m3_to_bf16(uint32_t x, float scale) {
+    union { bf16x2 v; uint32_t u; } a, b;
+    a.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, false);
+    b.v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, scale, true);
+    return u32x2{a.u, b.u};
+}
+
+}  // namespace hspmd

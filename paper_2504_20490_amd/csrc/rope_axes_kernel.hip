@@ -1,0 +1,67 @@
+// Rotary embedding of q and k with positions given per token on up to four axes.
+//
+// HBM-bound: every element of q and k is read once and written once.  A wave (or several, where there are few tokens) takes one token and
+// walks its heads, those of q and then those of k; a lane owns VEC pairs of columns, so that their cosines and sines are fetched once
+// per token and stay in registers, whatever axes the pairs belong to.
+#include "paged_device.hpp"
+
+namespace hspmd {
+
+namespace {
+
+// VEC pairs of every head per lane; F32: fp32 tensors
+template <int VEC, bool F32>
+__global__ __launch_bounds__(kThreads) void rope_axes_kernel(RopeAxesParams p) {
+    const int lane = threadIdx.x & 63;
+    const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int token = (int)(unit / p.shares), share = (int)(unit % p.shares);
+    if (token >= p.tokens) return;
+    const int half = p.head_dim / 2, pieces = half / VEC, heads_at_once = 64 / pieces;
+    const int sub = lane / pieces, piece = lane % pieces;
+    if (sub >= heads_at_once) return;
+    int pos[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+        if (a < p.rope.num_axes) pos[a] = p.rope.positions[a * p.rope.positions_stride + token];
+    float c[VEC], s[VEC];
+    load_turn<VEC>(p.rope, pos, piece * VEC, half, c, s);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) s[j] *= p.sin_sign;
+    const int heads = p.q_heads + p.kv_heads;
+    for (int h0 = share * heads_at_once; h0 < heads; h0 += p.shares * heads_at_once) {
+        const int h = h0 + sub;
+        if (h >= heads) continue;
+        const bool is_k = h >= p.q_heads;
+        const void* src = is_k ? p.k : p.q;
+        void* dst = is_k ? p.k_out : p.q_out;
+        const int col = (is_k ? h - p.q_heads : h) * p.head_dim + piece * VEC;
+        const int64_t from = token * (is_k ? p.kv_stride : p.q_stride) + col, to = token * (is_k ? p.kv_out_stride : p.q_out_stride) + col;
+        float lo[VEC], hi[VEC];
+        load_floats<VEC, F32>(src, from, lo);
+        load_floats<VEC, F32>(src, from + half, hi);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) turn_pair(lo[j], hi[j], c[j], s[j], lo[j], hi[j]);
+        store_floats<VEC, F32>(dst, to, lo);
+        store_floats<VEC, F32>(dst, to + half, hi);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_rope_axes(RopeAxesParams p, bool f32, hipStream_t stream) {
+    if (p.tokens == 0) return hipSuccess;
+    const int half = p.head_dim / 2;
+    const int vec = !f32 && half % 8 == 0 ? 8 : 4;
+    const int heads_at_once = 64 / (half / vec);
+    const int rounds = (p.q_heads + p.kv_heads + heads_at_once - 1) / heads_at_once;
+    // enough waves for the device: 16 for each of 256 compute units
+    p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, (4096 + p.tokens - 1) / p.tokens));
+    const int64_t units = (int64_t)p.tokens * p.shares;
+    const dim3 grid((unsigned)((units + 3) / 4)), threads(kThreads);
+    if (f32) hipLaunchKernelGGL((rope_axes_kernel<4, true>), grid, threads, 0, stream, p);
+    else if (vec == 8) hipLaunchKernelGGL((rope_axes_kernel<8, false>), grid, threads, 0, stream, p);
+    else hipLaunchKernelGGL((rope_axes_kernel<4, false>), grid, threads, 0, stream, p);
+    return hipGetLastError();
+}
+
+}  // namespace hspmd
