@@ -8,8 +8,9 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIBRARY = os.path.join(HERE, "libhspmd_attn.so")
 SOURCES = ["hspmd_attn_api.hip", "schedule.cpp", "fwd_kernel.hip", "bwd_kernels.hip", "bwd_dkv_kernel.hip", "merge_kernel.hip", "probe.hip", "rope_kernel.hip",
-           "rope_axes_kernel.hip", "kv_cache_kernel.hip", "paged_attn_kernel.hip"]
-HEADERS = ["attn_device.hpp", "fwd_tiles.hpp", "kernels.hpp", "schedule.hpp", "paged.hpp", "paged_device.hpp", os.path.join("..", "..", "include", "hspmd_attn.h")]
+           "rope_axes_kernel.hip", "kv_cache_kernel.hip", "paged_attn_kernel.hip", "paged_many_kernel.hip"]
+HEADERS = ["attn_device.hpp", "fwd_iteration.hpp", "fwd_tiles.hpp", "kernels.hpp", "schedule.hpp", "paged.hpp", "paged_device.hpp", "paged_index.hpp",
+           "paged_item.hpp", os.path.join("..", "..", "include", "hspmd_attn.h")]
 
 # Packed fp32 VALU forms are switched off for all device code of this library.
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
@@ -17,7 +18,7 @@ HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
 
 
 # what decides a kernel's HBM traffic: the attention kernels, their shared device code and the launch order
-KERNEL_SOURCES = ["fwd_kernel.hip", "bwd_kernels.hip", "bwd_dkv_kernel.hip", "attn_device.hpp", "fwd_tiles.hpp", "kernels.hpp",
+KERNEL_SOURCES = ["fwd_kernel.hip", "bwd_kernels.hip", "bwd_dkv_kernel.hip", "attn_device.hpp", "fwd_iteration.hpp", "fwd_tiles.hpp", "kernels.hpp",
                   "schedule.hpp", "schedule.cpp"]
 
 

@@ -1300,7 +1300,7 @@ size_t hspmd_attn_paged_workspace_bytes(const hspmd_kv_cache* cache, const hspmd
     hspmd::PagedRows rows;
     bool idle = false;
     if (check_cache(cache, batch, &pool, &rows, &idle, /*pointers=*/false) || check_paged_heads(cache, batch, local_q_heads)) return 0;
-    return idle ? 0 : hspmd::paged_sizes(rows, pool.page_shift, local_q_heads, pool.kv_heads, pool.head_dim).total_bytes();
+    return idle ? 0 : hspmd::paged_sizes(rows, batch->max_rows, pool.page_shift, local_q_heads, pool.kv_heads, pool.head_dim).total_bytes();
 }
 
 hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_batch* batch, const void* q, int64_t q_token_stride,
@@ -1317,7 +1317,7 @@ hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_ba
     if (!aligned16(q) || !aligned16(o) || !aligned16(workspace)) return fail(HSPMD_ERR_INVALID_ARG, "q, o, workspace must be 16-byte aligned");
     if (reinterpret_cast<uintptr_t>(lse) & 3u) return fail(HSPMD_ERR_INVALID_ARG, "lse must be 4-byte aligned");
     if (hspmd_status rc = check_stride(q_token_stride, local_q_heads, cache->head_dim, "q_token_stride")) return rc;
-    const hspmd::PagedSizes sizes = hspmd::paged_sizes(p.rows, p.pool.page_shift, local_q_heads, p.pool.kv_heads, p.pool.head_dim);
+    const hspmd::PagedSizes sizes = hspmd::paged_sizes(p.rows, batch->max_rows, p.pool.page_shift, local_q_heads, p.pool.kv_heads, p.pool.head_dim);
     if (workspace_bytes < sizes.total_bytes()) return fail(HSPMD_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than hspmd_attn_paged_workspace_bytes");
     p.q = static_cast<const uint16_t*>(q);
     p.o = static_cast<uint16_t*>(o);
@@ -1330,7 +1330,9 @@ hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_ba
     p.where = reinterpret_cast<int2*>(ws);
     p.part_stats = reinterpret_cast<float2*>(ws + sizes.where_bytes);
     p.part_o = reinterpret_cast<float*>(ws + sizes.where_bytes + sizes.stats_bytes);
+    p.few_part_rows = (int32_t)sizes.few_part_rows;
     p.part_rows = (int32_t)sizes.part_rows;
+    p.few_limit = sizes.few_limit;
     const hipError_t e = hspmd::launch_paged_attn(p, sizes, cache->dtype == HSPMD_CACHE_E4M3, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail_hip(e, "paged attention launch");
     return HSPMD_OK;

@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "../../include/hspmd_attn.h"
+#include "paged_index.hpp"
 
 namespace hspmd {
 
@@ -71,14 +72,9 @@ struct CacheReadParams {
 hipError_t launch_cache_read(const CacheReadParams& p, bool e4m3, hipStream_t stream);
 
 // ---- attention over the cache --------------------------------------------------------------------------------------
-// The rows of a sequence that share a KV head (n new tokens x group query heads, token by token) are cut into tiles; a row
-// tile and a KV head are an item, and the keys of an item are shared out over several workgroups ("chunks" of `units`
-// 128-key units) where there are few items.  How many units a chunk takes is worked out by every workgroup for itself from the
-// lengths on the device: the launch does not know them.
-constexpr int kUnitKeys = 128;
-constexpr int kFewRows = 16;       // rows per tile
-constexpr int kChunkTarget = 512;  // chunks to aim for: two for each of the 256 compute units
-
+// The rows of a sequence that share a KV head (n new tokens x group query heads, token by token) are cut into tiles; a row tile and a KV head
+// are an item, and the keys of an item are shared out over several workgroups ("chunks") where there are few items.  The launch does not know
+// the lengths: the workgroups work their shares out (find_item), the host launches as many as there can be (grid_bounds).
 struct PagedAttnParams {
     PagedPool pool;
     PagedRows rows;
@@ -87,23 +83,27 @@ struct PagedAttnParams {
     float* lse;                    // may be NULL
     int64_t q_stride;
     int32_t q_heads, group;
+    int32_t few_limit;             // sequences with more rows per KV head are for paged_many_kernel
     float scale_log2;              // softmax_scale * log2(e)
-    // workspace: results of chunks, row by row (fp32 sums of P V over the head's tile width, and (maximum, sum of weights)),
-    // and for every row of the call where its chunks' results are
+    // workspace: results of chunks, row by row (fp32 sums of P V over the head's tile width, and (maximum, sum of weights)), those of
+    // paged_few_kernel first; and for every row of the call where its chunks' results are
     float* part_o;
     float2* part_stats;
-    int2* where;                   // [total_rows][q_heads]: first row of part_o, chunks (1: the row's result is in o)
-    int32_t part_rows;             // rows that part_o holds
+    int2* where;                   // [total_rows][q_heads], see where_entry
+    int32_t few_part_rows, part_rows;
 };
 
 // sizes that follow from what the host knows
 struct PagedSizes {
-    int64_t few_grid;              // workgroups that the items and their chunks can need
-    int64_t part_rows;
+    bool few, many;                // which kernels run
+    int32_t few_limit;
+    int64_t few_grid, many_grid;
+    int64_t few_part_rows, part_rows;
     size_t where_bytes, stats_bytes, part_bytes;
     size_t total_bytes() const { return where_bytes + stats_bytes + part_bytes; }
 };
-PagedSizes paged_sizes(const PagedRows& rows, int page_shift, int q_heads, int kv_heads, int head_dim);
+PagedSizes paged_sizes(const PagedRows& rows, int max_rows, int page_shift, int q_heads, int kv_heads, int head_dim);
 hipError_t launch_paged_attn(const PagedAttnParams& p, const PagedSizes& sizes, bool e4m3, hipStream_t stream);
+hipError_t launch_paged_many(const PagedAttnParams& p, int64_t grid, bool e4m3, hipStream_t stream);
 
 }  // namespace hspmd

@@ -10,7 +10,7 @@
 //   S^T = K Q^T (16x16x32, 2 key blocks x D/32 steps),  P = exp2(c S - c m),  O^T += V^T P^T (D/16 blocks, one step of 32 keys)
 // 8-bit tiles are copied as they are; K is scaled to bf16 on its way from LDS (exact), V's scales go into the weights
 // before they are rounded, its bytes are converted as they are.
-#include "paged_device.hpp"
+#include "paged_item.hpp"
 
 namespace hspmd {
 
@@ -23,88 +23,6 @@ template <int N>
 __device__ __forceinline__ void wait_copies_except() {
     static_assert(N >= 0 && N < 64, "vmcnt field");
     __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
-}
-
-// A workgroup's work: a row tile of one (sequence, KV head) and a range of units of keys
-struct PagedItem {
-    int seq;               // -1: none
-    int row_start, n;      // the sequence's rows
-    int kv;                // keys in the cache
-    int tile, head;        // row tile, KV head
-    int chunk, chunks;     // which share of the keys
-    int units;             // units per share
-    int part;              // first tile of rows in part_o (chunks > 1)
-};
-
-__device__ __forceinline__ int64_t wave_sum(int64_t x) {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o, 64);
-    return x;
-}
-
-// What workgroup `slot` does.  Every workgroup computes the shares for itself: with U the units of all items together, a chunk
-// takes ceil(U / kChunkTarget) units, so that there are about as many chunks as the device takes at once, whatever the mix of lengths.
-// `tile_rows`: rows per tile.  The arrays hold anything: sums are 64-bit, rows and lengths clamped.
-__device__ __forceinline__ void find_item(const PagedAttnParams& p, int tile_rows, int64_t slot, PagedItem* out) {
-    __shared__ int64_t sums[2][4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, kvh = p.pool.kv_heads;
-    auto geometry = [&](int s, int& start, int& n, int& kv, int& tiles, int& units) {
-        start = n = kv = tiles = units = 0;
-        if (s >= p.rows.num_seqs) return;
-        start = min(max(p.rows.cu_rows[s], 0), p.rows.total_rows);
-        n = min(max(p.rows.cu_rows[s + 1], start), p.rows.total_rows) - start;
-        kv = kv_length(p.rows, p.pool.page_shift, s);
-        tiles = (int)(((int64_t)n * p.group + tile_rows - 1) / tile_rows);
-        units = max(1, (kv + kUnitKeys - 1) / kUnitKeys);
-    };
-    int64_t all = 0;
-    int start, n, kv, tiles, units;
-    for (int s = threadIdx.x; s < p.rows.num_seqs; s += kThreads) {
-        geometry(s, start, n, kv, tiles, units);
-        all += (int64_t)tiles * units * kvh;
-    }
-    all = wave_sum(all);
-    if (lane == 0) sums[0][wave] = all;
-    if (threadIdx.x == 0) out->seq = -1;
-    __syncthreads();
-    all = sums[0][0] + sums[0][1] + sums[0][2] + sums[0][3];
-    const int per_chunk = (int)min(max((all + kChunkTarget - 1) / kChunkTarget, (int64_t)1), (int64_t)(1 << 24));
-    int64_t slot_base = 0, part_base = 0;
-    for (int s0 = 0; s0 < p.rows.num_seqs; s0 += kThreads) {
-        const int s = s0 + threadIdx.x;
-        geometry(s, start, n, kv, tiles, units);
-        const int chunks = (units + per_chunk - 1) / per_chunk;
-        const int64_t slots = (int64_t)tiles * kvh * chunks;
-        int64_t x = slots, y = chunks > 1 ? slots : 0;       // inclusive sums over the wave, then over the waves
-#pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t a = __shfl_up(x, o, 64), b = __shfl_up(y, o, 64);
-            if (lane >= o) { x += a; y += b; }
-        }
-        __syncthreads();
-        if (lane == 63) { sums[0][wave] = x; sums[1][wave] = y; }
-        __syncthreads();
-        int64_t before = slot_base, part_before = part_base;
-        for (int w = 0; w < wave; ++w) { before += sums[0][w]; part_before += sums[1][w]; }
-        const int64_t first = before + x - slots;
-        if (slot >= first && slot < first + slots) {
-            const int64_t local = slot - first;
-            const int item = (int)(local / chunks);
-            out->seq = s;
-            out->row_start = start;
-            out->n = n;
-            out->kv = kv;
-            out->tile = item / kvh;
-            out->head = item % kvh;
-            out->chunk = (int)(local % chunks);
-            out->chunks = chunks;
-            out->units = per_chunk;
-            out->part = (int)min(part_before + y - (chunks > 1 ? slots : 0) + (int64_t)item * chunks, (int64_t)0x7fffffff / tile_rows);
-        }
-        for (int w = 0; w < 4; ++w) { slot_base += sums[0][w]; part_base += sums[1][w]; }
-        if (slot < slot_base) break;
-    }
-    __syncthreads();
 }
 
 // Tile geometry in LDS: rows of D elements, 16-byte chunks XOR-swizzled so that neither the row-wise operand reads (16 rows, the same
@@ -146,8 +64,6 @@ __device__ __forceinline__ bool tile_not_finite(const char* tile, int lane) {
     return __any(found != 0);
 }
 
-constexpr int kWindowPages = 2048;     // page numbers kept in LDS at a time (32768 keys of the smallest pages)
-
 template <int D, bool E4M3>
 struct FewGeom {
     using Tile = PagedTile<D, E4M3>;
@@ -169,12 +85,10 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
     __shared__ __attribute__((aligned(1024))) char lds[4 * G::kWaveBytes];
     __shared__ int pages[kWindowPages + 1];
     __shared__ float2 stats[4][R];
-    __shared__ PagedItem item_of;
     __shared__ int bad_key;                      // first key of the first page that does not exist
 
-    find_item(p, R, blockIdx.x, &item_of);
-    if (item_of.seq < 0) return;
-    const PagedItem it = item_of;
+    const PagedItem it = find_item<false>(p);
+    if (it.seq < 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r16 = lane & 15, quad = lane >> 4;
     const int hd = p.pool.head_dim, shift = p.pool.page_shift, page_mask = (1 << shift) - 1;
@@ -188,8 +102,8 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
     const int first_token = it.tile * R / p.group, last_token = min(it.n - 1, (it.tile * R + R - 1) / p.group);
     const int tile_limit = it.kv - it.n + first_token;             // last key that every real row sees
     const int keys_end = max(0, it.kv - it.n + last_token + 1);
-    const int k0 = it.chunk * it.units * kUnitKeys;
-    const int k1 = (int)min((int64_t)keys_end, (int64_t)k0 + (int64_t)it.units * kUnitKeys);
+    const int64_t unit_keys = (int64_t)it.units * kUnitKeys;
+    const int k0 = (int)min((int64_t)keys_end, it.chunk * unit_keys), k1 = (int)min((int64_t)keys_end, (it.chunk + 1) * unit_keys);
 
     bf16x8 qf[KS];
     const uint16_t* const q_row = p.q + (int64_t)(it.row_start + token) * p.q_stride + (int64_t)q_head * hd;
@@ -216,14 +130,7 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
         const int first_page = w0 >> shift;
         const int w1 = (int)min((int64_t)k1, ((int64_t)first_page + kWindowPages) << shift);
         __syncthreads();
-        for (int i = threadIdx.x; i <= ((w1 - 1) >> shift) - first_page; i += kThreads) {
-            int page = page_at(p.pool, p.rows, it.seq, first_page + i);
-            if (page < 0) {
-                atomicMin(&bad_key, (first_page + i) << shift);
-                page = 0;                          // (read, never shown: the rows that would see it become NaN)
-            }
-            pages[i] = page;
-        }
+        load_pages(p, it.seq, first_page, ((w1 - 1) >> shift) - first_page + 1, pages, &bad_key);
         // the row has to be here before copies are under way that the compiler does not count: it would wait for them too, in every tile
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
@@ -436,11 +343,11 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
             if (col == 0 && p.lse) p.lse[(int64_t)hq * p.rows.total_rows + row] = total == 0.f ? -INFINITY : (top * c + __log2f(total)) * kLn2;
         }
         const int64_t part_row = ((int64_t)it.part + it.chunk) * R + r;
-        if (!whole && part_row < p.part_rows) {
+        if (!whole && part_row < p.few_part_rows) {
             *reinterpret_cast<f32x4*>(p.part_o + part_row * D + col) = o;
             if (col == 0) p.part_stats[part_row] = make_float2(top, total);
         }
-        if (col == 0 && it.chunk == 0) p.where[row * p.q_heads + hq] = make_int2((int)part_row, it.chunks);
+        if (col == 0 && it.chunk == 0) p.where[row * p.q_heads + hq] = where_entry(part_row, it.chunks, false);
     }
 }
 
@@ -455,18 +362,20 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedAttnParams p)
     const int row = (int)(unit / p.q_heads), head = (int)(unit % p.q_heads);
     if (sequence_of(p.rows, row) < 0) return;
     const int2 at = p.where[unit];
-    if (at.y <= 1 || at.x < 0 || (int64_t)at.x + (int64_t)(at.y - 1) * kFewRows >= p.part_rows) return;
+    const bool many = at.y >> 30 & 1;
+    const int chunks = at.y & 0x3fffffff, tile_rows = many ? kManyRows : kFewRows;
+    if (chunks <= 1 || at.x < 0 || (int64_t)at.x + (int64_t)(chunks - 1) * tile_rows >= p.part_rows) return;
     const float c = p.scale_log2;
     float top = -INFINITY;
-    for (int i = lane; i < at.y; i += 64) top = fmaxf(top, p.part_stats[at.x + i * kFewRows].x);
+    for (int i = lane; i < chunks; i += 64) top = fmaxf(top, p.part_stats[at.x + i * tile_rows].x);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
     const float ref = top == -INFINITY ? 0.f : top;
     float total = 0.f, o[kPer];
 #pragma unroll
     for (int j = 0; j < kPer; ++j) o[j] = 0.f;
-    for (int i = 0; i < at.y; ++i) {
-        const int64_t r = at.x + (int64_t)i * kFewRows;
+    for (int i = 0; i < chunks; ++i) {
+        const int64_t r = at.x + (int64_t)i * tile_rows;
         const float2 st = p.part_stats[r];
         const float f = fast_exp2((st.x - ref) * c);
         total += f * st.y;
@@ -490,16 +399,24 @@ void launch_few(const PagedAttnParams& p, const PagedSizes& sizes, hipStream_t s
 
 }  // namespace
 
-PagedSizes paged_sizes(const PagedRows& rows, int page_shift, int q_heads, int kv_heads, int head_dim) {
+// Which kernel takes a sequence.  With up to 16 rows per KV head the kernel for few rows reads the keys once; the one for many takes 128 rows
+// in about the time that 16 take there, so two tiles of the former are already no faster.
+PagedSizes paged_sizes(const PagedRows& rows, int max_rows, int page_shift, int q_heads, int kv_heads, int head_dim) {
     const int64_t group = q_heads / kv_heads, D = tile_width(head_dim);
-    const int64_t units = std::max<int64_t>(1, (((int64_t)rows.table_width << page_shift) + kUnitKeys - 1) / kUnitKeys);
-    // tiles: every sequence with rows ends in one that may not be full
-    const int64_t items = kv_heads * ((rows.total_rows * group + kFewRows - 1) / kFewRows + std::min(rows.num_seqs, rows.total_rows));
+    const int64_t most = (max_rows > 0 ? std::min(max_rows, rows.total_rows) : rows.total_rows) * group;
     PagedSizes s{};
-    // a chunk takes at least 1 / kChunkTarget of all units, so the chunks of the items are at most one per item more than that many;
-    // those of items with several chunks at most twice as many
-    s.few_grid = std::min(items * units, items + kChunkTarget);
-    s.part_rows = std::min(items * units, (int64_t)2 * kChunkTarget) * kFewRows;
+    s.few = most <= kFewRows || rows.num_seqs > 1;
+    s.many = most > kFewRows;
+    // (one kernel alone takes every sequence, so that a wrong max_rows costs time and nothing else)
+    s.few_limit = !s.many ? 0x7fffffff : s.few ? kFewRows : 0;
+    auto bounds = [&](bool many, int few_limit) {
+        return grid_bounds(rows.total_rows, rows.num_seqs, rows.table_width, page_shift, group, kv_heads, many, few_limit);
+    };
+    s.few_grid = bounds(false, s.few_limit).grid;
+    s.many_grid = bounds(true, s.few_limit).grid;
+    // room for either choice: the size does not depend on the hint
+    s.few_part_rows = bounds(false, 0x7fffffff).part_tiles * kFewRows;
+    s.part_rows = s.few_part_rows + (rows.total_rows * group > kFewRows ? bounds(true, 0).part_tiles * kManyRows : 0);
     s.where_bytes = ((size_t)rows.total_rows * q_heads * sizeof(int2) + 255) / 256 * 256;
     s.stats_bytes = ((size_t)s.part_rows * sizeof(float2) + 255) / 256 * 256;
     s.part_bytes = (size_t)s.part_rows * D * sizeof(float);
@@ -508,14 +425,19 @@ PagedSizes paged_sizes(const PagedRows& rows, int page_shift, int q_heads, int k
 
 hipError_t launch_paged_attn(const PagedAttnParams& p, const PagedSizes& sizes, bool e4m3, hipStream_t stream) {
     const int width = tile_width(p.pool.head_dim);
-    if (width == 128) {
-        if (e4m3) launch_few<128, true>(p, sizes, stream);
-        else launch_few<128, false>(p, sizes, stream);
-    } else {
-        if (e4m3) launch_few<64, true>(p, sizes, stream);
-        else launch_few<64, false>(p, sizes, stream);
+    if (sizes.few) {
+        if (width == 128) {
+            if (e4m3) launch_few<128, true>(p, sizes, stream);
+            else launch_few<128, false>(p, sizes, stream);
+        } else {
+            if (e4m3) launch_few<64, true>(p, sizes, stream);
+            else launch_few<64, false>(p, sizes, stream);
+        }
+        if (const hipError_t e = hipGetLastError()) return e;
     }
-    if (const hipError_t e = hipGetLastError()) return e;
+    if (sizes.many) {
+        if (const hipError_t e = launch_paged_many(p, sizes.many_grid, e4m3, stream)) return e;
+    }
     const int64_t waves = (int64_t)p.rows.total_rows * p.q_heads;
     const dim3 grid((unsigned)((waves + 3) / 4)), threads(kThreads);
     if (width == 128) hipLaunchKernelGGL(paged_join_kernel<128>, grid, threads, 0, stream, p);

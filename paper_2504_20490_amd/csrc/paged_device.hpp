@@ -30,11 +30,6 @@ __device__ __forceinline__ int sequence_of(const PagedRows& b, int row) {
     return -1;
 }
 
-__device__ __forceinline__ int kv_length(const PagedRows& b, int page_shift, int seq) {
-    const int64_t most = (int64_t)b.table_width << page_shift;
-    return (int)min((int64_t)max(b.kv_lens[seq], 0), min(most, (int64_t)0x7fffff00));
-}
-
 __device__ __forceinline__ int page_at(const PagedPool& pool, const PagedRows& b, int seq, int index) {
     const int page = b.page_table[(int64_t)seq * b.table_width + index];
     return (unsigned)page < (unsigned)pool.num_pages ? page : -1;
@@ -43,7 +38,7 @@ __device__ __forceinline__ int page_at(const PagedPool& pool, const PagedRows& b
 __device__ __forceinline__ RowPlace place_of(const PagedPool& pool, const PagedRows& b, int row) {
     RowPlace r{sequence_of(b, row), -1, -1, 0};
     if (r.seq < 0) return r;
-    const int kv = kv_length(b, pool.page_shift, r.seq);
+    const int kv = seq_rows(0, 0, b.kv_lens[r.seq], 0, b.table_width, pool.page_shift).kv;
     const int pos = kv - (b.cu_rows[r.seq + 1] - row);   // (cu_rows[seq + 1] > row)
     if (pos < 0) return r;
     r.pos = pos;
