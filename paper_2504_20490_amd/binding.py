@@ -534,22 +534,25 @@ def _bad(what: str):
     return HspmdError(1, what)
 
 
-def _device_tensors(*tensors) -> None:
-    """All given tensors lie on the current GPU: the calls enqueue on a stream of that device."""
+def _stream_of(device: int, others: Sequence, stream) -> int:
+    """The handle of the stream that a call enqueues on; every tensor has to be on the current GPU, whose stream it is.  `others`: devices of
+    the call's other tensors."""
     import torch
-    here = torch.cuda.current_device() if torch.cuda.is_available() else None
-    for t in tensors:
-        if t is not None and (not t.is_cuda or t.get_device() != here):
-            raise _bad("every tensor has to be on the current GPU")
+    if device < 0 or any(d != device for d in others) or device != torch.cuda.current_device():
+        raise _bad("every tensor has to be on the current GPU")
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(device)
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _rows_stride(x, heads: int, head_dim: int, dtype, what: str, tokens: Optional[int] = None) -> int:
-    """The token stride of a [T, heads, head_dim] tensor of the given type whose rows are contiguous."""
-    if x.dtype != dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != head_dim or (tokens is not None and x.shape[0] != tokens):
-        raise _bad(f"{what} has to be [{'T' if tokens is None else tokens}, {heads}, {head_dim}] of {dtype}")
-    if x.numel() and (x.stride(2) != 1 and head_dim > 1 or x.stride(1) != head_dim and heads > 1):
+def _rows_stride(x, heads: int, head_dim: int, dtype, what: str, tokens: int) -> int:
+    """The token stride of a [tokens, heads, head_dim] tensor of the given type whose rows are contiguous."""
+    if x.dtype is not dtype or tuple(x.shape) != (tokens, heads, head_dim):
+        raise _bad(f"{what} has to be [{tokens}, {heads}, {head_dim}] of {dtype}")
+    s = x.stride()
+    if (s[2] != 1 or s[1] != head_dim and heads > 1) and x.numel():
         raise _bad(f"{what}: the heads of a token have to be contiguous")
-    return _token_stride(x, heads, head_dim)
+    return s[0] if tokens > 1 else heads * head_dim
 
 
 class RopeAxes:
@@ -560,57 +563,63 @@ class RopeAxes:
 
     def __init__(self, table, table_positions: int, positions=None, pair_axis: Optional[Sequence[int]] = None):
         import torch
-        a = _RopeAxesArgs()
-        if table.dtype != torch.float32 or not table.is_contiguous():
+        if table.dtype is not torch.float32 or not table.is_contiguous():
             raise _bad("the rope table has to be a contiguous fp32 tensor")
-        self.table, self.positions = table, positions              # (kept alive)
-        self.pairs, self.tokens = table.numel() // 2 // max(int(table_positions), 1), None
-        axes = 1
+        self.tensors = (table, positions)                          # (kept alive)
+        self.table = table
+        self.device = table.get_device()
+        self.pairs, self.tokens = table.numel() // 2 // max(table_positions, 1), None
+        axes, stride, where, pairs = 1, 0, None, None
         if positions is not None:
-            if positions.dtype != torch.int32 or positions.dim() not in (1, 2) or (positions.numel() > 1 and positions.stride(-1) != 1):
+            if positions.dtype is not torch.int32 or positions.dim() not in (1, 2) or positions.stride(-1) != 1 and positions.numel() > 1:
                 raise _bad("positions has to be int32 [num_axes, T] with contiguous rows")
-            self.tokens = positions.shape[-1]
-            if positions.dim() == 2:
-                axes, a.positions_stride = positions.shape[0], positions.stride(0) if positions.shape[0] > 1 else positions.shape[1]
-            a.positions = positions.data_ptr() or None
+            shape = positions.shape
+            self.tokens, where = shape[-1], positions.data_ptr() or None
+            if len(shape) == 2:
+                axes, stride = shape[0], positions.stride(0) if shape[0] > 1 else shape[1]
+            if positions.get_device() != self.device:
+                raise _bad("table and positions have to be on one GPU")
+        self.has_pairs = None
         if pair_axis is not None:
-            if any(not 0 <= int(x) < 256 for x in pair_axis):
-                raise _bad("pair_axis names an axis that does not exist")
-            self.pair_axis = bytes(int(x) for x in pair_axis)
-            a.pair_axis = self.pair_axis
-            axes = max(axes, 1 + max(self.pair_axis, default=0)) if positions is None else axes
-        self.has_pairs = None if pair_axis is None else len(self.pair_axis)
-        a.table, a.table_positions, a.num_axes = table.data_ptr(), int(table_positions), axes
-        self._args = a
+            try:
+                pairs = bytes(pair_axis)
+            except (TypeError, ValueError):
+                raise _bad("pair_axis has to name axes that exist") from None
+            self.has_pairs = len(pairs)
+            if positions is None:
+                axes = 1 + max(pairs, default=0)
+        self._args = _RopeAxesArgs(table.data_ptr(), table_positions, axes, where, stride, pairs)
+        self._ref = ctypes.byref(self._args)
 
-    def _check(self, head_dim: int, tokens: Optional[int]) -> None:
+    def _check(self, head_dim: int, tokens: int) -> None:
         if self.pairs < head_dim // 2:
             raise _bad("rope table tensor is too small")
         if self.has_pairs is not None and self.has_pairs != head_dim // 2:
             raise _bad("pair_axis has to have head_dim / 2 entries")
-        if tokens is not None and self.tokens is not None and self.tokens < tokens:
+        if self.tokens is not None and self.tokens < tokens:
             raise _bad("positions has fewer tokens than the tensors")
-        _device_tensors(self.table, self.positions)
 
 
 def rope_axes_qk(rope: RopeAxes, q, k, q_out, k_out, inverse: bool = False, stream=None) -> None:
     """q_out, k_out = q, k turned by each token's positions (inverse: turned back, as gradients are); bf16 or fp32 [T, heads, head_dim],
     in place where q_out is q and k_out is k.  k and k_out may be None."""
     import torch
-    T, hq, d = q.shape
-    if q.dtype not in (torch.bfloat16, torch.float32):
-        raise _bad("q has to be bf16 or fp32")
+    if q.dim() != 3 or q.dtype is not torch.bfloat16 and q.dtype is not torch.float32:
+        raise _bad("q has to be bf16 or fp32 [T, heads, head_dim]")
     if (k is None) != (k_out is None):
         raise _bad("k and k_out go together")
-    hkv = 0 if k is None else k.shape[1]
-    strides = [_rows_stride(x, h, d, q.dtype, what, T) if x is not None else 0
-               for x, h, what in ((q, hq, "q"), (k, hkv, "k"), (q_out, hq, "q_out"), (k_out, hkv, "k_out"))]
+    T, hq, d = q.shape
+    t = q.dtype
+    qs, qos = _rows_stride(q, hq, d, t, "q", T), _rows_stride(q_out, hq, d, t, "q_out", T)
     rope._check(d, T)
-    _device_tensors(q, k, q_out, k_out)
-    _check(load_library().hspmd_rope_axes_qk(ctypes.byref(rope._args), _dev_ptr(q), _opt_ptr(k), strides[0], strides[1], _dev_ptr(q_out),
-                                             _opt_ptr(k_out), strides[2], strides[3], T, hq, hkv, d,
-                                             GRAD_F32 if q.dtype == torch.float32 else GRAD_BF16, 1 if inverse else 0,
-                                             _stream_handle(stream)))
+    hkv, ks, kos, kp, kop, devices = 0, 0, 0, None, None, (q_out.get_device(), rope.device)
+    if k is not None:
+        hkv = k.shape[1] if k.dim() == 3 else -1
+        ks, kos = _rows_stride(k, hkv, d, t, "k", T), _rows_stride(k_out, hkv, d, t, "k_out", T)
+        kp, kop, devices = k.data_ptr(), k_out.data_ptr(), (*devices, k.get_device(), k_out.get_device())
+    handle = _stream_of(q.get_device(), devices, stream)
+    _check(load_library().hspmd_rope_axes_qk(rope._ref, q.data_ptr(), kp, qs, ks, q_out.data_ptr(), kop, qos, kos, T, hq, hkv, d,
+                                             GRAD_F32 if t is torch.float32 else GRAD_BF16, 1 if inverse else 0, handle))
 
 
 def kv_cache_row(head_dim: int, dtype: int) -> int:
@@ -624,31 +633,37 @@ class KVCache:
 
     def __init__(self, k, v, k_scale=None, v_scale=None, head_dim: Optional[int] = None):
         import torch
-        if k.dtype not in (torch.bfloat16, torch.float8_e4m3fn):
+        t = k.dtype
+        e4m3 = t is torch.float8_e4m3fn
+        if not e4m3 and t is not torch.bfloat16:
             raise _bad("the cache has to be bf16 or float8_e4m3fn")
-        e4m3 = k.dtype == torch.float8_e4m3fn
         if e4m3 != (k_scale is not None) or e4m3 != (v_scale is not None):
             raise _bad("an e4m3 cache has scales, a bf16 cache has none")
-        if k.dim() != 4 or v.shape != k.shape or v.dtype != k.dtype:
+        shape = k.shape
+        if len(shape) != 4 or v.shape != shape or v.dtype is not t:
             raise _bad("k and v have to be [num_pages, kv_heads, page_size, row], alike")
-        pages, heads, size, row = k.shape
-        for x, inner in ((k, (size * row, row, 1)), (v, (size * row, row, 1)), (k_scale, (size, 1)), (v_scale, (size, 1))):
-            if x is None:
-                continue
-            if len(inner) == 2 and (x.dtype != torch.uint8 or tuple(x.shape) != (pages, heads, size)):
+        pages, heads, size, row = shape
+        self.tensors = (k, v) if not e4m3 else (k, v, k_scale, v_scale)   # (kept alive)
+        self.device = k.get_device()
+        strides = []
+        for x, inner in zip(self.tensors, ((size * row, row, 1), (size * row, row, 1), (size, 1), (size, 1))):
+            if len(inner) == 2 and (x.dtype is not torch.uint8 or x.shape != shape[:3]):
                 raise _bad("scales have to be uint8 [num_pages, kv_heads, page_size]")
-            if any(x.stride(i + 1) != s and x.shape[i + 1] > 1 for i, s in enumerate(inner)):
+            s = x.stride()
+            if s[1:] != inner and any(a != b and n > 1 for a, b, n in zip(s[1:], inner, x.shape[1:])):
                 raise _bad("a page's heads, rows and columns have to be contiguous")
-        strides = [x.stride(0) if pages > 1 else heads * size * (row if x.dim() == 4 else 1) for x in (k, v, k_scale, v_scale) if x is not None]
-        if strides[0] != strides[1] or strides[2:3] != strides[3:]:
+            if x.get_device() != self.device:
+                raise _bad("the cache's tensors have to be on one GPU")
+            strides.append(s[0] if pages > 1 else inner[0] * heads)
+        if strides[0] != strides[1] or e4m3 and strides[2] != strides[3]:
             raise _bad("k and v have to have the same page stride")
-        self.tensors = (k, v, k_scale, v_scale)                    # (kept alive)
-        self.head_dim, self.kv_heads, self.row = row if head_dim is None else int(head_dim), heads, row
-        self.dtype = CACHE_E4M3 if e4m3 else CACHE_BF16
-        if row != (self.head_dim if not e4m3 else (self.head_dim + 15) // 16 * 16):
+        d = row if head_dim is None else int(head_dim)
+        if row != (d if not e4m3 else (d + 15) // 16 * 16):
             raise _bad("the cache's row does not fit head_dim")
+        self.head_dim, self.kv_heads, self.row, self.dtype = d, heads, row, CACHE_E4M3 if e4m3 else CACHE_BF16
         self._args = _KVCacheArgs(k.data_ptr(), v.data_ptr(), k_scale.data_ptr() if e4m3 else None, v_scale.data_ptr() if e4m3 else None,
-                                  strides[0], strides[2] if e4m3 else 0, pages, size, heads, self.head_dim, self.dtype)
+                                  strides[0], strides[2] if e4m3 else 0, pages, size, heads, d, self.dtype)
+        self._ref = ctypes.byref(self._args)
 
 
 class KVBatch:
@@ -657,71 +672,79 @@ class KVBatch:
 
     def __init__(self, cu_rows, kv_lens, page_table, max_rows: int = 0):
         import torch
-        n = kv_lens.numel()
-        if any(x.dtype != torch.int32 or not x.is_contiguous() for x in (cu_rows, kv_lens, page_table)):
+        i32 = torch.int32
+        if cu_rows.dtype is not i32 or kv_lens.dtype is not i32 or page_table.dtype is not i32 or not (
+                cu_rows.is_contiguous() and kv_lens.is_contiguous() and page_table.is_contiguous()):
             raise _bad("cu_rows, kv_lens and page_table have to be contiguous int32 tensors")
-        if cu_rows.numel() != n + 1 or page_table.dim() != 2 or page_table.shape[0] != n:
+        n, shape = kv_lens.numel(), page_table.shape
+        if cu_rows.numel() != n + 1 or len(shape) != 2 or shape[0] != n:
             raise _bad("cu_rows has to have one entry more than kv_lens, page_table as many rows")
+        self.device = cu_rows.get_device()
+        if kv_lens.get_device() != self.device or page_table.get_device() != self.device:
+            raise _bad("cu_rows, kv_lens and page_table have to be on one GPU")
         self.tensors = (cu_rows, kv_lens, page_table)              # (kept alive)
-        self._args = _KVBatchArgs(cu_rows.data_ptr(), kv_lens.data_ptr() or None, page_table.data_ptr() or None, n, page_table.shape[1],
-                                  0, int(max_rows))
+        self._fields = (cu_rows.data_ptr(), kv_lens.data_ptr() or None, page_table.data_ptr() or None, n, shape[1])
+        self._max_rows = int(max_rows)
 
-    def _with_rows(self, rows: int) -> _KVBatchArgs:
-        a = _KVBatchArgs.from_buffer_copy(self._args)
-        a.total_rows = rows
-        return a
+    def _with_rows(self, rows: int):
+        return ctypes.byref(_KVBatchArgs(*self._fields, rows, self._max_rows))   # (one per call: several threads may share the batch)
 
 
 def kv_cache_write(cache: KVCache, batch: KVBatch, k, v, rope: Optional[RopeAxes] = None, q=None, q_out=None, stream=None) -> None:
     """Writes k, v (bf16 [T, kv_heads, head_dim]) into their places, k turned by `rope` (positions None: the rows' own); q, if given, is
     turned into q_out in the same launch."""
     import torch
-    d, bf16 = cache.head_dim, torch.bfloat16
-    T = k.shape[0]
-    stride = _rows_stride(k, cache.kv_heads, d, bf16, "k")
+    d, bf16, T = cache.head_dim, torch.bfloat16, k.shape[0]
+    stride = _rows_stride(k, cache.kv_heads, d, bf16, "k", T)
     if _rows_stride(v, cache.kv_heads, d, bf16, "v", T) != stride:
         raise _bad("k and v have to have the same token stride")
     if (q is None) != (q_out is None):
         raise _bad("q and q_out go together")
-    hq = 0 if q is None else q.shape[1]
-    qs, qos = (0, 0) if q is None else (_rows_stride(q, hq, d, bf16, "q", T), _rows_stride(q_out, hq, d, bf16, "q_out", T))
+    hq, qs, qos, qp, qop, devices = 0, 0, 0, None, None, (v.get_device(), cache.device, batch.device)
+    if q is not None:
+        hq = q.shape[1] if q.dim() == 3 else -1
+        qs, qos = _rows_stride(q, hq, d, bf16, "q", T), _rows_stride(q_out, hq, d, bf16, "q_out", T)
+        qp, qop, devices = q.data_ptr(), q_out.data_ptr(), (*devices, q.get_device(), q_out.get_device())
     if rope is not None:
         rope._check(d, T)
-    _device_tensors(*cache.tensors, *batch.tensors, k, v, q, q_out)
-    _check(load_library().hspmd_kv_cache_write(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(T)), _dev_ptr(k), _dev_ptr(v), stride,
-                                               None if rope is None else ctypes.byref(rope._args), _opt_ptr(q), _opt_ptr(q_out), qs, qos, hq,
-                                               _stream_handle(stream)))
+        devices = (*devices, rope.device)
+    handle = _stream_of(k.get_device(), devices, stream)
+    _check(load_library().hspmd_kv_cache_write(cache._ref, batch._with_rows(T), k.data_ptr(), v.data_ptr(), stride,
+                                               None if rope is None else rope._ref, qp, qop, qs, qos, hq, handle))
 
 
 def kv_cache_read(cache: KVCache, batch: KVBatch, k, v, stream=None) -> None:
     """Reads the batch's rows back into k, v (bf16 [T, kv_heads, head_dim])."""
     import torch
-    stride = _rows_stride(k, cache.kv_heads, cache.head_dim, torch.bfloat16, "k")
-    if _rows_stride(v, cache.kv_heads, cache.head_dim, torch.bfloat16, "v", k.shape[0]) != stride:
+    T = k.shape[0]
+    stride = _rows_stride(k, cache.kv_heads, cache.head_dim, torch.bfloat16, "k", T)
+    if _rows_stride(v, cache.kv_heads, cache.head_dim, torch.bfloat16, "v", T) != stride:
         raise _bad("k and v have to have the same token stride")
-    _device_tensors(*cache.tensors, *batch.tensors, k, v)
-    _check(load_library().hspmd_kv_cache_read(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(k.shape[0])), _dev_ptr(k), _dev_ptr(v),
-                                              stride, _stream_handle(stream)))
+    handle = _stream_of(k.get_device(), (v.get_device(), cache.device, batch.device), stream)
+    _check(load_library().hspmd_kv_cache_read(cache._ref, batch._with_rows(T), k.data_ptr(), v.data_ptr(), stride, handle))
 
 
 def attn_paged_workspace_bytes(cache: KVCache, batch: KVBatch, total_rows: int, q_heads: int) -> int:
-    return int(load_library().hspmd_attn_paged_workspace_bytes(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(int(total_rows))),
-                                                               int(q_heads)))
+    return int(load_library().hspmd_attn_paged_workspace_bytes(cache._ref, batch._with_rows(int(total_rows)), int(q_heads)))
 
 
 def attn_paged_fwd(cache: KVCache, batch: KVBatch, q, o, lse, workspace, softmax_scale: float = 0.0, stream=None) -> None:
     """Attention of the rows q (bf16 [T, q_heads, head_dim]) over their sequences' cached keys and values; o bf16 like q, contiguous, and lse
     fp32 [q_heads, T] (may be None) are written; workspace: any device tensor of attn_paged_workspace_bytes(...) bytes."""
     import torch
-    T, hq, d = q.shape
-    stride = _rows_stride(q, hq, cache.head_dim, torch.bfloat16, "q")
-    if o.shape != q.shape or o.dtype != torch.bfloat16 or not o.is_contiguous():
+    if q.dim() != 3:
+        raise _bad("q has to be [T, q_heads, head_dim]")
+    T, hq, _ = q.shape
+    stride = _rows_stride(q, hq, cache.head_dim, torch.bfloat16, "q", T)
+    if o.shape != q.shape or o.dtype is not torch.bfloat16 or not o.is_contiguous():
         raise _bad("o has to be a contiguous bf16 tensor of q's shape")
-    if lse is not None and (tuple(lse.shape) != (hq, T) or lse.dtype != torch.float32 or not lse.is_contiguous()):
-        raise _bad("lse has to be a contiguous fp32 tensor [q_heads, T]")
+    devices, lse_ptr = (o.get_device(), workspace.get_device(), cache.device, batch.device), None
+    if lse is not None:
+        if lse.shape != (hq, T) or lse.dtype is not torch.float32 or not lse.is_contiguous():
+            raise _bad("lse has to be a contiguous fp32 tensor [q_heads, T]")
+        lse_ptr, devices = lse.data_ptr(), (*devices, lse.get_device())
     if not workspace.is_contiguous():
         raise _bad("the workspace has to be contiguous")
-    _device_tensors(*cache.tensors, *batch.tensors, q, o, lse, workspace)
-    _check(load_library().hspmd_attn_paged_fwd(ctypes.byref(cache._args), ctypes.byref(batch._with_rows(T)), _dev_ptr(q), stride, hq,
-                                               float(softmax_scale), _dev_ptr(o), _opt_ptr(lse), _dev_ptr(workspace),
-                                               workspace.numel() * workspace.element_size(), _stream_handle(stream)))
+    handle = _stream_of(q.get_device(), devices, stream)
+    _check(load_library().hspmd_attn_paged_fwd(cache._ref, batch._with_rows(T), q.data_ptr(), stride, hq, softmax_scale, o.data_ptr(), lse_ptr,
+                                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle))

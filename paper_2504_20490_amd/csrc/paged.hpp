@@ -95,7 +95,7 @@ struct PagedAttnParams {
 
 // sizes that follow from what the host knows
 struct PagedSizes {
-    bool few, many;                // which kernels run
+    bool few, many, join;          // which kernels run
     int32_t few_limit;
     int64_t few_grid, many_grid;
     int64_t few_part_rows, part_rows;

@@ -1,12 +1,13 @@
 // Attention of new tokens over the paged cache: few rows per sequence and KV head (single tokens, short runs of them), and
 // the join of chunks' results.
 //
-// With few rows the keys and values are read once and used for little arithmetic: the kernel is bound by reading the cache.  A
-// workgroup takes 16 rows (tokens x query heads of one KV head) and a range of keys; its four waves take 32-key tiles in turn, each wave with
-// LDS buffers of its own into which it copies pages directly, several tiles ahead, so that no wave waits for another and a compute
-// unit has tens of KB under way.  Products are transposed (keys, then head columns along the rows of the result; the 16 rows along its
-// columns): a lane owns one row, the weights of a tile are the second product's operand as they stand, and V's operand comes from the
-// row-major tile through the LDS transpose read.
+// With few rows the keys and values are read once and used for little arithmetic: the kernel is bound by reading the cache.  A workgroup is
+// one wave: it takes 16 rows (tokens x query heads of one KV head) and a range of keys, which it copies page by page to LDS, tiles of 32
+// keys, two ahead.  Single waves on their own keep a compute unit busiest: nothing waits at a barrier, and while one finds its work (lengths,
+// page numbers, first tiles: three trips to memory, some 5 us) the others of the unit (4 of them with 16-bit values at D = 128, 8 otherwise)
+// stream.  Products are transposed (keys, then head columns along the rows of the result; the 16 rows along its columns): a lane owns
+// one row, the weights of a tile are the second product's operand as they stand, and V's operand comes from the row-major tile through
+// the LDS transpose read.
 //   S^T = K Q^T (16x16x32, 2 key blocks x D/32 steps),  P = exp2(c S - c m),  O^T += V^T P^T (D/16 blocks, one step of 32 keys)
 // 8-bit tiles are copied as they are; K is scaled to bf16 on its way from LDS (exact), V's scales go into the weights
 // before they are rounded, its bytes are converted as they are.
@@ -44,6 +45,14 @@ struct PagedTile {
     static __device__ __forceinline__ int at(int row, int byte) { return row * kRowBytes + (((byte >> 4) ^ swizzle(row)) << 4) + (byte & 15); }
 };
 
+// the largest of the values that lanes l, l ^ 16, l ^ 32 and l ^ 48 hold
+__device__ __forceinline__ float quads_max(float x) {
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    const float y = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(y), __float_as_uint(y), false, false);
+    return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // whether a tile holds an infinity or NaN (a whole wave)
 template <int D, bool E4M3>
 __device__ __forceinline__ bool tile_not_finite(const char* tile, int lane) {
@@ -67,30 +76,29 @@ __device__ __forceinline__ bool tile_not_finite(const char* tile, int lane) {
 template <int D, bool E4M3>
 struct FewGeom {
     using Tile = PagedTile<D, E4M3>;
-    // K and V tiles per wave: 32 KB for 16-bit values at D = 128, 16 KB otherwise
-    static constexpr int kStages = D == 128 && !E4M3 ? 2 : 4;
+    static constexpr int kStages = 2;     // K and V tiles: 32 KB for 16-bit values at D = 128
     static constexpr int kScaleBytes = E4M3 ? 256 : 0;
     static constexpr int kStageBytes = 2 * Tile::kBytes + kScaleBytes;
-    static constexpr int kWaveBytes = kStages * kStageBytes;
+    static constexpr int kBytes = kStages * kStageBytes;
     static constexpr int kCopiesK = Tile::kCopies + (E4M3 ? 1 : 0);     // the scales travel with K
     static constexpr int kCopiesV = Tile::kCopies;
+    static constexpr int kCopiesRun = 16 / Tile::kRowsPerCopy;           // per run of 16 keys: the least that a page holds, and the swizzle's period
 };
 
+constexpr int kWave = 64;
+constexpr int kFewPages = 512;     // page numbers kept in LDS at a time (8192 keys of the smallest pages)
+
 template <int D, bool E4M3>
-__global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) {
+__global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
     using G = FewGeom<D, E4M3>;
     using Tile = typename G::Tile;
     constexpr int R = kFewRows, KS = D / 32, DB = D / 16, NST = G::kStages;
-    static_assert(4 * R * D * 4 <= 4 * G::kWaveBytes, "the waves' sums fit where their tiles were");
-    __shared__ __attribute__((aligned(1024))) char lds[4 * G::kWaveBytes];
-    __shared__ int pages[kWindowPages + 1];
-    __shared__ float2 stats[4][R];
-    __shared__ int bad_key;                      // first key of the first page that does not exist
+    __shared__ __attribute__((aligned(1024))) char lds[G::kBytes];
+    __shared__ int pages[kFewPages];
 
     const PagedItem it = find_item<false>(p);
     if (it.seq < 0) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int r16 = lane & 15, quad = lane >> 4;
+    const int lane = threadIdx.x, r16 = lane & 15, quad = lane >> 4;
     const int hd = p.pool.head_dim, shift = p.pool.page_shift, page_mask = (1 << shift) - 1;
     const float c = p.scale_log2;
 
@@ -102,8 +110,8 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
     const int first_token = it.tile * R / p.group, last_token = min(it.n - 1, (it.tile * R + R - 1) / p.group);
     const int tile_limit = it.kv - it.n + first_token;             // last key that every real row sees
     const int keys_end = max(0, it.kv - it.n + last_token + 1);
-    const int64_t unit_keys = (int64_t)it.units * kUnitKeys;
-    const int k0 = (int)min((int64_t)keys_end, it.chunk * unit_keys), k1 = (int)min((int64_t)keys_end, (it.chunk + 1) * unit_keys);
+    const int64_t share = (int64_t)it.units * unit_keys(false);
+    const int k0 = (int)min((int64_t)keys_end, it.chunk * share), k1 = (int)min((int64_t)keys_end, (it.chunk + 1) * share);
 
     bf16x8 qf[KS];
     const uint16_t* const q_row = p.q + (int64_t)(it.row_start + token) * p.q_stride + (int64_t)q_head * hd;
@@ -119,58 +127,80 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
     for (int i = 0; i < DB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
-    char* const mine = lds + wave * G::kWaveBytes;
-    const uint32_t mine_at = lds_address(lds) + wave * G::kWaveBytes;
+    const uint32_t lds_at = lds_address(lds);
     const int64_t head_at = (int64_t)it.head << shift;
     const int last_chunk = (hd * (E4M3 ? 1 : 2) + 15) / 16 - 1;
-    if (threadIdx.x == 0) bad_key = 0x7fffffff;
+    uint32_t lane_at[G::kCopiesRun];               // this lane's 16 bytes of a run's copies
+#pragma unroll
+    for (int i = 0; i < G::kCopiesRun; ++i) {
+        const int r = i * Tile::kRowsPerCopy + lane / Tile::kChunks;
+        lane_at[i] = (uint32_t)(r * p.pool.row_bytes + min((lane % Tile::kChunks) ^ Tile::swizzle(r), last_chunk) * 16);
+    }
+    int bad_key = 0x7fffffff;                      // first key of the first page that does not exist
 
     for (int w0 = k0; w0 < k1;) {
-        // the window's page numbers
+        // the window's page numbers; one that does not exist is replaced by 0: what is read there is shown to nobody
         const int first_page = w0 >> shift;
-        const int w1 = (int)min((int64_t)k1, ((int64_t)first_page + kWindowPages) << shift);
-        __syncthreads();
-        load_pages(p, it.seq, first_page, ((w1 - 1) >> shift) - first_page + 1, pages, &bad_key);
+        const int w1 = (int)min((int64_t)k1, ((int64_t)first_page + kFewPages) << shift);
+        const int count = ((w1 - 1) >> shift) - first_page + 1;
+        for (int i0 = 0; i0 < count; i0 += kWave) {
+            const int i = i0 + lane, page = i < count ? page_at(p.pool, p.rows, it.seq, first_page + i) : 0;
+            const uint64_t bad = __ballot(page < 0);
+            if (bad) bad_key = min(bad_key, (first_page + i0 + (int)__builtin_ctzll(bad)) << shift);
+            if (i < count) pages[i] = max(page, 0);
+        }
         // the row has to be here before copies are under way that the compiler does not count: it would wait for them too, in every tile
 #pragma unroll
         for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[ks]));
-        __syncthreads();
         const int tiles = (w1 - w0 + Tile::kKeys - 1) / Tile::kKeys;
-        const int my_tiles = (tiles - wave + 3) / 4;
 
-        auto issue = [&](int t) {
-            const int key0 = w0 + (t * 4 + wave) * Tile::kKeys;
-            const uint32_t dst = mine_at + (t % NST) * G::kStageBytes;
-            int64_t off[Tile::kCopies];
-#pragma unroll
-            for (int i = 0; i < Tile::kCopies; ++i) {
-                const int r = i * Tile::kRowsPerCopy + lane / Tile::kChunks;
-                const int key = min(key0 + r, w1 - 1);               // (rows past the end repeat the last key: weight 0, finite)
-                const int chunk = min((lane % Tile::kChunks) ^ Tile::swizzle(r), last_chunk);
-                off[i] = pages[(key >> shift) - first_page] * p.pool.page_bytes + (head_at + (key & page_mask)) * p.pool.row_bytes + chunk * 16;
-            }
-#pragma unroll
-            for (int i = 0; i < Tile::kCopies; ++i) global_to_lds<16>(p.pool.k + off[i], dst + i * 1024);
-            if constexpr (E4M3) {
-                // lanes 0 .. 7: K's scales of four keys each, lanes 8 .. 15: V's, the others the same again
-                const int key = min(key0 + (lane & 7) * 4, (w1 - 1) & ~3);
-                const int64_t at = pages[(key >> shift) - first_page] * p.pool.scale_page_bytes + head_at + (key & page_mask);
-                global_to_lds<4>((lane & 8 ? p.pool.v_scale : p.pool.k_scale) + at, dst + 2 * Tile::kBytes);
-            }
-#pragma unroll
-            for (int i = 0; i < Tile::kCopies; ++i) global_to_lds<16>(p.pool.v + off[i], dst + Tile::kBytes + i * 1024);
+        // Where tile t's two runs of 16 keys lie (each within a page), as byte offsets into k and v and into the scales.  Keys behind the last:
+        // what the page holds there, or the same run of the last page; never seen.
+        struct Where {
+            int64_t at[2], scale_at[2];
         };
+        auto locate = [&](int t) {
+            const int key0 = w0 + t * Tile::kKeys;
+            const int numbers = pages[(min(key0 + 16 * (lane & 1), w1 - 1) >> shift) - first_page];
+            Where w;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int64_t page = __builtin_amdgcn_readlane(numbers, half), row = head_at + ((key0 + 16 * half) & page_mask);
+                w.at[half] = page * p.pool.page_bytes + row * p.pool.row_bytes;
+                w.scale_at[half] = E4M3 ? page * p.pool.scale_page_bytes + row : 0;
+            }
+            return w;
+        };
+        auto copy = [&](const uint8_t* base, const Where& w, uint32_t dst) {
+#pragma unroll
+            for (int i = 0; i < Tile::kCopies; ++i) global_to_lds<16>(base + w.at[i / G::kCopiesRun], lane_at[i % G::kCopiesRun], dst + i * 1024);
+        };
+        auto copy_k = [&](int t, const Where& w) {
+            const uint32_t dst = lds_at + (t % NST) * G::kStageBytes;
+            copy(p.pool.k, w, dst);
+            // lanes 0 .. 7: K's scales of four keys each, lanes 8 .. 15: V's, the others the same again
+            if constexpr (E4M3)
+                global_to_lds<4>((lane & 8 ? p.pool.v_scale : p.pool.k_scale) + (lane & 4 ? w.scale_at[1] : w.scale_at[0]) + (lane & 3) * 4,
+                                 dst + 2 * Tile::kBytes);
+        };
+        auto copy_v = [&](int t, const Where& w) { copy(p.pool.v, w, lds_at + (t % NST) * G::kStageBytes + Tile::kBytes); };
 
-        const int ahead = min(NST, my_tiles);
-        for (int t = 0; t < ahead; ++t) issue(t);
-        for (int t = 0; t < my_tiles; ++t) {
-            const int key0 = w0 + (t * 4 + wave) * Tile::kKeys;
-            const char* const kt = mine + (t % NST) * G::kStageBytes;
+        for (int t = 0; t < min(NST, tiles); ++t) {
+            const Where w = locate(t);
+            copy_k(t, w);
+            copy_v(t, w);
+        }
+        for (int t = 0; t < tiles; ++t) {
+            const int key0 = w0 + t * Tile::kKeys;
+            const char* const kt = lds + (t % NST) * G::kStageBytes;
             const char* const vt = kt + Tile::kBytes;
-            const bool steady = t + NST <= my_tiles;                  // NST - 1 further tiles are under way
-            if (steady) wait_copies_except<(NST - 1) * (G::kCopiesK + G::kCopiesV) + G::kCopiesV>();
+            const bool more = t + NST < tiles;
+            // NST - 1 further tiles are under way, or the last ones
+            if (t + NST <= tiles) wait_copies_except<(NST - 1) * (G::kCopiesK + G::kCopiesV) + G::kCopiesV>();
             else wait_copies_except<0>();
             asm volatile("" ::: "memory");
+            Where next{};
+            if (more) next = locate(t + NST);
             f32x4 s[2];
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb) {
@@ -193,6 +223,15 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
                     s[mb] = mfma16(a, qf[ks], s[mb]);
                 }
             }
+            uint32_t v_scales[2] = {0u, 0u};
+            if constexpr (E4M3) {
+#pragma unroll
+                for (int mb = 0; mb < 2; ++mb) v_scales[mb] = *reinterpret_cast<const uint32_t*>(kt + 2 * Tile::kBytes + 32 + mb * 16 + quad * 4);
+            }
+            // K's buffer is free once its reads have returned
+            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+            asm volatile("" : "+v"(v_scales[0]), "+v"(v_scales[1]) :: "memory");
+            if (more) copy_k(t + NST, next);
             // element i of block mb: key key0 + 16 mb + 4 quad + i
             const bool masked = key0 + Tile::kKeys - 1 > min(tile_limit, w1 - 1);
             const int seen = min(limit, w1 - 1) - key0 - 4 * quad;
@@ -204,17 +243,11 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
                         if (16 * mb + i > seen) s[mb][i] = -INFINITY;
             }
             float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            top = fmaxf(top, __shfl_xor(top, 16, 64));
-            top = fmaxf(top, __shfl_xor(top, 32, 64));
+            top = quads_max(top);
             const float m_new = fmaxf(m, top);
             const float m_ref = m_new == -INFINITY ? 0.f : m_new;
             const float alpha = fast_exp2((m - m_ref) * c), mc = m_ref * c;
             m = m_new;
-            uint32_t v_scales[2] = {0u, 0u};
-            if constexpr (E4M3) {
-#pragma unroll
-                for (int mb = 0; mb < 2; ++mb) v_scales[mb] = *reinterpret_cast<const uint32_t*>(kt + 2 * Tile::kBytes + 32 + mb * 16 + quad * 4);
-            }
             float sum = 0.f;
             union { u32x4 u; bf16x8 v; } w;
 #pragma unroll
@@ -225,7 +258,10 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
                     e[i] = fast_exp2(fmaf(s[mb][i], c, -mc));
                     sum += e[i];
                     // (a scale behind the last key is whatever the page holds)
-                    if constexpr (E4M3) e[i] = masked && 16 * mb + i > seen ? 0.f : e[i] * scale_of((v_scales[mb] >> (8 * i)) & 0xffu);
+                    if constexpr (E4M3) {
+                        e[i] *= scale_of((v_scales[mb] >> (8 * i)) & 0xffu);
+                        if (masked) e[i] = 16 * mb + i > seen ? 0.f : e[i];
+                    }
                 }
                 w.u[2 * mb] = pack_bf16(e[0], e[1]);
                 w.u[2 * mb + 1] = pack_bf16(e[2], e[3]);
@@ -235,7 +271,8 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
 #pragma unroll
                 for (int i = 0; i < DB; ++i) acc[i] *= alpha;
             }
-            if (steady) wait_copies_except<(NST - 1) * (G::kCopiesK + G::kCopiesV)>();
+            if (more) wait_copies_except<(NST - 1) * (G::kCopiesK + G::kCopiesV) + G::kCopiesK>();
+            else if (t + NST <= tiles) wait_copies_except<(NST - 1) * (G::kCopiesK + G::kCopiesV)>();
             asm volatile("" ::: "memory");
             const int v_row = quad * 4 + (r16 >> 2), v_byte = (r16 & 3) * 8;
             auto add_values = [&](f32x4 (&sum_of)[DB]) {
@@ -266,10 +303,10 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
                     }
                 }
             };
-            // A weight of 0 hides a value only if the value is finite.  Where rows of several tokens share a masked tile and one of its
-            // values is not, the tokens take their products one by one, the last first, with the keys behind each set to zero.
-            if (masked && first_token < last_token && tile_not_finite<D, E4M3>(vt, lane)) {
-                char* const zeroed = mine + (vt - mine);
+            // A weight of 0 hides a value only if the value is finite.  Where some row does not see all of a tile and one of its values is not,
+            // the tokens take their products one by one, the last first, with the keys behind each set to zero.
+            if (masked && tile_not_finite<D, E4M3>(vt, lane)) {
+                char* const zeroed = lds + (vt - lds);
                 for (int tk = last_token; tk >= first_token; --tk) {
                     for (int r = max(it.kv - it.n + tk + 1 - key0, 0); r < Tile::kKeys; ++r)
                         if (lane < Tile::kChunks) *reinterpret_cast<u32x4*>(zeroed + r * Tile::kRowBytes + lane * 16) = u32x4{0u, 0u, 0u, 0u};
@@ -284,117 +321,131 @@ __global__ __launch_bounds__(kThreads) void paged_few_kernel(PagedAttnParams p) 
             } else {
                 add_values(acc);
             }
-            // the tile's buffers are free once its reads have returned
-            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): V's buffer is free as well
             asm volatile("" ::: "memory");
-            if (t + NST < my_tiles) issue(t + NST);
+            if (more) copy_v(t + NST, next);
         }
         w0 = w1;
     }
 
-    // ---- the four waves' shares meet in LDS
+    // ---- results: the lanes of a row hold a quarter of its weights' sum each
     l += __shfl_xor(l, 16, 64);
     l += __shfl_xor(l, 32, 64);
-    __syncthreads();                               // (every copy has been waited for by the wave that issued it)
-    if (quad == 0) {
-        if (limit >= bad_key) l = __builtin_nanf("");
-        stats[wave][r16] = make_float2(m, l);
-    }
-    float* const sums = reinterpret_cast<float*>(lds) + wave * R * D;
+    if (!real) return;
+    if (limit >= bad_key) l = __builtin_nanf("");
+    const int64_t row = it.row_start + token, part_row = ((int64_t)it.part + it.chunk) * R + r16;
+    const bool whole = it.chunks == 1;
+    if (!whole && part_row >= p.few_part_rows) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;            // no key: O = 0; a bad page: NaN
+    auto store4 = [&](int col, float a, float b, float d, float e) {
+        if (!whole) *reinterpret_cast<f32x4*>(p.part_o + part_row * D + col) = f32x4{a, b, d, e};
+        else if (col < hd) *reinterpret_cast<u32x2*>(p.o + (row * p.q_heads + q_head) * hd + col) = u32x2{pack_bf16(a * inv, b * inv), pack_bf16(d * inv, e * inv)};
+    };
     if constexpr (E4M3) {
 #pragma unroll
         for (int cb = 0; cb < D / 32; ++cb)
 #pragma unroll
-            for (int i = 0; i < 4; i += 2)
-                *reinterpret_cast<f32x4*>(sums + r16 * D + cb * 32 + quad * 8 + 2 * i) =
-                    f32x4{acc[2 * cb][i], acc[2 * cb + 1][i], acc[2 * cb][i + 1], acc[2 * cb + 1][i + 1]};
+            for (int i = 0; i < 4; i += 2) store4(cb * 32 + quad * 8 + 2 * i, acc[2 * cb][i], acc[2 * cb + 1][i], acc[2 * cb][i + 1], acc[2 * cb + 1][i + 1]);
     } else {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) *reinterpret_cast<f32x4*>(sums + r16 * D + db * 16 + quad * 4) = acc[db];
+        for (int db = 0; db < DB; ++db) store4(db * 16 + quad * 4, acc[db][0], acc[db][1], acc[db][2], acc[db][3]);
     }
-    __syncthreads();
-    const bool whole = it.chunks == 1;
-    for (int e = threadIdx.x; e < R * (D / 4); e += kThreads) {
-        const int r = e / (D / 4), col = e % (D / 4) * 4;
-        const int rr = it.tile * R + r, tk = rr / p.group, hq = it.head * p.group + rr % p.group;
-        if (tk >= it.n) continue;
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, stats[w][r].x);
-        const float ref = top == -INFINITY ? 0.f : top;
-        float total = 0.f;
-        f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const float2 st = stats[w][r];
-            const float f = fast_exp2((st.x - ref) * c);
-            total += f * st.y;
-            o += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(lds) + (w * R + r) * D + col);
-        }
-        const int64_t row = it.row_start + tk;
-        if (whole) {
-            const float inv = total == 0.f ? 0.f : 1.f / total;       // no key: O = 0; a bad page: NaN
-            if (col < hd) {
-                u32x2 x;
-                x[0] = pack_bf16(o[0] * inv, o[1] * inv);
-                x[1] = pack_bf16(o[2] * inv, o[3] * inv);
-                *reinterpret_cast<u32x2*>(p.o + (row * p.q_heads + hq) * hd + col) = x;
-            }
-            if (col == 0 && p.lse) p.lse[(int64_t)hq * p.rows.total_rows + row] = total == 0.f ? -INFINITY : (top * c + __log2f(total)) * kLn2;
-        }
-        const int64_t part_row = ((int64_t)it.part + it.chunk) * R + r;
-        if (!whole && part_row < p.few_part_rows) {
-            *reinterpret_cast<f32x4*>(p.part_o + part_row * D + col) = o;
-            if (col == 0) p.part_stats[part_row] = make_float2(top, total);
-        }
-        if (col == 0 && it.chunk == 0) p.where[row * p.q_heads + hq] = where_entry(part_row, it.chunks, false);
+    if (quad == 0) {
+        if (!whole) p.part_stats[part_row] = make_float2(m, l);
+        else if (p.lse) p.lse[(int64_t)q_head * p.rows.total_rows + row] = l == 0.f ? -INFINITY : (m * c + __log2f(l)) * kLn2;
+        if (it.chunk == 0) p.where[row * p.q_heads + q_head] = where_entry(part_row, it.chunks, false);
     }
 }
 
-// Chunks' results of a row joined: a wave per (row, query head).
-//   M = max m_i, L = sum exp2(c (m_i - M)) l_i, O = sum exp2(c (m_i - M)) o_i / L
+// ---- chunks' results joined, for the (row, query head) pairs that have several
+//   M = max m_i,  L = sum exp2(c (m_i - M)) l_i,  O = sum exp2(c (m_i - M)) o_i / L
+// Sums, weights and the maximum are carried along the chunks together, so that nothing is read twice and nothing waits for a maximum; the order of a
+// sum depends on the number of chunks alone.
+struct Joined {
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+    float top = -INFINITY, total = 0.f;
+    __device__ __forceinline__ void add(float2 st, f32x4 x, float c) {
+        const float m = fmaxf(top, st.x), ref = m == -INFINITY ? 0.f : m;
+        const float keep = fast_exp2((top - ref) * c), f = fast_exp2((st.x - ref) * c);
+        total = total * keep + f * st.y;
+        sum = sum * keep + f * x;
+        top = m;
+    }
+};
+
+// A pair's entry; no chunks where there is nothing to join: the result is in o already, or the row belongs to no sequence (no entry then)
+struct Pair {
+    int first, chunks, stride;
+};
+__device__ __forceinline__ Pair pair_at(const PagedAttnParams& p, int64_t unit) {
+    const int2 w = p.where[unit];
+    const int64_t begin = (int64_t)max(p.rows.cu_rows[0], 0) * p.q_heads, end = (int64_t)p.rows.cu_rows[p.rows.num_seqs] * p.q_heads;
+    Pair r{w.x, w.y & 0x3fffffff, w.y >> 30 & 1 ? kManyRows : kFewRows};
+    if (unit < begin || unit >= end || r.chunks <= 1 || r.first < 0 || (int64_t)r.first + (int64_t)(r.chunks - 1) * r.stride >= p.part_rows) r.chunks = 0;
+    return r;
+}
+
+// chunks from, from + step, ... of a pair, four of them read at a time; columns col .. col + 3
 template <int D>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(PagedAttnParams p) {
-    constexpr int kPer = D / 64;
-    const int lane = threadIdx.x & 63;
-    const int64_t unit = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (unit >= (int64_t)p.rows.total_rows * p.q_heads) return;
-    const int row = (int)(unit / p.q_heads), head = (int)(unit % p.q_heads);
-    if (sequence_of(p.rows, row) < 0) return;
-    const int2 at = p.where[unit];
-    const bool many = at.y >> 30 & 1;
-    const int chunks = at.y & 0x3fffffff, tile_rows = many ? kManyRows : kFewRows;
-    if (chunks <= 1 || at.x < 0 || (int64_t)at.x + (int64_t)(chunks - 1) * tile_rows >= p.part_rows) return;
-    const float c = p.scale_log2;
-    float top = -INFINITY;
-    for (int i = lane; i < chunks; i += 64) top = fmaxf(top, p.part_stats[at.x + i * tile_rows].x);
+__device__ __forceinline__ Joined gather(const PagedAttnParams& p, const Pair& pair, int from, int step, int col) {
+    constexpr int kAtOnce = 4;
+    Joined r;
+    for (int j = from; j < pair.chunks; j += step * kAtOnce) {
+        float2 st[kAtOnce];
+        f32x4 x[kAtOnce];
 #pragma unroll
-    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-    const float ref = top == -INFINITY ? 0.f : top;
-    float total = 0.f, o[kPer];
+        for (int i = 0; i < kAtOnce; ++i) {
+            const int64_t at = pair.first + (int64_t)min(j + i * step, pair.chunks - 1) * pair.stride;
+            st[i] = p.part_stats[at];
+            x[i] = *reinterpret_cast<const f32x4*>(p.part_o + at * D + col);
+        }
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) o[j] = 0.f;
-    for (int i = 0; i < chunks; ++i) {
-        const int64_t r = at.x + (int64_t)i * tile_rows;
-        const float2 st = p.part_stats[r];
-        const float f = fast_exp2((st.x - ref) * c);
-        total += f * st.y;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) o[j] += f * p.part_o[r * D + lane * kPer + j];
+        for (int i = 0; i < kAtOnce; ++i)
+            if (j + i * step < pair.chunks) r.add(st[i], x[i], p.scale_log2);
     }
-    const float inv = total == 0.f ? 0.f : 1.f / total;
-    const int hd = p.pool.head_dim;
-    uint16_t* const dst = p.o + unit * hd;
-    if (lane * kPer < hd) {
-        if constexpr (kPer == 2) *reinterpret_cast<uint32_t*>(dst + lane * 2) = pack_bf16(o[0] * inv, o[1] * inv);
-        else dst[lane] = (uint16_t)pack_bf16(o[0] * inv, 0.f);
-    }
-    if (lane == 0 && p.lse) p.lse[(int64_t)head * p.rows.total_rows + row] = total == 0.f ? -INFINITY : (top * c + __log2f(total)) * kLn2;
+    return r;
+}
+
+__device__ __forceinline__ void put(const PagedAttnParams& p, const Joined& r, int64_t unit, int col) {
+    const float inv = r.total == 0.f ? 0.f : 1.f / r.total;
+    if (col < p.pool.head_dim)
+        *reinterpret_cast<u32x2*>(p.o + unit * p.pool.head_dim + col) = u32x2{pack_bf16(r.sum[0] * inv, r.sum[1] * inv), pack_bf16(r.sum[2] * inv, r.sum[3] * inv)};
+    if (col == 0 && p.lse)
+        p.lse[unit % p.q_heads * p.rows.total_rows + unit / p.q_heads] = r.total == 0.f ? -INFINITY : (r.top * p.scale_log2 + __log2f(r.total)) * kLn2;
+}
+
+// Many pairs: a team of D / 4 lanes per pair, its chunks one after the other.  Bound by latency: as many pairs as fit are under way at once.
+template <int D>
+__global__ __launch_bounds__(kThreads, 8) void paged_join_kernel(PagedAttnParams p) {
+    constexpr int kLanes = D / 4, kTeams = kThreads / kLanes;
+    const int64_t units = (int64_t)p.rows.total_rows * p.q_heads, unit = (int64_t)blockIdx.x * kTeams + threadIdx.x / kLanes;
+    const int col = threadIdx.x % kLanes * 4;
+    if (unit >= units) return;
+    const Pair pair = pair_at(p, unit);
+    if (pair.chunks) put(p, gather<D>(p, pair, 0, 1, col), unit, col);
+}
+
+// Few pairs, of many chunks perhaps: a workgroup for COLUMNS columns of one, the chunks dealt out to its teams.
+template <int D, int COLUMNS>
+__global__ __launch_bounds__(kThreads) void paged_join_pair_kernel(PagedAttnParams p) {
+    constexpr int kLanes = COLUMNS / 4, kTeams = kThreads / kLanes;
+    __shared__ f32x4 sums[kTeams][kLanes];
+    __shared__ float2 stats[kTeams];
+    const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes, col = blockIdx.y * COLUMNS + lane * 4;
+    const Pair pair = pair_at(p, blockIdx.x);
+    if (pair.chunks == 0) return;
+    Joined r = gather<D>(p, pair, team, kTeams, col);
+    sums[team][lane] = r.sum;
+    if (lane == 0) stats[team] = make_float2(r.top, r.total);
+    __syncthreads();
+    if (team) return;
+    for (int g = 1; g < min(kTeams, pair.chunks); ++g) r.add(stats[g], sums[g][lane], p.scale_log2);
+    put(p, r, blockIdx.x, col);
 }
 
 template <int D, bool E4M3>
 void launch_few(const PagedAttnParams& p, const PagedSizes& sizes, hipStream_t stream) {
-    hipLaunchKernelGGL((paged_few_kernel<D, E4M3>), dim3((unsigned)sizes.few_grid), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((paged_few_kernel<D, E4M3>), dim3((unsigned)sizes.few_grid), dim3(kWave), 0, stream, p);
 }
 
 }  // namespace
@@ -408,6 +459,7 @@ PagedSizes paged_sizes(const PagedRows& rows, int max_rows, int page_shift, int 
     s.few = most <= kFewRows || rows.num_seqs > 1;
     s.many = most > kFewRows;
     // (one kernel alone takes every sequence, so that a wrong max_rows costs time and nothing else)
+    s.join = ((int64_t)rows.table_width << page_shift) > unit_keys(false);       // (a single unit is not shared out)
     s.few_limit = !s.many ? 0x7fffffff : s.few ? kFewRows : 0;
     auto bounds = [&](bool many, int few_limit) {
         return grid_bounds(rows.total_rows, rows.num_seqs, rows.table_width, page_shift, group, kv_heads, many, few_limit);
@@ -438,10 +490,24 @@ hipError_t launch_paged_attn(const PagedAttnParams& p, const PagedSizes& sizes, 
     if (sizes.many) {
         if (const hipError_t e = launch_paged_many(p, sizes.many_grid, e4m3, stream)) return e;
     }
-    const int64_t waves = (int64_t)p.rows.total_rows * p.q_heads;
-    const dim3 grid((unsigned)((waves + 3) / 4)), threads(kThreads);
-    if (width == 128) hipLaunchKernelGGL(paged_join_kernel<128>, grid, threads, 0, stream, p);
-    else hipLaunchKernelGGL(paged_join_kernel<64>, grid, threads, 0, stream, p);
+    if (!sizes.join) return hipSuccess;
+    // up to 4096 pairs: a workgroup each (64 rows of 32 heads, 5 to 30 chunks 7 us); long contexts: several, 32 columns each (one row of 32
+    // heads, 256 chunks 10 -> 7 us, but 5 heads of 34 chunks 3.7 -> 4.9); more: teams (22784 pairs of 2 or 3 chunks 19 us with a workgroup for 6)
+    const int64_t pairs = (int64_t)p.rows.total_rows * p.q_heads;
+    const dim3 threads(kThreads);
+    if (pairs > 4096) {
+        const int teams = kThreads / (width / 4);
+        const dim3 grid((unsigned)((pairs + teams - 1) / teams));
+        if (width == 128) hipLaunchKernelGGL(paged_join_kernel<128>, grid, threads, 0, stream, p);
+        else hipLaunchKernelGGL(paged_join_kernel<64>, grid, threads, 0, stream, p);
+    } else if (pairs <= 256 && ((int64_t)p.rows.table_width << p.pool.page_shift) >= 128 * unit_keys(false)) {
+        const dim3 grid((unsigned)pairs, width / 32);
+        if (width == 128) hipLaunchKernelGGL((paged_join_pair_kernel<128, 32>), grid, threads, 0, stream, p);
+        else hipLaunchKernelGGL((paged_join_pair_kernel<64, 32>), grid, threads, 0, stream, p);
+    } else {
+        if (width == 128) hipLaunchKernelGGL((paged_join_pair_kernel<128, 128>), dim3((unsigned)pairs), threads, 0, stream, p);
+        else hipLaunchKernelGGL((paged_join_pair_kernel<64, 64>), dim3((unsigned)pairs), threads, 0, stream, p);
+    }
     return hipGetLastError();
 }
 

@@ -11,12 +11,16 @@ namespace hspmd {
 #define HSPMD_INDEX constexpr inline
 #endif
 
-constexpr int kUnitKeys = 128;       // keys are shared out in units of these
 constexpr int kFewRows = 16;         // rows per tile of the kernel for few rows ...
 constexpr int kManyRows = 128;       // ... and of the one for many
-constexpr int kChunkTarget = 512;    // chunks to aim for: two for each of the 256 compute units
+// Keys are shared out in units of so many.
+HSPMD_INDEX int unit_keys(bool many) { return many ? 128 : 32; }
+// Chunks to aim for, over the 256 compute units.  Few rows: 8 waves each, as many as a unit holds with 8-bit tiles at D = 128; with 16-bit tiles
+// (4 waves) that is two rounds, which even out lengths better than one (64 sequences of 500 .. 16000 keys, 32 heads on 8, one token: bf16 217
+// against 231 us with half as many, e4m3 126 against 164; of 4265 keys each bf16 209 against 206, e4m3 121 against 116 to 133).  Many rows: 2 workgroups each, which
+// is what a unit holds.
+HSPMD_INDEX int chunk_target(bool many) { return many ? 512 : 2048; }
 constexpr int kXcds = 8;             // workgroups go to the XCDs in turn
-constexpr int kWindowPages = 2048;   // page numbers kept in LDS at a time (32768 keys of the smallest pages)
 
 // A sequence's rows and keys as the device arrays give them, clamped to what there is.
 struct SeqRows {
@@ -38,24 +42,29 @@ struct SeqTiles {
 HSPMD_INDEX SeqTiles seq_tiles(const SeqRows& s, int group, int tile_rows, bool many, int few_limit) {
     const int64_t rows = (int64_t)s.n * group;
     if (rows == 0 || (rows > few_limit) != many) return SeqTiles{0, 0};
-    const int units = (s.kv + kUnitKeys - 1) / kUnitKeys;
+    const int units = (int)(((int64_t)s.kv + unit_keys(many) - 1) / unit_keys(many));
     return SeqTiles{(int)((rows + tile_rows - 1) / tile_rows), units > 1 ? units : 1};
 }
 
-// With U the units of all items together, a chunk is to take about U / kChunkTarget of them: the device then has about as many chunks as it
-// takes at once, whatever the mix of lengths.
-HSPMD_INDEX int units_per_chunk(int64_t all_units) {
-    const int64_t per = (all_units + kChunkTarget - 1) / kChunkTarget;
+// With U the units of all items together, a chunk is to take U / chunk_target() of them, so that the device has as many chunks as it takes at
+// once, whatever the mix of lengths; an item's chunks are equal.  Items that end in a short chunk make them more than that: the units per
+// chunk are raised until they are not, by a factor of two at most (where there are more items than that, nothing is gained by it).
+HSPMD_INDEX int units_per_chunk(int64_t all_units, bool many) {
+    const int64_t per = (all_units + chunk_target(many) - 1) / chunk_target(many);
     return per < 1 ? 1 : per > (1 << 24) ? (1 << 24) : (int)per;
 }
-// Chunks of an item: to the nearest number, so that an item a little longer than the others is not cut for it.
+constexpr int kRaises = 3;
+HSPMD_INDEX int raised(int per_chunk, int first, int64_t slots, bool many) {
+    if (slots <= chunk_target(many)) return per_chunk;
+    const int64_t more = (per_chunk * slots + chunk_target(many) - 1) / chunk_target(many);
+    return more < 2 * (int64_t)first ? (int)more : 2 * first;
+}
 struct Shares {
     int chunks, units;   // units of each
 };
 HSPMD_INDEX Shares shares_of(int units, int per_chunk) {
-    const int chunks = (int)((2 * (int64_t)units + per_chunk) / (2 * (int64_t)per_chunk));
-    const int c = chunks < 1 ? 1 : chunks;
-    return Shares{c, (units + c - 1) / c};
+    const int c = (int)(((int64_t)units + per_chunk - 1) / per_chunk);
+    return Shares{c < 1 ? 1 : c, c < 1 ? 0 : (units + c - 1) / c};
 }
 
 // Slots are dealt out to the XCDs in runs: neighbouring slots are row tiles that read the same keys, and meet in one L2.
@@ -64,19 +73,19 @@ HSPMD_INDEX int64_t slot_of_block(int64_t block, int64_t slots) {
     const int64_t run = (slots + kXcds - 1) / kXcds, slot = block % kXcds * run + block / kXcds;
     return block / kXcds < run && slot < slots ? slot : -1;
 }
-// slot within a sequence -> KV head, chunk, row tile (tiles innermost)
+// slot within a sequence -> KV head, chunk, row tile.  Tiles innermost: they read the same keys; the last, which see the most, first.
 struct SlotPlace {
     int head, chunk, tile;
 };
 HSPMD_INDEX SlotPlace place_of_slot(int64_t local, int tiles, int chunks) {
     const int64_t rest = local / tiles;
-    return SlotPlace{(int)(rest / chunks), (int)(rest % chunks), (int)(local % tiles)};
+    return SlotPlace{(int)(rest / chunks), (int)(rest % chunks), tiles - 1 - (int)(local % tiles)};
 }
 // tile of partial results of an item's first chunk, counted from the sequence's first; its chunks follow each other
 HSPMD_INDEX int64_t part_of(const SlotPlace& p, int tiles, int chunks) { return ((int64_t)p.head * tiles + p.tile) * chunks; }
 
 // What the host can say about the number of workgroups and of partial results.  A chunk count is at most units / per_chunk + 1 and, where it is
-// above one, at most 2 units / per_chunk; the sum of units / per_chunk is at most kChunkTarget.
+// above one, at most 2 units / per_chunk; the sum of units / per_chunk is at most chunk_target().
 struct GridBounds {
     int64_t grid, part_tiles;
 };
@@ -96,9 +105,9 @@ HSPMD_INDEX GridBounds grid_bounds(int64_t total_rows, int64_t num_seqs, int64_t
         full = full < 0 ? 0 : full;
     }
     const int64_t items = kv_heads * (full + ends);
-    const int64_t u = ((table_width << page_shift) + kUnitKeys - 1) / kUnitKeys, units = items * (u < 1 ? 1 : u);
-    const int64_t slots = units < items + kChunkTarget ? units : items + kChunkTarget;
-    return GridBounds{(slots + kXcds - 1) / kXcds * kXcds, units < 2 * kChunkTarget ? units : 2 * kChunkTarget};
+    const int64_t u = ((table_width << page_shift) + unit_keys(many) - 1) / unit_keys(many), units = items * (u < 1 ? 1 : u);
+    const int64_t target = chunk_target(many), slots = units < items + target ? units : items + target;
+    return GridBounds{(slots + kXcds - 1) / kXcds * kXcds, units < 2 * target ? units : 2 * target};
 }
 
 }  // namespace hspmd

@@ -15,6 +15,7 @@ namespace hspmd {
 namespace {
 
 constexpr int kTileKeys = kFwdKTile;
+constexpr int kWindowPages = 2048;   // page numbers kept in LDS at a time (32768 keys of the smallest pages)
 
 // Where the item's keys lie.  A copy of 1 KB (kRowsPerPiece rows) stays within a page.
 template <int D, bool E4M3>
@@ -133,8 +134,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
     const int first_limit = offset + wave_row0 / p.group, group_limit = offset + it.tile * kManyRows / p.group;   // ... and the workgroup's first
     const int last_limit = wave_real ? offset + min(it.n - 1, (wave_row0 + 31) / p.group) : -1;
     const int keys_end = max(0, offset + min(it.n - 1, (it.tile * kManyRows + kManyRows - 1) / p.group) + 1);
-    const int64_t unit_keys = (int64_t)it.units * kUnitKeys;
-    const int k0 = (int)min((int64_t)keys_end, it.chunk * unit_keys), k1 = (int)min((int64_t)keys_end, (it.chunk + 1) * unit_keys);
+    const int64_t share = (int64_t)it.units * unit_keys(true);
+    const int k0 = (int)min((int64_t)keys_end, it.chunk * share), k1 = (int)min((int64_t)keys_end, (it.chunk + 1) * share);
 
     FwdState<D, KD, 2> st;
     const uint16_t* const q_row = p.q + (int64_t)(it.row_start + token) * p.q_stride + (int64_t)q_head * hd;
@@ -186,7 +187,14 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
         const int first_page = w0 >> shift;
         const int w1 = (int)min((int64_t)k1, ((int64_t)first_page + kWindowPages) << shift);
         __syncthreads();                                              // every wave has left the previous window's tiles and numbers
-        load_pages(p, it.seq, first_page, ((w1 - 1) >> shift) - first_page + 1, pages, &bad_key);
+        for (int i = threadIdx.x; i <= ((w1 - 1) >> shift) - first_page; i += kThreads) {
+            int page = page_at(p.pool, p.rows, it.seq, first_page + i);
+            if (page < 0) {
+                atomicMin(&bad_key, (first_page + i) << shift);
+                page = 0;                                             // (what is read there is shown to nobody)
+            }
+            pages[i] = page;
+        }
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk) asm volatile("" : "+v"(st.qf[kk]));   // the row is here before copies are under way
         __syncthreads();

@@ -31,7 +31,14 @@ extern "C" int check(const int* cu, const int* len, int num_seqs, int total_rows
             t[i] = seq_tiles(s[i], group, R, kind, limit);
             units += (long)t[i].tiles * t[i].units * kv_heads;
         }
-        const int per = units_per_chunk(units);
+        int per = units_per_chunk(units, kind);
+        for (int raise = 0, first = per; raise < kRaises; ++raise) {
+            long n = 0;
+            for (int i = 0; i < num_seqs; ++i) n += (long)t[i].tiles * kv_heads * shares_of(t[i].units, per).chunks;
+            const int next = raised(per, first, n, kind);
+            if (next == per) break;
+            per = next;
+        }
         std::vector<long> first(num_seqs), first_part(num_seqs);
         for (int i = 0; i < num_seqs; ++i) {
             const Shares sh = shares_of(t[i].units, per);
@@ -144,6 +151,6 @@ def test_arrays_that_make_no_sense(check):
 
 def test_one_long_sequence_is_shared_out_and_equal_ones_are_not(check):
     slots, grid, parts, room = check(_cu([1]), [131001], 1, 8188, 4, 4, 8, 1)[:4]
-    assert slots == parts and 400 <= slots <= 520
-    slots, grid, parts, room = check(_cu([1] * 64), [4096 + 3 * i for i in range(64)], 64, 300, 4, 4, 8, 1)[:4]
+    assert slots == parts and 800 <= slots <= grid
+    slots, grid, parts, room = check(_cu([64] * 64), [4096 + 3 * i for i in range(64)], 64 * 64, 300, 4, 2, 8, 64)[4:]
     assert slots == 512 and parts == 0
