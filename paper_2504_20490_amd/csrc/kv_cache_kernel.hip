@@ -30,30 +30,37 @@ __global__ __launch_bounds__(kThreads) void kv_cache_write_kernel(CacheWritePara
         }
         if (sub < heads_at_once) load_turn<VEC>(p.rope, pos, piece * VEC, half, c, s);
     }
-    const int kv = p.pool.kv_heads, heads = p.q_heads + 2 * kv;
-    for (int h0 = share * heads_at_once; h0 < heads; h0 += p.shares * heads_at_once) {
-        const int h = h0 + sub;
-        const bool mine = sub < heads_at_once && h < heads;
-        const bool is_q = h < p.q_heads, is_v = h >= p.q_heads + kv;
-        const int head = is_q ? h : is_v ? h - p.q_heads - kv : h - p.q_heads;
+    // rounds of heads, those of q, of k and of v: everything but the lane's place in a round is the same for the wave
+    const int kv = p.pool.kv_heads, q_rounds = (p.q_heads + heads_at_once - 1) / heads_at_once, kv_rounds = (kv + heads_at_once - 1) / heads_at_once;
+    const int mine = sub * hd + piece * VEC, shift = p.pool.page_shift;
+    const uint32_t place = (uint32_t)(sub << shift) * (uint32_t)p.pool.row_bytes;      // of the lane's head in a page, from the round's first
+    const bool lane_used = sub < heads_at_once;
+    for (int round = share; round < q_rounds + 2 * kv_rounds; round += p.shares) {
+        const bool is_q = round < q_rounds, is_v = round >= q_rounds + kv_rounds;
+        const int h0 = (is_q ? round : is_v ? round - q_rounds - kv_rounds : round - q_rounds) * heads_at_once;
+        const bool in = lane_used && h0 + sub < (is_q ? p.q_heads : kv);
+        const uint16_t* const src = (is_q ? p.q : is_v ? p.v : p.k) + row * (is_q ? p.q_stride : p.kv_stride) + h0 * hd;
         float lo[VEC], hi[VEC];
 #pragma unroll
         for (int j = 0; j < VEC; ++j) lo[j] = hi[j] = 0.f;
-        if (mine) {
-            const uint16_t* src = is_q ? p.q : is_v ? p.v : p.k;
-            const int64_t from = row * (is_q ? p.q_stride : p.kv_stride) + head * hd + piece * VEC;
-            load_floats<VEC, false>(src, from, lo);
-            load_floats<VEC, false>(src, from + half, hi);
-            if (turned && !is_v)
+        if (in) {
+            load_floats<VEC, false>(src, mine, lo);
+            load_floats<VEC, false>(src, mine + half, hi);
+        }
+        if (turned && !is_v)
 #pragma unroll
-                for (int j = 0; j < VEC; ++j) turn_pair(lo[j], hi[j], c[j], s[j], lo[j], hi[j]);
+            for (int j = 0; j < VEC; ++j) turn_pair(lo[j], hi[j], c[j], s[j], lo[j], hi[j]);
+        if (is_q) {
+            uint16_t* const to = p.q_out + row * p.q_out_stride + h0 * hd;
+            if (in) {
+                store_floats<VEC, false>(to, mine, lo);
+                store_floats<VEC, false>(to, mine + half, hi);
+            }
+            continue;
         }
-        if (mine && is_q) {
-            const int64_t to = row * p.q_out_stride + head * hd + piece * VEC;
-            store_floats<VEC, false>(p.q_out, to, lo);
-            store_floats<VEC, false>(p.q_out, to + half, hi);
-        }
-        int e = 0;
+        if (at.page < 0) continue;
+        const int64_t token = ((int64_t)h0 << shift) + at.slot;
+        uint8_t* const dst = (is_v ? p.pool.v : p.pool.k) + at.page * p.pool.page_bytes + token * p.pool.row_bytes + place;
         if constexpr (E4M3) {
             float amax = 0.f;
 #pragma unroll
@@ -65,15 +72,10 @@ __global__ __launch_bounds__(kThreads) void kv_cache_write_kernel(CacheWritePara
             for (int step = 1; step < pieces; step *= 2) {
                 int from = piece + step;
                 from = (from >= pieces ? from - pieces : from) + sub * pieces;
-                amax = fmaxf(amax, __shfl(amax, sub < heads_at_once ? from : lane, 64));
+                amax = fmaxf(amax, __shfl(amax, lane_used ? from : lane, 64));
             }
-            e = e4m3_exponent(amax);
-        }
-        if (!mine || is_q || at.page < 0) continue;
-        uint8_t* const cache = is_v ? p.pool.v : p.pool.k;
-        const int64_t token = ((int64_t)head << p.pool.page_shift) + at.slot;
-        uint8_t* const dst = cache + at.page * p.pool.page_bytes + token * p.pool.row_bytes;
-        if constexpr (E4M3) {
+            if (!in) continue;
+            const int e = e4m3_exponent(amax);
             const float unit_of = pow2(-e);
 #pragma unroll
             for (int part = 0; part < 2; ++part) {
@@ -94,10 +96,9 @@ __global__ __launch_bounds__(kThreads) void kv_cache_write_kernel(CacheWritePara
             }
             if (piece == 0) {
                 if (hd & 8) *reinterpret_cast<u32x2*>(dst + hd) = u32x2{0u, 0u};   // the columns up to a multiple of 16
-                uint8_t* const scales = is_v ? p.pool.v_scale : p.pool.k_scale;
-                scales[at.page * p.pool.scale_page_bytes + token] = (uint8_t)(e + 127);
+                (is_v ? p.pool.v_scale : p.pool.k_scale)[at.page * p.pool.scale_page_bytes + token + (sub << shift)] = (uint8_t)(e + 127);
             }
-        } else {
+        } else if (in) {
             store_floats<VEC, false>(dst, piece * VEC, lo);
             store_floats<VEC, false>(dst, half + piece * VEC, hi);
         }
@@ -146,7 +147,7 @@ hipError_t launch_cache_write(CacheWriteParams p, bool e4m3, hipStream_t stream)
     if (p.rows.total_rows == 0 || p.rows.num_seqs == 0) return hipSuccess;
     const int half = p.pool.head_dim / 2, vec = half % 8 == 0 ? 8 : 4;
     const int heads_at_once = 64 / (half / vec);
-    const int rounds = (p.q_heads + 2 * p.pool.kv_heads + heads_at_once - 1) / heads_at_once;
+    const int rounds = (p.q_heads + heads_at_once - 1) / heads_at_once + 2 * ((p.pool.kv_heads + heads_at_once - 1) / heads_at_once);
     p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, (4096 + p.rows.total_rows - 1) / p.rows.total_rows));
     const int64_t units = (int64_t)p.rows.total_rows * p.shares;
     const dim3 grid((unsigned)((units + 3) / 4)), threads(kThreads);

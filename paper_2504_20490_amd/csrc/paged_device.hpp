@@ -74,7 +74,7 @@ __device__ __forceinline__ void turn_pair(float lo, float hi, float c, float s, 
 
 // VEC consecutive elements, 2 or 4 bytes each, as floats and back
 template <int VEC, bool F32>
-__device__ __forceinline__ void load_floats(const void* base, int64_t elem, float (&x)[VEC]) {
+__device__ __forceinline__ void load_floats(const void* base, int elem, float (&x)[VEC]) {
     if constexpr (F32) {
 #pragma unroll
         for (int j = 0; j < VEC; j += 4) {
@@ -93,7 +93,7 @@ __device__ __forceinline__ void load_floats(const void* base, int64_t elem, floa
     }
 }
 template <int VEC, bool F32>
-__device__ __forceinline__ void store_floats(void* base, int64_t elem, const float (&x)[VEC]) {
+__device__ __forceinline__ void store_floats(void* base, int elem, const float (&x)[VEC]) {
     if constexpr (F32) {
 #pragma unroll
         for (int j = 0; j < VEC; j += 4)

@@ -20,7 +20,6 @@ HSPMD_INDEX int unit_keys(bool many) { return many ? 128 : 32; }
 // against 231 us with half as many, e4m3 126 against 164; of 4265 keys each bf16 209 against 206, e4m3 121 against 116 to 133).  Many rows: 2 workgroups each, which
 // is what a unit holds.
 HSPMD_INDEX int chunk_target(bool many) { return many ? 512 : 2048; }
-constexpr int kXcds = 8;             // workgroups go to the XCDs in turn
 
 // A sequence's rows and keys as the device arrays give them, clamped to what there is.
 struct SeqRows {
@@ -67,19 +66,15 @@ HSPMD_INDEX Shares shares_of(int units, int per_chunk) {
     return Shares{c < 1 ? 1 : c, c < 1 ? 0 : (units + c - 1) / c};
 }
 
-// Slots are dealt out to the XCDs in runs: neighbouring slots are row tiles that read the same keys, and meet in one L2.
-// -1: the workgroup has none.
-HSPMD_INDEX int64_t slot_of_block(int64_t block, int64_t slots) {
-    const int64_t run = (slots + kXcds - 1) / kXcds, slot = block % kXcds * run + block / kXcds;
-    return block / kXcds < run && slot < slots ? slot : -1;
-}
-// slot within a sequence -> KV head, chunk, row tile.  Tiles innermost: they read the same keys; the last, which see the most, first.
+// slot within a sequence -> KV head, chunk, row tile.  The last row tiles, which see the most keys, come first (a workgroup that starts late has
+// little to do); heads are innermost: workgroups go to the XCDs in turn, so that with 8 heads, or 16, the tiles and chunks of a head meet in one L2.
+// 12 prompts of 300 .. 4000 tokens, 16 heads, 165 us against 215 with the heads outermost and first tiles first.
 struct SlotPlace {
     int head, chunk, tile;
 };
-HSPMD_INDEX SlotPlace place_of_slot(int64_t local, int tiles, int chunks) {
-    const int64_t rest = local / tiles;
-    return SlotPlace{(int)(rest / chunks), (int)(rest % chunks), tiles - 1 - (int)(local % tiles)};
+HSPMD_INDEX SlotPlace place_of_slot(int64_t local, int tiles, int chunks, int heads) {
+    const int64_t rest = local / heads;
+    return SlotPlace{(int)(local % heads), (int)(rest % chunks), tiles - 1 - (int)(rest / chunks)};
 }
 // tile of partial results of an item's first chunk, counted from the sequence's first; its chunks follow each other
 HSPMD_INDEX int64_t part_of(const SlotPlace& p, int tiles, int chunks) { return ((int64_t)p.head * tiles + p.tile) * chunks; }
@@ -107,7 +102,7 @@ HSPMD_INDEX GridBounds grid_bounds(int64_t total_rows, int64_t num_seqs, int64_t
     const int64_t items = kv_heads * (full + ends);
     const int64_t u = ((table_width << page_shift) + unit_keys(many) - 1) / unit_keys(many), units = items * (u < 1 ? 1 : u);
     const int64_t target = chunk_target(many), slots = units < items + target ? units : items + target;
-    return GridBounds{(slots + kXcds - 1) / kXcds * kXcds, units < 2 * target ? units : 2 * target};
+    return GridBounds{slots, units < 2 * target ? units : 2 * target};
 }
 
 }  // namespace hspmd

@@ -71,18 +71,17 @@ __device__ __forceinline__ PagedItem find_item(const PagedAttnParams& p) {
         per_chunk = next;
     }
     const uint32_t slots_to = lanes_up_to(slots), parts_to = lanes_up_to(parts);
-    const int64_t slot64 = slot_of_block(blockIdx.x, (uint32_t)__builtin_amdgcn_readlane((int)slots_to, 63));
-    const uint32_t slot = (uint32_t)slot64;
+    const uint32_t slot = blockIdx.x;
     PagedItem it{};
     it.seq = -1;
     uint32_t first = slots_to - slots, part = parts_to - parts;
-    if (slot64 >= 0 && slot >= first && slot < slots_to)
+    if (slot >= first && slot < slots_to)
         for (int i = 0; i < per_lane; ++i) {
             if (per_lane > 1) look(i);
             const Shares sh = shares_of(t.units, per_chunk);
             const uint32_t n = slots_of(sh);
             if (slot - first < n) {
-                const SlotPlace at = place_of_slot(slot - first, t.tiles, sh.chunks);
+                const SlotPlace at = place_of_slot(slot - first, t.tiles, sh.chunks, kvh);
                 const int64_t mine = part + part_of(at, t.tiles, sh.chunks);
                 it = PagedItem{lane * per_lane + i, s.start, s.n, s.kv, at.tile, at.head, at.chunk, sh.chunks, sh.units,
                                (int)min(mine, (int64_t)(0x7fffffff / kRows))};

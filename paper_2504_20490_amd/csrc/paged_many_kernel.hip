@@ -350,10 +350,16 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
         w0 = w1;
     }
 
-    // ---- results
+    // ---- results.  The row as a new value of the lane index, which the tile loop then does not have to keep.
+    int lane_now = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane_now));
+    const int r = lane_now & 31, half = lane_now >> 5;
+    const int my_token = (wave_row0 + r) / p.group, my_head = it.head * p.group + (wave_row0 + r) % p.group;
+    const bool exists = my_token < it.n;
+    const int seen_to = exists ? offset + my_token : -1;
     float l_row = st.l + partner32(st.l);
     __syncthreads();                                                  // every wave has left the tiles
-    if (my_limit >= bad_key) l_row = __builtin_nanf("");
+    if (seen_to >= bad_key) l_row = __builtin_nanf("");
     if (!wave_real) return;
     if (taken_out) {
         for (int key = max(k0, group_limit + 1 - BK); key < k1; ++key) {      // (from the start of the first tile that was looked at, or before)
@@ -366,7 +372,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int i4 = 0; i4 < 4; ++i4) {
-                    const int col = db * 32 + i4 * 8 + hh * 4;
+                    const int col = db * 32 + i4 * 8 + half * 4;
                     u32x2 w = {0u, 0u};
                     if (col < hd) {
                         if constexpr (E4M3) w = e4m3_to_bf16(*reinterpret_cast<const uint32_t*>(row + col), scale);
@@ -375,43 +381,42 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float x = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
-                        if (key <= my_limit && !is_finite(x)) st.acc[db][4 * i4 + j] += x;
+                        if (key <= seen_to && !is_finite(x)) st.acc[db][4 * i4 + j] += x;
                     }
                 }
         }
     }
     const bool whole = it.chunks == 1;
     const int64_t part_row0 = p.few_part_rows + ((int64_t)it.part + it.chunk) * kManyRows + wave * 32;
-    if (hh == 0 && real) {
-        const int64_t row = it.row_start + token;
-        if (it.chunk == 0) p.where[row * p.q_heads + q_head] = where_entry(part_row0 + (lane & 31), it.chunks, true);
-        if (whole && p.lse) p.lse[(int64_t)q_head * p.rows.total_rows + row] = l_row == 0.f ? -INFINITY : (st.m * c + __log2f(l_row)) * kLn2;
+    if (half == 0 && exists) {
+        const int64_t row = it.row_start + my_token;
+        if (it.chunk == 0) p.where[row * p.q_heads + my_head] = where_entry(part_row0 + r, it.chunks, true);
+        if (whole && p.lse) p.lse[(int64_t)my_head * p.rows.total_rows + row] = l_row == 0.f ? -INFINITY : (st.m * c + __log2f(l_row)) * kLn2;
     }
     char* const area = lds + wave * (32 * D * 4);
     if (!whole) {
         if (part_row0 + 32 > p.part_rows) return;
-        if (hh == 0) p.part_stats[part_row0 + (lane & 31)] = make_float2(st.m, l_row);
-        store_tile_f32<D, false>(area, st.acc, 1.f, p.part_o + part_row0 * D, D, 32, D, lane);
+        if (half == 0) p.part_stats[part_row0 + r] = make_float2(st.m, l_row);
+        store_tile_f32<D, false>(area, st.acc, 1.f, p.part_o + part_row0 * D, D, 32, D, lane_now);
         return;
     }
     // O leaves through LDS as in store_tile_bf16, but a row's address follows from its token and query head
     constexpr int kChunks = D / 8, kRowsPerInstr = 64 / kChunks;
     const float inv = l_row == 0.f ? 0.f : 1.f / l_row;
-    const int r = lane & 31;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int i4 = 0; i4 < 4; ++i4) {
-            const int col = db * 32 + i4 * 8 + hh * 4;
+            const int col = db * 32 + i4 * 8 + half * 4;
             u32x2 w;
             w[0] = pack_bf16(st.acc[db][4 * i4 + 0] * inv, st.acc[db][4 * i4 + 1] * inv);
             w[1] = pack_bf16(st.acc[db][4 * i4 + 2] * inv, st.acc[db][4 * i4 + 3] * inv);
             *reinterpret_cast<u32x2*>(area + (r * kChunks + ((col / 8) ^ (r & (kChunks - 1)))) * 16 + (col & 4) * 2) = w;
         }
-    const int chunk = lane % kChunks;
+    const int chunk = lane_now % kChunks;
 #pragma unroll
     for (int i = 0; i < 32 / kRowsPerInstr; ++i) {
-        const int row = i * kRowsPerInstr + lane / kChunks, x = wave_row0 + row, t = x / p.group;
+        const int row = i * kRowsPerInstr + lane_now / kChunks, x = wave_row0 + row, t = x / p.group;
         if (t < it.n && chunk * 8 < hd)
             *reinterpret_cast<u32x4*>(p.o + ((int64_t)(it.row_start + t) * p.q_heads + it.head * p.group + x % p.group) * hd + chunk * 8) =
                 *reinterpret_cast<const u32x4*>(area + (row * kChunks + (chunk ^ (row & (kChunks - 1)))) * 16);

@@ -27,22 +27,23 @@ __global__ __launch_bounds__(kThreads) void rope_axes_kernel(RopeAxesParams p) {
     load_turn<VEC>(p.rope, pos, piece * VEC, half, c, s);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) s[j] *= p.sin_sign;
-    const int heads = p.q_heads + p.kv_heads;
-    for (int h0 = share * heads_at_once; h0 < heads; h0 += p.shares * heads_at_once) {
-        const int h = h0 + sub;
-        if (h >= heads) continue;
-        const bool is_k = h >= p.q_heads;
-        const void* src = is_k ? p.k : p.q;
-        void* dst = is_k ? p.k_out : p.q_out;
-        const int col = (is_k ? h - p.q_heads : h) * p.head_dim + piece * VEC;
-        const int64_t from = token * (is_k ? p.kv_stride : p.q_stride) + col, to = token * (is_k ? p.kv_out_stride : p.q_out_stride) + col;
+    // rounds of heads, those of q and then those of k: everything but the lane's place in a round is the same for the wave
+    const int q_rounds = (p.q_heads + heads_at_once - 1) / heads_at_once, k_rounds = (p.kv_heads + heads_at_once - 1) / heads_at_once;
+    const int mine = sub * p.head_dim + piece * VEC;
+    for (int round = share; round < q_rounds + k_rounds; round += p.shares) {
+        const bool is_k = round >= q_rounds;
+        const int h0 = (is_k ? round - q_rounds : round) * heads_at_once;
+        if (h0 + sub >= (is_k ? p.kv_heads : p.q_heads)) continue;
+        constexpr int kBytes = F32 ? 4 : 2;
+        const char* const src = static_cast<const char*>(is_k ? p.k : p.q) + (token * (is_k ? p.kv_stride : p.q_stride) + h0 * p.head_dim) * kBytes;
+        char* const dst = static_cast<char*>(is_k ? p.k_out : p.q_out) + (token * (is_k ? p.kv_out_stride : p.q_out_stride) + h0 * p.head_dim) * kBytes;
         float lo[VEC], hi[VEC];
-        load_floats<VEC, F32>(src, from, lo);
-        load_floats<VEC, F32>(src, from + half, hi);
+        load_floats<VEC, F32>(src, mine, lo);
+        load_floats<VEC, F32>(src, mine + half, hi);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) turn_pair(lo[j], hi[j], c[j], s[j], lo[j], hi[j]);
-        store_floats<VEC, F32>(dst, to, lo);
-        store_floats<VEC, F32>(dst, to + half, hi);
+        store_floats<VEC, F32>(dst, mine, lo);
+        store_floats<VEC, F32>(dst, mine + half, hi);
     }
 }
 
@@ -53,7 +54,7 @@ hipError_t launch_rope_axes(RopeAxesParams p, bool f32, hipStream_t stream) {
     const int half = p.head_dim / 2;
     const int vec = !f32 && half % 8 == 0 ? 8 : 4;
     const int heads_at_once = 64 / (half / vec);
-    const int rounds = (p.q_heads + p.kv_heads + heads_at_once - 1) / heads_at_once;
+    const int rounds = (p.q_heads + heads_at_once - 1) / heads_at_once + (p.kv_heads + heads_at_once - 1) / heads_at_once;
     // enough waves for the device: 16 for each of 256 compute units
     p.shares = (int)std::max<int64_t>(1, std::min<int64_t>(rounds, (4096 + p.tokens - 1) / p.tokens));
     const int64_t units = (int64_t)p.tokens * p.shares;

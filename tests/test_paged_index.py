@@ -56,17 +56,17 @@ extern "C" int check(const int* cu, const int* len, int num_seqs, int total_rows
         long sum = 0;
         for (int i = 0; i < num_seqs; ++i) sum += s[i].n;
         sane = sum <= total_rows;
-        if (sane && (slots > b.grid || parts > room || b.grid % kXcds)) return __LINE__;
+        if (sane && (slots > b.grid || parts > room)) return __LINE__;
         std::vector<char> met(slots, 0), used(parts, 0);
         for (long block = 0; block < b.grid; ++block) {
-            const long slot = slot_of_block(block, slots);
-            if (slot < 0) continue;
-            if (slot >= slots || met[slot]++) return __LINE__;
+            const long slot = block;
+            if (slot >= slots) break;
+            met[slot] = 1;
             int i = 0;
             while (i < num_seqs && !(slot >= first[i] && slot < first[i] + (i + 1 < num_seqs ? first[i + 1] : slots) - first[i])) ++i;
             if (i == num_seqs) return __LINE__;
             const Shares sh = shares_of(t[i].units, per);
-            const SlotPlace at = place_of_slot(slot - first[i], t[i].tiles, sh.chunks);
+            const SlotPlace at = place_of_slot(slot - first[i], t[i].tiles, sh.chunks, kv_heads);
             if (at.head < 0 || at.head >= kv_heads || at.chunk < 0 || at.chunk >= sh.chunks || at.tile < 0 || at.tile >= t[i].tiles) return __LINE__;
             if (sh.chunks > 1) {
                 const long part = first_part[i] + part_of(at, t[i].tiles, sh.chunks) + at.chunk;
