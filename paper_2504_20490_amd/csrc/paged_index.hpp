@@ -61,9 +61,9 @@ HSPMD_INDEX int raised(int per_chunk, int first, int64_t slots, bool many) {
 struct Shares {
     int chunks, units;   // units of each
 };
-HSPMD_INDEX Shares shares_of(int units, int per_chunk) {
-    const int c = (int)(((int64_t)units + per_chunk - 1) / per_chunk);
-    return Shares{c < 1 ? 1 : c, c < 1 ? 0 : (units + c - 1) / c};
+HSPMD_INDEX Shares shares_of(int units, int per_chunk) {    // (32-bit: a 64-bit division takes a hundred instructions)
+    const unsigned c = ((unsigned)units + (unsigned)per_chunk - 1u) / (unsigned)per_chunk;
+    return Shares{c < 1 ? 1 : (int)c, c < 1 ? 0 : (int)(((unsigned)units + c - 1) / c)};
 }
 
 // slot within a sequence -> KV head, chunk, row tile.  The last row tiles, which see the most keys, come first (a workgroup that starts late has
@@ -72,9 +72,9 @@ HSPMD_INDEX Shares shares_of(int units, int per_chunk) {
 struct SlotPlace {
     int head, chunk, tile;
 };
-HSPMD_INDEX SlotPlace place_of_slot(int64_t local, int tiles, int chunks, int heads) {
-    const int64_t rest = local / heads;
-    return SlotPlace{(int)(local % heads), (int)(rest % chunks), tiles - 1 - (int)(rest / chunks)};
+HSPMD_INDEX SlotPlace place_of_slot(uint32_t local, int tiles, int chunks, int heads) {
+    const uint32_t rest = local / (uint32_t)heads;
+    return SlotPlace{(int)(local % (uint32_t)heads), (int)(rest % (uint32_t)chunks), tiles - 1 - (int)(rest / (uint32_t)chunks)};
 }
 // tile of partial results of an item's first chunk, counted from the sequence's first; its chunks follow each other
 HSPMD_INDEX int64_t part_of(const SlotPlace& p, int tiles, int chunks) { return ((int64_t)p.head * tiles + p.tile) * chunks; }

@@ -74,15 +74,15 @@ struct ConvertLoad {
     Raw* v_raw;
     char* k_dst;               // the tiles that the pieces go to ...
     char* v_dst;
-    int k_next, v_next;        // ... and first keys of those that are fetched
-    int last_chunk;
-    __device__ __forceinline__ void fetch(Raw& raw, bool v, int key0, int i) const {
-        const int lane = threadIdx.x & 63, r = lane / (D / 16), chunk = min(lane % (D / 16), last_chunk);
-        const int page = __builtin_amdgcn_readlane(src->page_numbers(key0), i);
+    int k_next, v_next;        // ... and first keys of those that are fetched,
+    int k_pages, v_pages;      // with (lane i) the page number of piece i
+    uint32_t lane_offset;      // of this lane's 16 bytes from the piece's first row
+    __device__ __forceinline__ void fetch(Raw& raw, bool v, int pages, int key0, int i) const {
+        const int page = __builtin_amdgcn_readlane(pages, i);
         const uint8_t* base = (v ? src->pool->v : src->pool->k) + src->offset(page, key0, i);
-        raw.bytes[i] = *reinterpret_cast<const u32x4*>(base + (uint32_t)(r * src->pool->row_bytes + chunk * 16));
+        raw.bytes[i] = *reinterpret_cast<const u32x4*>(base + lane_offset);
         const uint8_t* scales = (v ? src->pool->v_scale : src->pool->k_scale) + page * src->pool->scale_page_bytes + src->row_of(key0, i);
-        raw.scale[i] = scales[(uint32_t)r];
+        raw.scale[i] = scales[(uint32_t)(threadIdx.x & 63) / (D / 16)];
     }
     __device__ __forceinline__ void convert(const Raw& raw, char* tile, int i) const {
         const int lane = threadIdx.x & 63, row = src->first_row(i) + lane / (D / 16), col = lane % (D / 16) * 16;
@@ -96,11 +96,11 @@ struct ConvertLoad {
     }
     __device__ __forceinline__ void k_piece(int i) const {
         convert(*k_raw, k_dst, i);
-        fetch(*k_raw, false, k_next, i);
+        fetch(*k_raw, false, k_pages, k_next, i);
     }
     __device__ __forceinline__ void v_piece(int i) const {
         convert(*v_raw, v_dst, i);
-        fetch(*v_raw, true, v_next, i);
+        fetch(*v_raw, true, v_pages, v_next, i);
     }
 };
 
@@ -177,7 +177,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
     if constexpr (E4M3) {
         load.k_raw = &k_raw;
         load.v_raw = &v_raw;
-        load.last_chunk = last_chunk;
+        load.lane_offset = (uint32_t)(lane / (D / 16) * p.pool.row_bytes + min(lane % (D / 16), last_chunk) * 16);
     } else {
         const int r = lane / (D / 8);
         load.lane_offset = (uint32_t)(r * p.pool.row_bytes + min(swizzle<D>(src.first_row(0) + r, lane % (D / 8)), last_chunk) * 16);
@@ -219,8 +219,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
         };
         auto fetch = [&](bool v, int kt) {
             if constexpr (E4M3) {
+                const int numbers = src.page_numbers(key0(kt));
 #pragma unroll
-                for (int i = 0; i < Source::kPieces; ++i) load.fetch(v ? v_raw : k_raw, v, key0(kt), i);
+                for (int i = 0; i < Source::kPieces; ++i) load.fetch(v ? v_raw : k_raw, v, numbers, key0(kt), i);
             }
         };
         auto convert = [&](bool v, int kt) {
@@ -320,6 +321,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
                 load.v_dst = vbuf0 + (1 - par) * kTileBytes;
                 load.k_next = key0(kt + 3);
                 load.v_next = key0(kt + 2);
+                load.k_pages = src.page_numbers(load.k_next);
+                load.v_pages = src.page_numbers(load.v_next);
             } else {
                 load.k_dst = kdst0 + par * kTileBytes;
                 load.v_dst = vdst0 + (1 - par) * kTileBytes;
