@@ -592,8 +592,8 @@ class RopeAxes:
         self._ref = ctypes.byref(self._args)
 
     def _check(self, head_dim: int, tokens: int) -> None:
-        if self.pairs < head_dim // 2:
-            raise _bad("rope table tensor is too small")
+        if self.pairs < head_dim // 2 or self.table.dim() == 3 and self.table.shape[1] != head_dim // 2:
+            raise _bad("the rope table is too small, or made for another head_dim")
         if self.has_pairs is not None and self.has_pairs != head_dim // 2:
             raise _bad("pair_axis has to have head_dim / 2 entries")
         if self.tokens is not None and self.tokens < tokens:

@@ -1108,6 +1108,12 @@ hspmd_status hspmd_attn_block_bwd_rope(const hspmd_attn_plan* plan, const void* 
 // Rows of a call: a launch has one wave per row (and head) at most, and a grid holds fewer than 2^32 threads
 static constexpr int64_t kMaxRows = (int64_t)1 << 25, kMaxRowHeads = (int64_t)1 << 25;
 
+// a tensor that is turned in place keeps its stride: with another one a row would land on rows that others still read
+static hspmd_status check_in_place(const void* from, const void* to, int64_t stride, int64_t out_stride) {
+    if (from == to && stride != out_stride) return fail(HSPMD_ERR_INVALID_ARG, "in place the token strides have to be the same");
+    return HSPMD_OK;
+}
+
 static hspmd_status check_stride(int64_t stride, int64_t heads, int32_t head_dim, const char* what) {
     if (stride < heads * head_dim || stride % 8 != 0)
         return fail(HSPMD_ERR_INVALID_ARG, std::string(what) + " must be a multiple of 8 and >= heads*head_dim");
@@ -1158,7 +1164,9 @@ hspmd_status hspmd_rope_axes_qk(const hspmd_rope_axes* rope, const void* q, cons
     if (keys) {
         if (hspmd_status rc = check_stride(kv_token_stride, local_kv_heads, head_dim, "kv_token_stride")) return rc;
         if (hspmd_status rc = check_stride(kv_out_token_stride, local_kv_heads, head_dim, "kv_out_token_stride")) return rc;
+        if (hspmd_status rc = check_in_place(k, k_out, kv_token_stride, kv_out_token_stride)) return rc;
     }
+    if (hspmd_status rc = check_in_place(q, q_out, q_token_stride, q_out_token_stride)) return rc;
     p.q = q;
     p.k = k;
     p.q_out = q_out;
@@ -1210,6 +1218,7 @@ static hspmd_status check_cache(const hspmd_kv_cache* cache, const hspmd_kv_batc
     if (e4m3 && (cache->scale_page_stride < tokens || cache->scale_page_stride % 4 != 0))
         return fail(HSPMD_ERR_INVALID_ARG, "scale_page_stride must be a multiple of 4 and hold the heads' page_size scales");
     if (batch->num_seqs < 0 || batch->table_width < 0 || batch->max_rows < 0) return fail(HSPMD_ERR_INVALID_ARG, "negative count in the batch");
+    if (batch->num_seqs > kMaxRows) return fail(HSPMD_ERR_INVALID_ARG, "num_seqs must be 0 .. 2^25");
     if (batch->total_rows < 0 || batch->total_rows > kMaxRows) return fail(HSPMD_ERR_INVALID_ARG, "total_rows must be 0 .. 2^25");
     *idle = batch->num_seqs == 0 || batch->total_rows == 0;
     if (pointers && !*idle) {
@@ -1252,6 +1261,7 @@ hspmd_status hspmd_kv_cache_write(const hspmd_kv_cache* cache, const hspmd_kv_ba
     if (q) {
         if (hspmd_status rc = check_stride(q_token_stride, local_q_heads, hd, "q_token_stride")) return rc;
         if (hspmd_status rc = check_stride(q_out_token_stride, local_q_heads, hd, "q_out_token_stride")) return rc;
+        if (hspmd_status rc = check_in_place(q, q_out, q_token_stride, q_out_token_stride)) return rc;
     }
     if (rope) {
         if (hspmd_status rc = check_axes(rope, hd, batch->total_rows, true, &p.rope)) return rc;

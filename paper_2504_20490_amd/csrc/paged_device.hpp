@@ -15,19 +15,19 @@ struct RowPlace {
     int slot;       // slot in the page
 };
 
-// by a whole wave, the same row in every lane: the sequence s with cu_rows[s] <= row < cu_rows[s + 1]
+// by a whole wave, the same row in every lane: the sequence s with cu_rows[s] <= row < cu_rows[s + 1], 64 ends at a time
 __device__ __forceinline__ int sequence_of(const PagedRows& b, int row) {
     const int lane = threadIdx.x & 63;
-    for (int s0 = 0; s0 < b.num_seqs; s0 += 64) {
-        const int s = s0 + lane;
-        const bool ends_behind = s < b.num_seqs && b.cu_rows[s + 1] > row;
-        const uint64_t m = __ballot(ends_behind);
-        if (m != 0) {
-            const int found = s0 + __builtin_ctzll(m);
-            return b.cu_rows[found] <= row ? found : -1;
-        }
+    int lo = 0, hi = b.num_seqs;                           // it is one of lo .. hi - 1, or none
+    for (;;) {
+        const int step = (hi - lo + 63) / 64, end = min(lo + (lane + 1) * step, hi);
+        const uint64_t m = __ballot(b.cu_rows[end] > row);
+        if (m == 0) return -1;
+        const int found = __builtin_ctzll(m);
+        hi = min(lo + (found + 1) * step, hi);
+        lo += found * step;
+        if (step == 1) return b.cu_rows[lo] <= row ? lo : -1;
     }
-    return -1;
 }
 
 __device__ __forceinline__ int page_at(const PagedPool& pool, const PagedRows& b, int seq, int index) {

@@ -89,6 +89,107 @@ def test_many_rows(rows, kv, hq, hkv, d, page_size, e4m3):
     run_attention(rows, kv, hq, hkv, d, page_size, e4m3, seed=2, extra_rows=2)
 
 
+@pytest.mark.parametrize("max_rows", [0, 1, 5])
+@pytest.mark.parametrize("rows,kv", [([70, 1, 9], [400, 300, 9]), ([90], [500])])
+def test_a_wrong_hint_changes_no_result(rows, kv, max_rows):
+    import torch
+    import paper_2504_20490_amd as A
+    b = Batch(rows, kv, 2, 128, 16, seed=14)
+    b.device(A)
+    b.batch = A.KVBatch(b.cu_dev, b.kv_dev, b.table_dev, max_rows)
+    q64, q = rows_of_q(b, 6)
+    o, lse = attend(A, b, q)
+    torch.cuda.synchronize()
+    check_attention(b, 6, o, lse, q64, 1.0 / math.sqrt(128))
+
+
+def test_rows_in_front_of_the_first_sequence_are_left_alone():
+    import torch
+    import paper_2504_20490_amd as A
+    b = Batch([2, 40], [3000, 300], 2, 64, 16, seed=15, extra_rows=5)
+    b.device(A)
+    _, q = rows_of_q(b, 4)
+    want, want_lse = attend(A, b, q)
+    shifted = torch.cat([q[-3:], q[:-3]])
+    b.cu_dev += 3
+    got, got_lse = attend(A, b, shifted)
+    torch.cuda.synchronize()
+    assert torch.equal(got[3:45], want[:42]) and torch.equal(got_lse[:, 3:45], want_lse[:, :42])
+    assert torch.isnan(got[:3].float()).all() and torch.isnan(got[45:].float()).all() and torch.isnan(got_lse[:, :3]).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("seqs,rows,kv", [(40, 1, 20000), (9, 17, 40000)])
+def test_more_pages_than_are_kept_at_a_time(seqs, rows, kv, e4m3):
+    """So many heads that no keys are shared out, and a workgroup walks more pages than it keeps the numbers of (512 and 2048).  64 pages
+    take turns in all of them."""
+    import torch
+    import paper_2504_20490_amd as A
+    heads, d, size, distinct = 64, 8, 16, 64
+    b = Batch([distinct * size], [distinct * size], heads, d, size, e4m3, seed=16, extra_pages=0, extra_width=0)
+    cache, _ = b.device(A)
+    table = np.resize(b.table[0], (seqs, -(-kv // size)))
+    i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x)).int().cuda()
+    b.cache, T = cache, seqs * rows
+    b.batch = A.KVBatch(i32(np.arange(seqs + 1) * rows), i32(np.full(seqs, kv)), i32(table), rows)
+    q64 = bf16(b.rng.standard_normal((T, heads, d)))
+    o, lse = attend(A, b, torch.from_numpy(q64).to(torch.bfloat16).cuda())
+    torch.cuda.synchronize()
+    k, v = (paged.gather(pool, b.table[0], distinct * size, size) for pool in (b.k, b.v))
+    where = np.argsort(b.table[0])[table]                                          # [seqs, pages]: which of the 64
+    key = (where[:, :, None] * size + np.arange(size)).reshape(seqs, -1)[:, :kv]   # [seqs, kv]
+    seq, pos = np.repeat(np.arange(seqs), rows), kv - rows + np.tile(np.arange(rows), seqs)
+    for h in range(0, heads, 7):
+        s = np.take_along_axis(q64[:, h] @ k[:, h].T / math.sqrt(d), key[seq], 1)  # [T, kv]
+        s[np.arange(kv)[None] > pos[:, None]] = -np.inf
+        top = s.max(-1, keepdims=True)
+        w = np.exp(s - top)
+        total = w.sum(-1, keepdims=True)
+        per_key = np.stack([np.bincount(key[seq[t]], w[t] / total[t], distinct * size) for t in range(T)])
+        ref, mass = per_key @ v[:, h], per_key @ np.abs(v[:, h])
+        got = o[:, h].double().cpu().numpy()
+        assert (np.abs(got - ref) <= BF16_HALF_STEP * np.abs(ref) + (BF16_HALF_STEP + 1e-4) * mass).all()
+        assert (np.abs(lse[h].double().cpu().numpy() - (top + np.log(total))[:, 0]) <= LSE_ABS).all()
+
+
+def test_thousands_of_sequences():
+    """The rows' sequences are found among many; writes, reads and attends to 5000 of 0 to 3 rows."""
+    import torch
+    import paper_2504_20490_amd as A
+    rng = np.random.default_rng(17)
+    seqs, hkv, d, size = 5000, 1, 16, 16
+    rows = rng.integers(0, 4, seqs)
+    kv = rows + rng.integers(0, 20, seqs)
+    cu = np.concatenate([[0], np.cumsum(rows)])
+    T = int(cu[-1])
+    table = np.stack([2 * np.arange(seqs), 2 * np.arange(seqs) + 1], 1)
+    i32 = lambda x: torch.from_numpy(np.ascontiguousarray(x)).int().cuda()
+    pool = torch.from_numpy(rng.standard_normal((2, 2 * seqs, hkv, size, d))).to(torch.bfloat16).cuda()
+    cache = A.KVCache(pool[0], pool[1])
+    batch = A.KVBatch(i32(cu), i32(kv), i32(table), 3)
+    x = torch.from_numpy(rng.standard_normal((T, 2, hkv, d))).to(torch.bfloat16).cuda()
+    k, v = x[:, 0], x[:, 1]
+    A.kv_cache_write(cache, batch, k, v)
+    back = torch.empty(2, T, hkv, d, dtype=torch.bfloat16, device="cuda")
+    A.kv_cache_read(cache, batch, back[0], back[1])
+    q = torch.from_numpy(rng.standard_normal((T, 2, d))).to(torch.bfloat16).cuda()
+    o, lse = torch.empty_like(q), torch.empty(2, T, device="cuda")
+    ws = torch.empty(A.attn_paged_workspace_bytes(cache, batch, T, 2), dtype=torch.uint8, device="cuda")
+    A.attn_paged_fwd(cache, batch, q, o, lse, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(back[0], k) and torch.equal(back[1], v)
+    keys, values = (p.double().cpu().numpy().reshape(seqs, 2 * size, d) for p in pool)       # (one head: a sequence's pages are neighbours)
+    seq = np.repeat(np.arange(seqs), rows)
+    pos = kv[seq] - rows[seq] + np.arange(T) - cu[seq]
+    for h in range(2):
+        s = np.einsum("td,tkd->tk", q[:, h].double().cpu().numpy(), keys[seq]) / 4.0
+        s[np.arange(2 * size)[None] > pos[:, None]] = -np.inf
+        w = np.exp(s - s.max(-1, keepdims=True))
+        w /= w.sum(-1, keepdims=True)
+        ref, mass = np.einsum("tk,tkd->td", w, values[seq]), np.einsum("tk,tkd->td", w, np.abs(values[seq]))
+        assert (np.abs(o[:, h].double().cpu().numpy() - ref) <= BF16_HALF_STEP * np.abs(ref) + (BF16_HALF_STEP + 1e-4) * mass).all()
+
+
 @pytest.mark.parametrize("scale", [0.01, 3.0])
 def test_other_scales_and_no_lse(scale):
     run_attention([1, 40], [100, 300], 4, 2, 128, 16, False, seed=4, lse=False, scale=scale)

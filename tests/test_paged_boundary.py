@@ -33,8 +33,9 @@ def batch(**change):
     return a
 
 
-def axes(r=None, q=P, k=P, qs=256, ks=128, qo=P, ko=P, T=12, hq=4, hkv=2, d=64, dtype=0):
-    return A.load_library().hspmd_rope_axes_qk(None if r is None else ctypes.byref(r), q, k, qs, ks, qo, ko, qs, ks, T, hq, hkv, d, dtype, 0, None)
+def axes(r=None, q=P, k=P, qs=256, ks=128, qo=P, ko=P, T=12, hq=4, hkv=2, d=64, dtype=0, qos=None, kos=None):
+    return A.load_library().hspmd_rope_axes_qk(None if r is None else ctypes.byref(r), q, k, qs, ks, qo, ko, qos or qs, kos or ks, T, hq, hkv, d,
+                                               dtype, 0, None)
 
 
 def write(c, b, k=P, v=P, ks=128, r=None, q=None, qo=None, qs=256, hq=4):
@@ -55,7 +56,7 @@ def attend(c, b, q=P, qs=256, hq=4, scale=0.0, o=P, lse=P, ws=P, n=1 << 40):
     (dict(r=rope(num_axes=0)), 1), (dict(r=rope(num_axes=5)), 1), (dict(r=rope(positions=None)), 1), (dict(r=rope(positions=P + 2)), 1),
     (dict(r=rope(positions_stride=11)), 1), (dict(r=rope(num_axes=2)), 1), (dict(q=None), 1), (dict(qo=None), 1), (dict(k=None), 1), (dict(ko=None), 1),
     (dict(q=P + 8), 1), (dict(k=P + 2), 1), (dict(qs=248), 1), (dict(qs=260), 1), (dict(ks=120), 1), (dict(T=-1), 1), (dict(T=(1 << 25) + 1), 1),
-    (dict(hq=0), 1), (dict(hkv=-1), 1), (dict(d=60), 2), (dict(d=136), 2), (dict(d=0), 2), (dict(dtype=2), 2)])
+    (dict(qos=264), 1), (dict(kos=136), 1), (dict(hq=0), 1), (dict(hkv=-1), 1), (dict(d=60), 2), (dict(d=136), 2), (dict(d=0), 2), (dict(dtype=2), 2)])
 def test_rope_axes_refusals(change, status):
     args = dict(r=rope())
     args.update(change)
@@ -76,7 +77,7 @@ CACHES = [(dict(k=None), 1), (dict(v=None), 1), (dict(k=P + 8), 1), (dict(page_s
           (dict(local_kv_heads=0), 1), (dict(head_dim=63), 2), (dict(head_dim=0), 2), (dict(head_dim=136), 2), (dict(dtype=2), 2), (dict(dtype=-1), 2)]
 SCALES = [(dict(k_scale=None), 1), (dict(v_scale=None), 1), (dict(v_scale=P + 1), 1), (dict(scale_page_stride=28), 1), (dict(scale_page_stride=34), 1),
           (dict(page_stride=2 * 16 * 64 + 8), 1)]
-BATCHES = [(dict(cu_rows=None), 1), (dict(kv_lens=None), 1), (dict(page_table=None), 1), (dict(cu_rows=P + 1), 1), (dict(num_seqs=-1), 1),
+BATCHES = [(dict(cu_rows=None), 1), (dict(kv_lens=None), 1), (dict(page_table=None), 1), (dict(cu_rows=P + 1), 1), (dict(num_seqs=-1), 1), (dict(num_seqs=(1 << 25) + 1), 1),
            (dict(table_width=-1), 1), (dict(total_rows=-1), 1), (dict(total_rows=(1 << 25) + 1), 1), (dict(max_rows=-1), 1)]
 
 
@@ -199,3 +200,5 @@ def test_tensors_of_the_wrong_shape_type_or_place():
     refused(A.RopeAxes._check, A.RopeAxes(table, 10, i(5), [0] * 31), 64, 5)
     refused(A.RopeAxes._check, A.RopeAxes(table, 10, i(4)), 64, 5)
     refused(A.RopeAxes._check, A.RopeAxes(table, 11), 64, 5)
+    refused(A.RopeAxes._check, A.RopeAxes(table, 10), 40, 5)              # a table of another head_dim
+    A.RopeAxes(table, 10, i(5), [0] * 32)._check(64, 5)
