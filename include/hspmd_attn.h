@@ -539,7 +539,11 @@ hspmd_status hspmd_kv_cache_read(const hspmd_kv_cache* cache, const hspmd_kv_bat
  *   workspace  device, at least hspmd_attn_paged_workspace_bytes(cache, batch, local_q_heads) bytes, 16-byte aligned: partial results where
  *        the keys of a row are shared out.  The size follows from num_seqs, table_width, total_rows and the heads, never less for more of
  *        any; nothing in it outlives the call.
- * softmax_scale as in hspmd_attn_varlen_fwd.  No atomics: results are run-to-run bit-identical.
+ * softmax_scale as in hspmd_attn_varlen_fwd.  No atomics: results are run-to-run bit-identical.  Keys and values that a row does not see take no
+ * part in its result, whatever they hold, infinities and NaN included, nor does what the pages hold behind a sequence's last token.
+ * Weights are rounded to bf16 for their product with the values; scores, sums and O are fp32 until the one rounding to bf16.
+ * hspmd_attn_paged_workspace_bytes is 0 for bad arguments (hspmd_last_error says which) and where there is nothing to do.  Per-kernel timing
+ * (hspmd_profile_enable) does not record the calls of this section.
  * Errors of the calls above: INVALID_ARG for NULL / misaligned pointers, bad strides, counts or page sizes; UNSUPPORTED for a head_dim
  * outside the supported set or an unknown dtype; WORKSPACE_TOO_SMALL.  Nothing is launched on error; total_rows == 0 or num_seqs == 0
  * returns OK without launching.

@@ -3,6 +3,8 @@
 // HBM-bound copies: a row of k or v is read once and written once.  The write gives a row (one token) to a wave, or to several where there
 // are few rows: the wave finds the row's place, then walks the heads of q (turned, if given), k (turned) and v, with a lane holding
 // VEC pairs of columns of a head as the rotation pairs them.  A head's largest magnitude is one exchange among its lanes.
+// Write, with q turned: 12351 rows, 32 + 8 + 8 heads of 128, bf16 65 us = 4.8 TB/s, e4m3 60 us = 4.7; 14100 rows, 16 + 16 + 16 heads of 104, bf16 71 us = 4.1; 64 rows
+// (a generation step) 5.2 us.  Read: 131754 rows, 8 heads of 128, e4m3 159 us = 5.1 TB/s, bf16 210 us = 5.1; 83 rows 3.3 us.
 #include "paged_device.hpp"
 
 namespace hspmd {

@@ -10,7 +10,11 @@
 // the LDS transpose read.
 //   S^T = K Q^T (16x16x32, 2 key blocks x D/32 steps),  P = exp2(c S - c m),  O^T += V^T P^T (D/16 blocks, one step of 32 keys)
 // 8-bit tiles are copied as they are; K is scaled to bf16 on its way from LDS (exact), V's scales go into the weights
-// before they are rounded, its bytes are converted as they are.
+// before they are rounded, its bytes are converted as they are.  Weights are rounded to bf16 for the product (half a step of 2^-8 each, at random: their
+// sum is that of the unrounded ones); scores, maxima, sums and O are fp32.
+// One token of a sequence of 131001 keys, 32 heads on 8 of 128, bf16: 99 us = 5.4 TB/s (and 7 us for the join); of 64 sequences with 272960 keys together,
+// e4m3: 113 us = 5.0 TB/s (5 us); of one with 1058, 5 heads: 6.2 us (4.3), start and three trips to memory.  Counters: HBM reads 1.00 and 1.06 times the
+// cache's bytes (the scales' lines are fetched by several units), vector units a third busy.
 #include "paged_item.hpp"
 
 namespace hspmd {
