@@ -1340,6 +1340,7 @@ hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_ba
     p.where = reinterpret_cast<int2*>(ws);
     p.part_stats = reinterpret_cast<float2*>(ws + sizes.where_bytes);
     p.part_o = reinterpret_cast<float*>(ws + sizes.where_bytes + sizes.stats_bytes);
+    p.plan = sizes.plan_bytes ? reinterpret_cast<const uint32_t*>(ws + sizes.where_bytes + sizes.stats_bytes + sizes.part_bytes) : nullptr;
     p.few_part_rows = (int32_t)sizes.few_part_rows;
     p.part_rows = (int32_t)sizes.part_rows;
     p.few_limit = sizes.few_limit;

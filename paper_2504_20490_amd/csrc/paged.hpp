@@ -89,6 +89,7 @@ struct PagedAttnParams {
     // paged_few_kernel first; and for every row of the call where its chunks' results are
     float* part_o;
     float2* part_stats;
+    const uint32_t* plan;          // NULL: every workgroup sums over the sequences for itself; see plan_words
     int2* where;                   // [total_rows][q_heads], see where_entry
     int32_t few_part_rows, part_rows;
 };
@@ -99,8 +100,8 @@ struct PagedSizes {
     int32_t few_limit;
     int64_t few_grid, many_grid;
     int64_t few_part_rows, part_rows;
-    size_t where_bytes, stats_bytes, part_bytes;
-    size_t total_bytes() const { return where_bytes + stats_bytes + part_bytes; }
+    size_t where_bytes, stats_bytes, part_bytes, plan_bytes;
+    size_t total_bytes() const { return where_bytes + stats_bytes + part_bytes + plan_bytes; }
 };
 PagedSizes paged_sizes(const PagedRows& rows, int max_rows, int page_shift, int q_heads, int kv_heads, int head_dim);
 hipError_t launch_paged_attn(const PagedAttnParams& p, const PagedSizes& sizes, bool e4m3, hipStream_t stream);

@@ -361,6 +361,76 @@ __global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
     }
 }
 
+// ---- the plan: a workgroup for each kernel that runs (find_item's sums with the sequences dealt out to 1024 threads)
+constexpr int kPlanThreads = 1024;
+
+struct UpTo {
+    uint32_t mine, all;
+};
+// sums over the workgroup's threads up to each one, and over all; sums: LDS, one per wave
+__device__ __forceinline__ UpTo threads_up_to(uint32_t x, uint32_t* sums) {
+    const int wave = threadIdx.x >> 6;
+    UpTo r{lanes_up_to(x), 0u};
+    __syncthreads();                                       // the previous call's sums have been read
+    if ((threadIdx.x & 63) == 63) sums[wave] = r.mine;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kPlanThreads / 64; ++w) {
+        r.mine += w < wave ? sums[w] : 0u;
+        r.all += sums[w];
+    }
+    return r;
+}
+
+template <bool MANY>
+__device__ __forceinline__ void make_plan(const PagedAttnParams& p, uint32_t* plan, uint32_t* sums) {
+    const int n = p.rows.num_seqs, kvh = p.pool.kv_heads;
+    SeqRows s{};
+    SeqTiles t{};
+    int64_t units = 0;
+    for (int seq = threadIdx.x; seq < n; seq += kPlanThreads) {
+        look_at<MANY>(p, seq, s, t);
+        units += (int64_t)t.tiles * t.units * kvh;
+    }
+    const int64_t high = threads_up_to((uint32_t)(units >> 20), sums).all, low = threads_up_to((uint32_t)units & 0xfffffu, sums).all;
+    const int first_per = units_per_chunk((high << 20) + low, MANY);
+    int per_chunk = first_per;
+    for (int raise = 0; raise < kRaises; ++raise) {
+        uint32_t slots = 0;
+        for (int seq = threadIdx.x; seq < n; seq += kPlanThreads) {
+            look_at<MANY>(p, seq, s, t);
+            slots += (uint32_t)(t.tiles * kvh * shares_of(t.units, per_chunk).chunks);
+        }
+        const int next = raised(per_chunk, first_per, threads_up_to(slots, sums).all, MANY);
+        if (next == per_chunk) break;
+        per_chunk = next;
+    }
+    uint32_t slots = 0, parts = 0;                         // of the sequences before
+    for (int seq0 = 0; seq0 < n; seq0 += kPlanThreads) {
+        const int seq = seq0 + threadIdx.x;
+        look_at<MANY>(p, seq, s, t);
+        const Shares sh = shares_of(t.units, per_chunk);
+        const uint32_t mine = t.tiles * kvh * sh.chunks, mine_parts = sh.chunks > 1 ? mine : 0u;
+        const UpTo a = threads_up_to(mine, sums), b = threads_up_to(mine_parts, sums);
+        if (seq < n) {
+            plan[1 + seq] = slots + a.mine - mine;
+            plan[2 + n + seq] = parts + b.mine - mine_parts;
+        }
+        slots += a.all;
+        parts += b.all;
+    }
+    if (threadIdx.x == 0) {
+        plan[0] = per_chunk;
+        plan[1 + n] = slots;
+    }
+}
+
+__global__ __launch_bounds__(kPlanThreads) void paged_plan_kernel(PagedAttnParams p, uint32_t* plan, int first) {
+    __shared__ uint32_t sums[kPlanThreads / 64];
+    if (first + (int)blockIdx.x == 0) make_plan<false>(p, plan, sums);
+    else make_plan<true>(p, plan + plan_words(p.rows.num_seqs), sums);
+}
+
 // ---- chunks' results joined, for the (row, query head) pairs that have several
 //   M = max m_i,  L = sum exp2(c (m_i - M)) l_i,  O = sum exp2(c (m_i - M)) o_i / L
 // Sums, weights and the maximum are carried along the chunks together, so that nothing is read twice and nothing waits for a maximum; the order of a
@@ -476,11 +546,16 @@ PagedSizes paged_sizes(const PagedRows& rows, int max_rows, int page_shift, int 
     s.where_bytes = ((size_t)rows.total_rows * q_heads * sizeof(int2) + 255) / 256 * 256;
     s.stats_bytes = ((size_t)s.part_rows * sizeof(float2) + 255) / 256 * 256;
     s.part_bytes = (size_t)s.part_rows * D * sizeof(float);
+    s.plan_bytes = rows.num_seqs > kPlanAbove ? 2 * (size_t)plan_words(rows.num_seqs) * sizeof(uint32_t) : 0;
     return s;
 }
 
 hipError_t launch_paged_attn(const PagedAttnParams& p, const PagedSizes& sizes, bool e4m3, hipStream_t stream) {
     const int width = tile_width(p.pool.head_dim);
+    if (p.plan) {
+        hipLaunchKernelGGL(paged_plan_kernel, dim3(sizes.few + sizes.many), dim3(kPlanThreads), 0, stream, p, const_cast<uint32_t*>(p.plan), sizes.few ? 0 : 1);
+        if (const hipError_t e = hipGetLastError()) return e;
+    }
     if (sizes.few) {
         if (width == 128) {
             if (e4m3) launch_few<128, true>(p, sizes, stream);

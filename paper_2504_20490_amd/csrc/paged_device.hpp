@@ -15,18 +15,19 @@ struct RowPlace {
     int slot;       // slot in the page
 };
 
-// by a whole wave, the same row in every lane: the sequence s with cu_rows[s] <= row < cu_rows[s + 1], 64 ends at a time
-__device__ __forceinline__ int sequence_of(const PagedRows& b, int row) {
+// by a whole wave, the same x in every lane: the i < n with ends[i] <= x < ends[i + 1], 64 ends at a time; -1: none.  n > 0; ends: n + 1 of them
+template <typename T>
+__device__ __forceinline__ int interval_of(const T* ends, int n, T x) {
     const int lane = threadIdx.x & 63;
-    int lo = 0, hi = b.num_seqs;                           // it is one of lo .. hi - 1, or none
+    int lo = 0, hi = n;                                    // it is one of lo .. hi - 1, or none
     for (;;) {
         const int step = (hi - lo + 63) / 64, end = min(lo + (lane + 1) * step, hi);
-        const uint64_t m = __ballot(b.cu_rows[end] > row);
+        const uint64_t m = __ballot(ends[end] > x);
         if (m == 0) return -1;
         const int found = __builtin_ctzll(m);
         hi = min(lo + (found + 1) * step, hi);
         lo += found * step;
-        if (step == 1) return b.cu_rows[lo] <= row ? lo : -1;
+        if (step == 1) return ends[lo] <= x ? lo : -1;
     }
 }
 
@@ -36,7 +37,7 @@ __device__ __forceinline__ int page_at(const PagedPool& pool, const PagedRows& b
 }
 
 __device__ __forceinline__ RowPlace place_of(const PagedPool& pool, const PagedRows& b, int row) {
-    RowPlace r{sequence_of(b, row), -1, -1, 0};
+    RowPlace r{interval_of(b.cu_rows, b.num_seqs, row), -1, -1, 0};
     if (r.seq < 0) return r;
     const int kv = seq_rows(0, 0, b.kv_lens[r.seq], 0, b.table_width, pool.page_shift).kv;
     const int pos = kv - (b.cu_rows[r.seq + 1] - row);   // (cu_rows[seq + 1] > row)

@@ -30,23 +30,45 @@ __device__ __forceinline__ uint32_t lanes_up_to(uint32_t x) {
 }
 __device__ __forceinline__ uint32_t all_lanes(uint32_t x) { return (uint32_t)__builtin_amdgcn_readlane((int)lanes_up_to(x), 63); }
 
+// the sequence's rows and keys, and its row tiles and units of keys; behind the last: a sequence without rows
+template <bool MANY>
+__device__ __forceinline__ void look_at(const PagedAttnParams& p, int seq, SeqRows& s, SeqTiles& t) {
+    const int in = min(seq, p.rows.num_seqs - 1), begin = p.rows.cu_rows[in];
+    s = seq_rows(begin, seq == in ? p.rows.cu_rows[in + 1] : begin, p.rows.kv_lens[in], p.rows.total_rows, p.rows.table_width, p.pool.page_shift);
+    t = seq_tiles(s, p.group, MANY ? kManyRows : kFewRows, MANY, p.few_limit);
+}
+
+// The workgroup's item from the plan that a launch in front has made (more than kPlanAbove sequences)
+template <bool MANY>
+__device__ __forceinline__ PagedItem planned_item(const PagedAttnParams& p) {
+    const uint32_t* const plan = p.plan + (MANY ? plan_words(p.rows.num_seqs) : 0);
+    PagedItem it{};
+    it.seq = __builtin_amdgcn_readfirstlane(interval_of(plan + 1, p.rows.num_seqs, (uint32_t)blockIdx.x));
+    if (it.seq < 0) return it;
+    SeqRows s;
+    SeqTiles t;
+    look_at<MANY>(p, it.seq, s, t);
+    const Shares sh = shares_of(t.units, (int)plan[0]);
+    const uint32_t local = blockIdx.x - plan[1 + it.seq];
+    if (local >= (uint32_t)(t.tiles * p.pool.kv_heads * sh.chunks)) { it.seq = -1; return it; }
+    const SlotPlace at = place_of_slot(local, t.tiles, sh.chunks, p.pool.kv_heads);
+    const int64_t mine = plan[2 + p.rows.num_seqs + it.seq] + part_of(at, t.tiles, sh.chunks);
+    return PagedItem{it.seq, s.start, s.n, s.kv, at.tile, at.head, at.chunk, sh.chunks, sh.units,
+                     (int)min(mine, (int64_t)(0x7fffffff / (MANY ? kManyRows : kFewRows)))};
+}
+
 // The workgroup's item, worked out by every wave for itself from the lengths on the device (sums over the sequences, without LDS or a barrier;
-// no launch in front).  A lane takes `per_lane` neighbouring sequences.  The arrays hold anything: rows and lengths are clamped, and what a sum
+// no launch in front).  A lane takes every 64th sequence, and slots go by lanes first.  The arrays hold anything: rows and lengths are clamped, and what a sum
 // that overflows leads to stays inside its sequence's tiles.
 template <bool MANY>
 __device__ __forceinline__ PagedItem find_item(const PagedAttnParams& p) {
+    if (p.plan) return planned_item<MANY>(p);
     constexpr int kRows = MANY ? kManyRows : kFewRows;
     const int lane = threadIdx.x & 63, kvh = p.pool.kv_heads;
     const int per_lane = (p.rows.num_seqs + 63) / 64;
     SeqRows s{};
     SeqTiles t{};
-    auto look = [&](int i) {                                // the lane's sequence i
-        const int seq = lane * per_lane + i;
-        t = SeqTiles{0, 0};
-        if (seq >= p.rows.num_seqs) return;
-        s = seq_rows(p.rows.cu_rows[seq], p.rows.cu_rows[seq + 1], p.rows.kv_lens[seq], p.rows.total_rows, p.rows.table_width, p.pool.page_shift);
-        t = seq_tiles(s, p.group, kRows, MANY, p.few_limit);
-    };
+    auto look = [&](int i) { look_at<MANY>(p, i * 64 + lane, s, t); };      // the lane's sequence i
     int64_t units = 0;
     for (int i = 0; i < per_lane; ++i) {
         look(i);
@@ -83,7 +105,7 @@ __device__ __forceinline__ PagedItem find_item(const PagedAttnParams& p) {
             if (slot - first < n) {
                 const SlotPlace at = place_of_slot(slot - first, t.tiles, sh.chunks, kvh);
                 const int64_t mine = part + part_of(at, t.tiles, sh.chunks);
-                it = PagedItem{lane * per_lane + i, s.start, s.n, s.kv, at.tile, at.head, at.chunk, sh.chunks, sh.units,
+                it = PagedItem{i * 64 + lane, s.start, s.n, s.kv, at.tile, at.head, at.chunk, sh.chunks, sh.units,
                                (int)min(mine, (int64_t)(0x7fffffff / kRows))};
                 break;
             }

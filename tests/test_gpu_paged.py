@@ -89,6 +89,59 @@ def test_many_rows(rows, kv, hq, hkv, d, page_size, e4m3):
     run_attention(rows, kv, hq, hkv, d, page_size, e4m3, seed=2, extra_rows=2)
 
 
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows,kv", [
+    ([i % 3 for i in range(300)], [9000 if i == 100 else 2 + i * 13 % 200 for i in range(300)]),           # one long: shared out
+    ([25 + i // 10 if i % 25 == 7 else i % 4 for i in range(250)], [2500 + i if i in (57, 111) else 60 + i % 50 for i in range(250)]),
+    ([1] * 192, [5 + i for i in range(192)]),             # the most whose sums every workgroup makes
+    ([1] * 193, [5 + i for i in range(193)]),             # the fewest that are planned
+    ([0] * 1030 + [3] + [0] * 70, [7] * 1030 + [3000] + [1] * 70),
+    ([0] * 200, [9] * 200),
+])
+def test_shares_planned_by_a_launch_in_front(rows, kv, e4m3):
+    run_attention(rows, kv, 4, 2, 64, 16, e4m3, seed=18, extra_rows=3)
+
+
+def test_replays_of_a_planned_batch():
+    """More sequences than the workgroups sum over by themselves: a captured call follows the lengths, from a workspace that holds anything."""
+    import torch
+    import paper_2504_20490_amd as A
+    rng = np.random.default_rng(19)
+    seqs, width, hkv, hq, d, size, T = 230, 40, 1, 3, 64, 16, 600
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")
+    cu, lens, table = ints(seqs + 1), ints(seqs), ints(seqs, width)
+    pool = torch.from_numpy(rng.standard_normal((2, 500, hkv, size, d))).to(torch.bfloat16).cuda()
+    cache, batch = A.KVCache(pool[0], pool[1]), A.KVBatch(cu, lens, table)
+    q = torch.from_numpy(rng.standard_normal((T, hq, d))).to(torch.bfloat16).cuda()
+    bytes_ = A.attn_paged_workspace_bytes(cache, batch, T, hq)
+    got, want = ([torch.empty_like(q), torch.empty(hq, T, device="cuda"), torch.zeros(bytes_, dtype=torch.uint8, device="cuda")] for _ in range(2))
+    call = lambda x: A.attn_paged_fwd(cache, batch, q, *x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call(got)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call(got)
+    for most in (1, 3, 12, 0):
+        rows = rng.integers(0, most + 1, seqs)
+        rows[np.cumsum(rows) > T] = 0
+        cu.copy_(torch.from_numpy(np.concatenate([[0], np.cumsum(rows)])).int())
+        lens.copy_(torch.from_numpy(rng.integers(0, width * size, seqs)).int())
+        table.copy_(torch.from_numpy(rng.integers(0, 500, (seqs, width))).int())
+        for x in (got, want):
+            x[0].fill_(float("nan")), x[1].fill_(float("nan")), x[2].fill_(255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        call(want)
+        torch.cuda.synchronize()
+        n = int(rows.sum())
+        assert torch.equal(got[0][:n], want[0][:n]) and torch.equal(got[1][:, :n], want[1][:, :n])
+        assert not torch.isnan(got[0][:n].float()).any() and torch.isnan(got[0][n:].float()).all() and torch.isnan(got[1][:, n:]).all()
+
+
 @pytest.mark.parametrize("max_rows", [0, 1, 5])
 @pytest.mark.parametrize("rows,kv", [([70, 1, 9], [400, 300, 9]), ([90], [500])])
 def test_a_wrong_hint_changes_no_result(rows, kv, max_rows):
