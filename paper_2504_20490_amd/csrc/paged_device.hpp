@@ -40,7 +40,7 @@ __device__ __forceinline__ RowPlace place_of(const PagedPool& pool, const PagedR
     RowPlace r{interval_of(b.cu_rows, b.num_seqs, row), -1, -1, 0};
     if (r.seq < 0) return r;
     const int kv = seq_rows(0, 0, b.kv_lens[r.seq], 0, b.table_width, pool.page_shift).kv;
-    const int pos = kv - (b.cu_rows[r.seq + 1] - row);   // (cu_rows[seq + 1] > row)
+    const int pos = kv - (min(b.cu_rows[r.seq + 1], b.total_rows) - row);   // (cu_rows[seq + 1] > row)
     if (pos < 0) return r;
     r.pos = pos;
     r.page = page_at(pool, b, r.seq, pos >> pool.page_shift);

@@ -7,7 +7,7 @@
 // in one page (16 tokens at least), so its base is a scalar, worked out from page numbers that the workgroup keeps in LDS.
 // 8-bit tiles go through registers: fetched an iteration ahead, scaled to bf16 (exact) and written to the tile, in the same places of the
 // schedule where the 16-bit copies are issued; the tile and all that follows is the same.
-// 2048 tokens behind 27034, 32 heads on 8 of 128: bf16 877 to 917 us on four boxes = 1030 to 1070 TFLOP/s of the visible pairs (a large bf16 matrix product here:
+// 2048 tokens behind 27034, 32 heads on 8 of 128: bf16 877 to 923 us on five cards = 1020 to 1070 TFLOP/s of the visible pairs (a large bf16 matrix product here:
 // 1330), e4m3 926 (the conversions are vector work beside the softmax).  8 prompts of 2048, 16 heads: 200 us = 690 TFLOP/s: items of 2 to 32 tiles, whose start
 // (lengths, page numbers, first tiles) and masked tiles weigh more.
 #include "fwd_iteration.hpp"

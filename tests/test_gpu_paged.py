@@ -289,6 +289,28 @@ def test_lengths_and_rows_beyond_the_table_are_clamped():
     torch.cuda.synchronize()
 
 
+def test_rows_cut_off_by_the_tensors_stand_at_the_same_positions_in_every_call():
+    """cu_rows names more rows than the tensors have: the sequence has those that there are, its last ones, in write, read and attention."""
+    import torch
+    import paper_2504_20490_amd as A
+    b = Batch([3, 10], [20, 40], 2, 64, 16, seed=22)
+    b.device(A)
+    _, q = rows_of_q(b, 4)
+    x = torch.randn(b.T, 2, 64, device="cuda").bfloat16()
+    A.kv_cache_write(b.cache, b.batch, x, -x)
+    want, want_lse = attend(A, b, q)
+    before = [t.clone() for t in b.cache.tensors]
+    b.cu_dev[2] = 100
+    A.kv_cache_write(b.cache, b.batch, x, -x)
+    got, got_lse = attend(A, b, q)
+    k, v = torch.empty_like(x), torch.empty_like(x)
+    A.kv_cache_read(b.cache, b.batch, k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want) and torch.equal(got_lse, want_lse) and torch.equal(k, x) and torch.equal(v, -x)
+    for old, new in zip(before, b.cache.tensors):
+        assert torch.equal(old.view(torch.int16), new.view(torch.int16))
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("rows", [[6], [140]])
 def test_infinities_and_nan_where_a_row_does_not_see_them(rows, e4m3):
