@@ -488,15 +488,26 @@ __device__ __forceinline__ void put(const PagedAttnParams& p, const Joined& r, i
         p.lse[unit % p.q_heads * p.rows.total_rows + unit / p.q_heads] = r.total == 0.f ? -INFINITY : (r.top * p.scale_log2 + __log2f(r.total)) * kLn2;
 }
 
-// Many pairs: a team of D / 4 lanes per pair, its chunks one after the other.  Bound by latency: as many pairs as fit are under way at once.
+// Many pairs: a wave looks at `per_wave` of them at once, one per lane, and joins those that have something to join, a team of D / 4 lanes each, their
+// chunks one after the other.  Bound by latency.
 template <int D>
-__global__ __launch_bounds__(kThreads, 8) void paged_join_kernel(PagedAttnParams p) {
-    constexpr int kLanes = D / 4, kTeams = kThreads / kLanes;
-    const int64_t units = (int64_t)p.rows.total_rows * p.q_heads, unit = (int64_t)blockIdx.x * kTeams + threadIdx.x / kLanes;
-    const int col = threadIdx.x % kLanes * 4;
-    if (unit >= units) return;
-    const Pair pair = pair_at(p, unit);
-    if (pair.chunks) put(p, gather<D>(p, pair, 0, 1, col), unit, col);
+__global__ __launch_bounds__(kThreads, 8) void paged_join_kernel(PagedAttnParams p, int per_wave) {
+    constexpr int kLanes = D / 4, kTeams = 64 / kLanes;
+    const int lane = threadIdx.x & 63, team = lane / kLanes, col = lane % kLanes * 4;
+    const int64_t units = (int64_t)p.rows.total_rows * p.q_heads, first = ((int64_t)blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6)) * per_wave;
+    Pair mine{0, 0, 0};
+    if (lane < per_wave && first + lane < units) mine = pair_at(p, first + lane);
+    for (uint64_t left = __ballot(mine.chunks != 0); left;) {
+        int at = -1;                                       // the team's: the first, second, ... of those left
+#pragma unroll
+        for (int t = 0; t < kTeams; ++t) {
+            if (t == team && left) at = __builtin_ctzll(left);
+            left &= left - 1;
+        }
+        const int from = max(at, 0);
+        const Pair pair{__shfl(mine.first, from, 64), __shfl(mine.chunks, from, 64), __shfl(mine.stride, from, 64)};
+        if (at >= 0) put(p, gather<D>(p, pair, 0, 1, col), first + at, col);
+    }
 }
 
 // Few pairs, of many chunks perhaps: a workgroup for COLUMNS columns of one, the chunks dealt out to its teams.
@@ -571,14 +582,15 @@ hipError_t launch_paged_attn(const PagedAttnParams& p, const PagedSizes& sizes, 
     }
     if (!sizes.join) return hipSuccess;
     // up to 4096 pairs: a workgroup each (64 rows of 32 heads, 5 to 30 chunks 7 us); long contexts: several, 32 columns each (one row of 32
-    // heads, 256 chunks 10 -> 7 us, but 5 heads of 34 chunks 3.7 -> 4.9); more: teams (22784 pairs of 2 or 3 chunks 19 us with a workgroup for 6)
+    // heads, 256 chunks 10 -> 7 us, but 5 heads of 34 chunks 3.7 -> 4.9); more: teams (22784 pairs of 2 or 3 chunks 11 us,
+    // 19 us with a workgroup for 6), and as many pairs per wave as keep 8192 waves busy (131072 with nothing to join 4.7 us, 12.4 with one per team)
     const int64_t pairs = (int64_t)p.rows.total_rows * p.q_heads;
     const dim3 threads(kThreads);
     if (pairs > 4096) {
-        const int teams = kThreads / (width / 4);
-        const dim3 grid((unsigned)((pairs + teams - 1) / teams));
-        if (width == 128) hipLaunchKernelGGL(paged_join_kernel<128>, grid, threads, 0, stream, p);
-        else hipLaunchKernelGGL(paged_join_kernel<64>, grid, threads, 0, stream, p);
+        const int teams = 64 / (width / 4), per_wave = (int)std::max<int64_t>(teams, std::min<int64_t>(64, pairs / 8192)), per_group = per_wave * (kThreads / 64);
+        const dim3 grid((unsigned)((pairs + per_group - 1) / per_group));
+        if (width == 128) hipLaunchKernelGGL(paged_join_kernel<128>, grid, threads, 0, stream, p, per_wave);
+        else hipLaunchKernelGGL(paged_join_kernel<64>, grid, threads, 0, stream, p, per_wave);
     } else if (pairs <= 256 && ((int64_t)p.rows.table_width << p.pool.page_shift) >= 128 * unit_keys(false)) {
         const dim3 grid((unsigned)pairs, width / 32);
         if (width == 128) hipLaunchKernelGGL((paged_join_pair_kernel<128, 32>), grid, threads, 0, stream, p);

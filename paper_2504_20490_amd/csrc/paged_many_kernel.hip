@@ -8,7 +8,7 @@
 // 8-bit tiles go through registers: fetched an iteration ahead, scaled to bf16 (exact) and written to the tile, in the same places of the
 // schedule where the 16-bit copies are issued; the tile and all that follows is the same.
 // 2048 tokens behind 27034, 32 heads on 8 of 128: bf16 877 to 923 us on five cards = 1020 to 1070 TFLOP/s of the visible pairs (a large bf16 matrix product here:
-// 1330), e4m3 926 (the conversions are vector work beside the softmax).  8 prompts of 2048, 16 heads: 200 us = 690 TFLOP/s: items of 2 to 32 tiles, whose start
+// 1330), e4m3 926 (the conversions are vector work beside the softmax).  8 prompts of 2048, 16 heads: 188 us = 730 TFLOP/s: items of 2 to 32 tiles, whose start
 // (lengths, page numbers, first tiles) and masked tiles weigh more.
 #include "fwd_iteration.hpp"
 #include "paged_item.hpp"
@@ -256,7 +256,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
                     }
                     if (any) {
                         *reinterpret_cast<u32x4*>(at) = x;
-                        taken_out = 1;
+                        // (behind the last key nobody gets it back)
+                        if (key0(kt) + src.first_row(i) + (j * 1024 + lane * 16) / (D * 2) < w1) taken_out = 1;
                     }
                 }
         };
