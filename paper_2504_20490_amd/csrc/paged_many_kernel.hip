@@ -256,8 +256,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
                     }
                     if (any) {
                         *reinterpret_cast<u32x4*>(at) = x;
-                        // (behind the last key nobody gets it back)
-                        if (key0(kt) + src.first_row(i) + (j * 1024 + lane * 16) / (D * 2) < w1) taken_out = 1;
+                        taken_out = 1;
                     }
                 }
         };
@@ -369,28 +368,48 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
     if (seen_to >= bad_key) l_row = __builtin_nanf("");
     if (!wave_real) return;
     if (taken_out) {
-        for (int key = max(k0, group_limit + 1 - BK); key < k1; ++key) {      // (from the start of the first tile that was looked at, or before)
-            const int page = max(page_at(p.pool, p.rows, it.seq, key >> shift), 0);
-            const int64_t at = src.head_row + (key & ((1 << shift) - 1));
-            const uint8_t* const row = p.pool.v + page * p.pool.page_bytes + at * p.pool.row_bytes;
-            float scale = 1.f;
-            if constexpr (E4M3) scale = scale_of(p.pool.v_scale[page * p.pool.scale_page_bytes + at]);
+        // the keys from the start of the first tile that was looked at, or before; 64 at once, one per lane, are searched for what was taken out (there may
+        // be nothing: what lies behind the last key is taken out too, and nobody gets it back)
+        for (int key0 = max(k0, group_limit + 1 - BK); key0 < k1; key0 += 64) {
+            auto row_at = [&](int key, float& scale) {
+                const int page = max(page_at(p.pool, p.rows, it.seq, key >> shift), 0);
+                const int64_t at = src.head_row + (key & ((1 << shift) - 1));
+                if constexpr (E4M3) scale = scale_of(p.pool.v_scale[page * p.pool.scale_page_bytes + at]);
+                return p.pool.v + page * p.pool.page_bytes + at * p.pool.row_bytes;
+            };
+            uint32_t odd = 0;
+            if (key0 + lane_now < k1) {
+                float scale = 1.f;
+                const uint8_t* const row = row_at(key0 + lane_now, scale);
+                for (int b = 0; b < p.pool.row_bytes; b += 16) {
+                    const u32x4 x = *reinterpret_cast<const u32x4*>(row + b);
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int i4 = 0; i4 < 4; ++i4) {
-                    const int col = db * 32 + i4 * 8 + half * 4;
-                    u32x2 w = {0u, 0u};
-                    if (col < hd) {
-                        if constexpr (E4M3) w = e4m3_to_bf16(*reinterpret_cast<const uint32_t*>(row + col), scale);
-                        else w = *reinterpret_cast<const u32x2*>(row + col * 2);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float x = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
-                        if (key <= seen_to && !is_finite(x)) st.acc[db][4 * i4 + j] += x;
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        odd |= E4M3 ? ((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
                 }
+                if (E4M3 && scale > pow2(119)) odd = 1;                // (a scale that the library does not write: 448 times it may be infinite)
+            }
+            for (uint64_t left = __ballot(odd != 0); left; left &= left - 1) {
+                const int key = key0 + __builtin_ctzll(left);
+                float scale = 1.f;
+                const uint8_t* const row = row_at(key, scale);
+#pragma unroll
+                for (int db = 0; db < DB; ++db)
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const int col = db * 32 + i4 * 8 + half * 4;
+                        u32x2 w = {0u, 0u};
+                        if (col < hd) {
+                            if constexpr (E4M3) w = e4m3_to_bf16(*reinterpret_cast<const uint32_t*>(row + col), scale);
+                            else w = *reinterpret_cast<const u32x2*>(row + col * 2);
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const float x = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+                            if (key <= seen_to && !is_finite(x)) st.acc[db][4 * i4 + j] += x;
+                        }
+                    }
+            }
         }
     }
     const bool whole = it.chunks == 1;
