@@ -717,3 +717,11 @@ def test_pool_beyond_32_bit_offsets(e4m3):
     A.kv_cache_read(b.cache, b.batch, k_want, v_want)
     torch.cuda.synchronize()
     assert torch.equal(k_want, v) and torch.equal(v_want, k)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("d", range(8, 129, 8))
+def test_every_head_dim(d, e4m3):
+    test_write([2, 40], [40, 41], 4, 2, d, 16, True, None, e4m3)
+    test_read([2, 40], [40, 41], 3, d, 16, e4m3)
+    run_attention([1, 45], [100, 150], 4, 2, d, 16, e4m3, seed=23, extra_rows=1)

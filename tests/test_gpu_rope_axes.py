@@ -126,3 +126,9 @@ def test_the_inverse_is_the_gradient(f32):
         e[at] = 0.5                                    # (the map is linear: any step is exact but for rounding)
         diff = f(x + e) - f(x - e)
         assert abs(got[at] - diff) <= 1e-9 + float(tolerance(w, np.array(diff), f32).max())
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("d", range(8, 129, 8))
+def test_every_head_dim(d, f32):
+    test_against_the_oracle(37, 5, 2, d, 3, interleaved, True, d % 16 == 0, f32)
