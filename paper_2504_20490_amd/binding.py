@@ -683,6 +683,7 @@ class KVBatch:
         if kv_lens.get_device() != self.device or page_table.get_device() != self.device:
             raise _bad("cu_rows, kv_lens and page_table have to be on one GPU")
         self.tensors = (cu_rows, kv_lens, page_table)              # (kept alive)
+        self.num_seqs = n
         self._fields = (cu_rows.data_ptr(), kv_lens.data_ptr() or None, page_table.data_ptr() or None, n, shape[1])
         self._max_rows = int(max_rows)
 
@@ -725,7 +726,14 @@ def kv_cache_read(cache: KVCache, batch: KVBatch, k, v, stream=None) -> None:
 
 
 def attn_paged_workspace_bytes(cache: KVCache, batch: KVBatch, total_rows: int, q_heads: int) -> int:
-    return int(load_library().hspmd_attn_paged_workspace_bytes(cache._ref, batch._with_rows(int(total_rows)), int(q_heads)))
+    """Bytes of workspace that attn_paged_fwd takes for total_rows rows of q_heads heads; 0 where there is nothing to do."""
+    lib, rows, heads = load_library(), int(total_rows), int(q_heads)
+    size = int(lib.hspmd_attn_paged_workspace_bytes(cache._ref, batch._with_rows(rows), heads))
+    # (the library answers 0 to what it refuses as well)
+    if size == 0 and (rows < 0 or rows and batch.num_seqs or heads < 1 or heads % cache.kv_heads):
+        status = 1 if lib.hspmd_kv_cache_row(cache.head_dim, cache.dtype) else 2
+        raise HspmdError(status, lib.hspmd_last_error().decode())
+    return size
 
 
 def attn_paged_fwd(cache: KVCache, batch: KVBatch, q, o, lse, workspace, softmax_scale: float = 0.0, stream=None) -> None:
