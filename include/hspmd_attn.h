@@ -442,7 +442,8 @@ typedef struct {
  *   q, q_out   [total_tokens, local_q_heads, head_dim]; k, k_out [total_tokens, local_kv_heads, head_dim]; token strides in
  *              elements, multiples of 8 and >= heads*head_dim, each tensor its own; in place (q_out == q, k_out == k, with the same
  *              stride) is allowed, other overlaps are not; 16-byte aligned
- *   local_kv_heads 0 .. : with 0 only q is turned and k, k_out are not looked at
+ *   total_tokens 0 .. 2^25, local_q_heads 1 .. 65536
+ *   local_kv_heads 0 .. 65536: with 0 only q is turned and k, k_out are not looked at
  *   dtype      HSPMD_GRAD_BF16 or HSPMD_GRAD_F32, the same for all four.  Arithmetic in fp32 (every product and sum rounded once),
  *              one rounding to bf16
  * A position outside the table is not read: the pairs of its axis become NaN for that token.
@@ -482,7 +483,7 @@ typedef struct {
     uint8_t* v_scale;
     int64_t page_stride;         /* elements */
     int64_t scale_page_stride;   /* bytes, e4m3 only */
-    int32_t num_pages, page_size, local_kv_heads, head_dim;
+    int32_t num_pages, page_size, local_kv_heads, head_dim;   /* num_pages >= 1, local_kv_heads 1 .. 65536 */
     hspmd_cache_dtype dtype;
 } hspmd_kv_cache;
 
@@ -502,8 +503,8 @@ typedef struct {
     const int32_t* cu_rows;      /* device, [num_seqs + 1], non-decreasing */
     const int32_t* kv_lens;      /* device, [num_seqs] */
     const int32_t* page_table;   /* device, [num_seqs, table_width] */
-    int32_t num_seqs, table_width;
-    int32_t total_rows;          /* rows of the call's tensors, >= cu_rows[num_seqs] */
+    int32_t num_seqs, table_width;   /* num_seqs 0 .. 2^25 */
+    int32_t total_rows;          /* rows of the call's tensors, >= cu_rows[num_seqs]; 0 .. 2^25 */
     int32_t max_rows;            /* the most rows of a sequence (0: unknown).  Chooses the attention's kernels; a sequence with more is
                                     computed all the same, slower */
 } hspmd_kv_batch;
@@ -515,7 +516,7 @@ int32_t hspmd_kv_cache_row(int32_t head_dim, hspmd_cache_dtype dtype);   /* 0 on
  *   k, v     bf16 [total_rows, local_kv_heads, head_dim], strides as in hspmd_attn_varlen_fwd
  *   rope     NULL: k is written as it is.  Otherwise positions may be NULL: every axis of a row then stands at the row's position
  *            in its sequence (a row without a place stands at none: its q becomes NaN).  k is turned in fp32 and rounded once, to the cache's type
- *   q, q_out with rope: bf16 [total_rows, local_q_heads, head_dim], turned in the same launch (in place allowed); both NULL: k only.
+ *   q, q_out with rope: bf16 [total_rows, local_q_heads, head_dim], local_q_heads 1 .. 65536, turned in the same launch (in place allowed); both NULL: k only.
  *            Without rope both have to be NULL
  * Two rows of one call must not have the same place.
  */
@@ -534,7 +535,7 @@ hspmd_status hspmd_kv_cache_read(const hspmd_kv_cache* cache, const hspmd_kv_bat
  * Attention of the batch's rows over the cache (their own keys and values have been written before): the row at position p
  * sees the keys at positions 0 .. p of its sequence.
  *   q    bf16 [total_rows, local_q_heads, head_dim], 16-byte aligned, token stride as in hspmd_attn_varlen_fwd; local_q_heads a multiple of
- *        the cache's heads, grouped as everywhere
+ *        the cache's heads, grouped as everywhere; total_rows * local_q_heads at most 2^25 (the launch's grid and 32-bit row numbers rest on it)
  *   o    bf16 [total_rows, local_q_heads, head_dim], contiguous, written; lse fp32 [local_q_heads, total_rows], written, may be NULL
  *   workspace  device, at least hspmd_attn_paged_workspace_bytes(cache, batch, local_q_heads) bytes, 16-byte aligned: partial results where
  *        the keys of a row are shared out.  The size follows from num_seqs, table_width, total_rows and the heads, never less for more of

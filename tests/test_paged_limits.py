@@ -1,8 +1,11 @@
 """Sizes at the limits of the calls around the paged cache (no GPU): what the binding and the library say to them."""
+import ctypes
+
 import pytest
 import torch
 
 import paper_2504_20490_amd as A
+from paper_2504_20490_amd import binding
 
 
 def pool(h=2, size=16, d=64, pages=3):
@@ -31,3 +34,32 @@ def test_a_batch_with_nothing_to_do_takes_no_workspace():
     cache = A.KVCache(*pool())
     assert A.attn_paged_workspace_bytes(cache, batch(), 0, 4) == 0 and A.attn_paged_workspace_bytes(cache, batch(seqs=0), 5, 4) == 0
     assert A.attn_paged_workspace_bytes(cache, batch(), 5, 4) > 0
+
+
+def test_the_stated_limits_are_the_ones_that_hold():
+    """The largest sizes that the header names are taken, the next ones are not."""
+    lib, cache = A.load_library(), A.KVCache(*pool())
+    size = lambda heads=2, **change: lib.hspmd_attn_paged_workspace_bytes(cache._ref, ctypes.byref(with_(**change)), heads)
+
+    def with_(num_seqs=2, total_rows=5):
+        b = batch()._with_rows(total_rows)._obj
+        b.num_seqs = num_seqs
+        return b
+
+    assert size(total_rows=1 << 24) > 0 and size(total_rows=(1 << 24) + 1) == 0               # 2^25 rows x heads
+    assert size(num_seqs=1 << 25) > 0 and size(num_seqs=(1 << 25) + 1) == 0
+    assert size(heads=(1 << 25) // 5 // 2 * 2) > 0 and size(heads=((1 << 25) // 5 // 2 + 1) * 2) == 0
+    one = A.KVCache(*pool(h=1))
+    rows = lambda n: lib.hspmd_attn_paged_workspace_bytes(one._ref, batch()._with_rows(n), 1)
+    assert rows(1 << 25) > 0 and rows((1 << 25) + 1) == 0
+    P = 1 << 20                                             # never followed
+    rope = binding._RopeAxesArgs(P, 100, 1, P, 1 << 26, None)
+    for d, hq, hkv, tokens in ((8, 65537, 0, 5), (8, 1, 65537, 5), (8, 1, 1, (1 << 25) + 1), (8, -1, 0, 5)):
+        assert lib.hspmd_rope_axes_qk(ctypes.byref(rope), P, P, 1 << 20, 1 << 20, P, P, 1 << 20, 1 << 20, tokens, hq, hkv, d, 0, 0, None) == 1
+        assert b"65536" in lib.hspmd_last_error() or b"2^25" in lib.hspmd_last_error()
+    for heads in (0, 65537):
+        assert lib.hspmd_kv_cache_write(cache._ref, batch()._with_rows(5), P, P, 128, ctypes.byref(rope), P, P, 1 << 23, 1 << 23, heads, None) == 1
+        assert b"65536" in lib.hspmd_last_error()
+    cache._args.local_kv_heads, cache._args.page_stride = 65537, 1 << 40
+    assert size(heads=65537) == 0 and b"65536" in lib.hspmd_last_error()
+
