@@ -538,8 +538,10 @@ hspmd_status hspmd_kv_cache_read(const hspmd_kv_cache* cache, const hspmd_kv_bat
  *        the cache's heads, grouped as everywhere; total_rows * local_q_heads at most 2^25 (the launch's grid and 32-bit row numbers rest on it)
  *   o    bf16 [total_rows, local_q_heads, head_dim], contiguous, written; lse fp32 [local_q_heads, total_rows], written, may be NULL
  *   workspace  device, at least hspmd_attn_paged_workspace_bytes(cache, batch, local_q_heads) bytes, 16-byte aligned: partial results where
- *        the keys of a row are shared out.  The size follows from num_seqs, table_width, total_rows and the heads, never less for more of
- *        any; nothing in it outlives the call.
+ *        the keys of a row are shared out.  The size follows from the cache's heads, page size and head_dim and from num_seqs, table_width,
+ *        total_rows and local_q_heads (max_rows and the cache's type do not change it).  For one cache it is never less for more of any of the
+ *        latter, so one buffer serves all smaller batches over it; another cache, with more heads of its own for the same query heads say,
+ *        may take less or more.  Nothing in it outlives the call.
  * softmax_scale as in hspmd_attn_varlen_fwd.  No atomics: results are run-to-run bit-identical.  Keys and values that a row does not see take no
  * part in its result, whatever they hold, infinities and NaN included, nor does what the pages hold behind a sequence's last token.
  * An infinity or NaN in a key that a row sees may make that row NaN; in a value, its column.

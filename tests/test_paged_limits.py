@@ -1,5 +1,6 @@
 """Sizes at the limits of the calls around the paged cache (no GPU): what the binding and the library say to them."""
 import ctypes
+import random
 
 import pytest
 import torch
@@ -63,3 +64,30 @@ def test_the_stated_limits_are_the_ones_that_hold():
     cache._args.local_kv_heads, cache._args.page_stride = 65537, 1 << 40
     assert size(heads=65537) == 0 and b"65536" in lib.hspmd_last_error()
 
+
+
+def test_the_workspace_for_one_cache_never_shrinks_with_the_batch():
+    """A buffer for the largest batch serves every smaller one: each of the four sizes alone, at every step, over caches of several shapes."""
+    rng = random.Random(3)
+    lib = A.load_library()
+    pointer = 1 << 20
+    for _ in range(300):
+        h, d, size = rng.choice([1, 2, 3, 8]), rng.choice([8, 64, 72, 128]), rng.choice([16, 64, 1024])
+        cache = binding._KVCacheArgs(pointer, pointer, None, None, h * size * d, 0, 10, size, h, d, A.CACHE_BF16)
+        at = dict(num_seqs=rng.choice([1, 2, 30, 192, 5000]), table_width=rng.choice([0, 1, 3, 200, 8192]), total_rows=rng.choice([1, 2, 3, 17, 300, 5000]),
+                  group=rng.choice([1, 2, 5, 16, 17, 64]))
+
+        def bytes_(num_seqs, table_width, total_rows, group, max_rows=0):
+            batch = binding._KVBatchArgs(pointer, pointer, pointer, num_seqs, table_width, total_rows, max_rows)
+            return lib.hspmd_attn_paged_workspace_bytes(ctypes.byref(cache), ctypes.byref(batch), group * h)
+
+        for name, value in at.items():
+            last = 0
+            for more in sorted([value + i for i in range(20)] + [value * 2, value * 7 + 11, value * 40 + 1]):
+                changed = dict(at, **{name: more})
+                if changed["total_rows"] * changed["group"] * h > 1 << 25:
+                    break
+                now = bytes_(**changed)
+                assert now >= last, (name, more, at, h, d, size)
+                last = now
+        assert bytes_(**at) == bytes_(**at, max_rows=1) == bytes_(**at, max_rows=10 ** 6)
