@@ -534,6 +534,14 @@ def _bad(what: str):
     return HspmdError(1, what)
 
 
+def _count(n, what: str) -> int:
+    """n as the library's 32-bit counts take it (ctypes would cut it off)."""
+    n = int(n)
+    if n + (1 << 31) >> 32:
+        raise _bad(f"{what} does not fit 32 bits")
+    return n
+
+
 def _stream_of(device: int, others: Sequence, stream) -> int:
     """The handle of the stream that a call enqueues on; every tensor has to be on the current GPU, whose stream it is.  `others`: devices of
     the call's other tensors."""
@@ -547,6 +555,8 @@ def _stream_of(device: int, others: Sequence, stream) -> int:
 
 def _rows_stride(x, heads: int, head_dim: int, dtype, what: str, tokens: int) -> int:
     """The token stride of a [tokens, heads, head_dim] tensor of the given type whose rows are contiguous."""
+    if (tokens | heads) >> 31 > 0:
+        raise _bad(f"{what}: its tokens or heads do not fit 32 bits")
     if x.dtype is not dtype or tuple(x.shape) != (tokens, heads, head_dim):
         raise _bad(f"{what} has to be [{tokens}, {heads}, {head_dim}] of {dtype}")
     s = x.stride()
@@ -568,6 +578,7 @@ class RopeAxes:
         self.tensors = (table, positions)                          # (kept alive)
         self.table = table
         self.device = table.get_device()
+        table_positions = _count(table_positions, "table_positions")
         self.pairs, self.tokens = table.numel() // 2 // max(table_positions, 1), None
         axes, stride, where, pairs = 1, 0, None, None
         if positions is not None:
@@ -676,16 +687,18 @@ class KVBatch:
         if cu_rows.dtype is not i32 or kv_lens.dtype is not i32 or page_table.dtype is not i32 or not (
                 cu_rows.is_contiguous() and kv_lens.is_contiguous() and page_table.is_contiguous()):
             raise _bad("cu_rows, kv_lens and page_table have to be contiguous int32 tensors")
-        n, shape = kv_lens.numel(), page_table.shape
+        n, shape, max_rows = kv_lens.numel(), page_table.shape, int(max_rows)
         if cu_rows.numel() != n + 1 or len(shape) != 2 or shape[0] != n:
             raise _bad("cu_rows has to have one entry more than kv_lens, page_table as many rows")
+        if (n | shape[1]) >> 31 or max_rows + (1 << 31) >> 32:
+            raise _bad("num_seqs, table_width or max_rows does not fit 32 bits")
         self.device = cu_rows.get_device()
         if kv_lens.get_device() != self.device or page_table.get_device() != self.device:
             raise _bad("cu_rows, kv_lens and page_table have to be on one GPU")
         self.tensors = (cu_rows, kv_lens, page_table)              # (kept alive)
         self.num_seqs = n
         self._fields = (cu_rows.data_ptr(), kv_lens.data_ptr() or None, page_table.data_ptr() or None, n, shape[1])
-        self._max_rows = int(max_rows)
+        self._max_rows = max_rows
 
     def _with_rows(self, rows: int):
         return ctypes.byref(_KVBatchArgs(*self._fields, rows, self._max_rows))   # (one per call: several threads may share the batch)
@@ -727,7 +740,7 @@ def kv_cache_read(cache: KVCache, batch: KVBatch, k, v, stream=None) -> None:
 
 def attn_paged_workspace_bytes(cache: KVCache, batch: KVBatch, total_rows: int, q_heads: int) -> int:
     """Bytes of workspace that attn_paged_fwd takes for total_rows rows of q_heads heads; 0 where there is nothing to do."""
-    lib, rows, heads = load_library(), int(total_rows), int(q_heads)
+    lib, rows, heads = load_library(), _count(total_rows, "total_rows"), _count(q_heads, "q_heads")
     size = int(lib.hspmd_attn_paged_workspace_bytes(cache._ref, batch._with_rows(rows), heads))
     # (the library answers 0 to what it refuses as well)
     if size == 0 and (rows < 0 or rows and batch.num_seqs or heads < 1 or heads % cache.kv_heads):

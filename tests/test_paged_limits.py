@@ -91,3 +91,28 @@ def test_the_workspace_for_one_cache_never_shrinks_with_the_batch():
                 assert now >= last, (name, more, at, h, d, size)
                 last = now
         assert bytes_(**at) == bytes_(**at, max_rows=1) == bytes_(**at, max_rows=10 ** 6)
+
+
+def test_counts_that_do_not_fit_32_bits_are_refused_not_cut():
+    """2^32 + 12 rows are not 12."""
+    cache, wide = A.KVCache(*pool()), 1 << 32
+    rows = lambda n, h: torch.zeros(1, 1, 1, dtype=torch.bfloat16).expand(n, h, 64)
+    table = torch.zeros(10, 32, 2)
+
+    def refused(f, *args, **kw):
+        with pytest.raises(A.HspmdError) as e:
+            f(*args, **kw)
+        assert e.value.status == 1 and "32 bits" in str(e.value)
+
+    for n in (wide + 12, 1 << 31, -wide + 12):
+        refused(A.attn_paged_workspace_bytes, cache, batch(), n, 4)
+        refused(A.attn_paged_workspace_bytes, cache, batch(), 12, n)
+        refused(batch, max_rows=n)
+        refused(A.RopeAxes, table, n)
+    for x, q in ((rows(wide + 5, 2), rows(wide + 5, 4)), (rows(wide + 5, 2), rows(5, wide + 4))):
+        refused(A.kv_cache_read, cache, batch(), x, x)
+        refused(A.kv_cache_write, cache, batch(), x, x)
+        refused(A.attn_paged_fwd, cache, batch(), q, q, None, table)
+        refused(A.rope_axes_qk, A.RopeAxes(table, 10), q, None, q, None)
+    meta = lambda *s: torch.empty(*s, dtype=torch.int32, device="meta")
+    refused(A.KVBatch, meta(2), meta(1), meta(1, 1 << 31))
