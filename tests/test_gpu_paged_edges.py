@@ -1,0 +1,54 @@
+"""The attention over the paged cache where a token's query heads outnumber a tile's rows or a wave's, and where one long sequence meets many
+short rows in one call.  Oracle and tolerances are those of test_gpu_paged."""
+import numpy as np
+import pytest
+
+from paged_util import Batch, attend
+from test_gpu_paged import check_attention, rows_of_q, run_attention
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("group", [17, 32, 33, 40, 136, 300])
+@pytest.mark.parametrize("rows,kv,kv_heads,d", [
+    ([1], [300], 1, 128),
+    ([1, 1, 1], [31, 129, 640], 2, 64),
+    ([3, 0, 2], [200, 70, 65], 1, 104),                   # a token in two tiles, a tile of two tokens
+    ([1, 30, 1], [500, 90, 7], 1, 64),
+    ([1], [9000], 1, 64),                                 # keys shared out
+    ([5, 1], [3, 0], 1, 40),                              # rows without a place, and no key at all
+])
+def test_groups_above_a_tile_of_few_rows(rows, kv, kv_heads, d, group, e4m3):
+    """17: the fewest that single tokens leave the kernel for few rows with; 32, 33, 40: whole waves without a row; 136, 300: a token in several tiles."""
+    run_attention(rows, kv, group * kv_heads, kv_heads, d, 16, e4m3, seed=24 + group % 2, extra_rows=2)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("group", [17, 40, 136])
+def test_hidden_infinities_and_nan_with_large_groups(group, e4m3):
+    """The last token's key and value, and the one's in the middle, are not finite: the tokens before do not see them."""
+    import torch
+    import paper_2504_20490_amd as A
+    kv = 200
+    b = Batch([4], [kv], 1, 128, 16, e4m3, seed=26)
+    for back, value in ((1, np.nan), (3, np.inf)):
+        page, slot = b.table[0, (kv - back) // 16], (kv - back) % 16
+        if e4m3:
+            b.v_code[page, :, slot, 5], b.k_code[page, :, slot, 7] = 127, 255
+            b.v[page, :, slot, 5] = b.k[page, :, slot, 7] = np.nan
+        else:
+            b.v[page, :, slot, 5] = value
+    b.device(A)
+    q64, q = rows_of_q(b, group)
+    o, lse = attend(A, b, q)
+    torch.cuda.synchronize()
+    check_attention(b, group, o, lse, q64, 1.0 / np.sqrt(128))
+    assert torch.isfinite(o[0].float()).all() and not torch.isfinite(o[3].float()).all()
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows,kv,hq,hkv", [([1, 700], [20000, 700], 8, 2), ([70, 1, 40, 1], [90, 9000, 40, 30000], 40, 1)])
+def test_one_long_sequence_among_many_rows(rows, kv, hq, hkv, e4m3):
+    """More than 4096 (row, head) pairs, a few of which have results of many chunks to join."""
+    run_attention(rows, kv, hq, hkv, 64, 16, e4m3, seed=27, extra_rows=3)
