@@ -470,9 +470,12 @@ hspmd_status hspmd_rope_axes_qk(const hspmd_rope_axes* rope, const void* q, cons
  *   HSPMD_CACHE_E4M3 8-bit floats (4 exponent, 3 mantissa bits, no infinities) with one power-of-two scale per token and head:
  *                    value = e4m3 * 2^(scale - 127), scales in k_scale, v_scale, uint8 [num_pages, local_kv_heads, page_size], page i
  *                    at i * scale_page_stride (a multiple of 4).  A power of two costs a float no precision, makes
- *                    quantisation and reading back exact but for the one rounding to 8 bits, and every value is a bf16 number.
+ *                    quantisation and reading back exact but for the one rounding to 8 bits, and every value is a bf16 number, with one
+ *                    exception: from |x| = 1.9375 * 2^127 on 8 bits round to 2^128, which reads back as an infinity.
  *                    hspmd_kv_cache_write takes e = the smallest integer >= -100 with max |x| <= 448 * 2^e over the row's finite
- *                    elements, stores scale = e + 127 and round-to-nearest-even(x / 2^e); infinities and NaN become NaN
+ *                    elements, stores scale = e + 127 and round-to-nearest-even(x / 2^e); infinities and NaN become NaN.
+ *                    Scales are 27 .. 247 therefore; a cache that was filled otherwise has to keep to that (nothing checks it: rows that see
+ *                    another scale have no defined result, the others theirs)
  *   page_size        a power of two, 16 .. 1024
  */
 typedef enum { HSPMD_CACHE_BF16 = 0, HSPMD_CACHE_E4M3 = 1 } hspmd_cache_dtype;

@@ -387,7 +387,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_many_kernel(PagedAttnParams
                     for (int e = 0; e < 4; ++e)
                         odd |= E4M3 ? ((x[e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u : ((x[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
                 }
-                if (E4M3 && scale > pow2(119)) odd = 1;                // (a scale that the library does not write: 448 times it may be infinite)
+                if (E4M3 && scale > pow2(119)) odd = 1;                // (the largest scale, 2^120: from 256 times it on the value is infinite)
             }
             for (uint64_t left = __ballot(odd != 0); left; left &= left - 1) {
                 const int key = key0 + __builtin_ctzll(left);

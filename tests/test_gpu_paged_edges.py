@@ -1,8 +1,9 @@
 """The attention over the paged cache where a token's query heads outnumber a tile's rows or a wave's, and where one long sequence meets many
-short rows in one call.  Oracle and tolerances are those of test_gpu_paged."""
+short rows in one call; the largest numbers of the 8-bit cache.  Oracle and tolerances are those of test_gpu_paged."""
 import numpy as np
 import pytest
 
+from oracle import paged
 from paged_util import Batch, attend
 from test_gpu_paged import check_attention, rows_of_q, run_attention
 
@@ -52,3 +53,28 @@ def test_hidden_infinities_and_nan_with_large_groups(group, e4m3):
 def test_one_long_sequence_among_many_rows(rows, kv, hq, hkv, e4m3):
     """More than 4096 (row, head) pairs, a few of which have results of many chunks to join."""
     run_attention(rows, kv, hq, hkv, 64, 16, e4m3, seed=27, extra_rows=3)
+
+
+def test_the_largest_numbers_of_the_8_bit_cache():
+    """Values up to where 8 bits round to 2^128, which is no number of bf16: those read back as infinities, everything below as it is stored."""
+    import torch
+    import paper_2504_20490_amd as A
+    b = Batch([6], [6], 1, 16, 16, True, seed=28)
+    b.device(A)
+    top = 2.0 ** 127
+    x = np.zeros((6, 1, 16))
+    for row, first in enumerate((1.75, 1.7578125, 1.9296875, 1.9375, 1.9921875, 0.875)):
+        x[row, 0] = np.array([first] + [1.0, -0.5, 2.0 ** -9] * 5) * top
+        x[row, 0, 7] = -first * top
+    k = torch.from_numpy(x).to(torch.bfloat16).cuda()
+    assert (k.double().cpu().numpy() == x).all()
+    A.kv_cache_write(b.cache, b.batch, k, -k)
+    back = torch.empty(2, 6, 1, 16, dtype=torch.bfloat16, device="cuda")
+    A.kv_cache_read(b.cache, b.batch, back[0], back[1])
+    torch.cuda.synchronize()
+    codes, byte = paged.quantise(x)
+    want = paged.dequantise(codes, byte)
+    want = np.where(np.abs(want) >= 2.0 ** 128, np.sign(want) * np.inf, want)
+    assert np.isinf(want[3:5, 0, [0, 7]]).all() and np.isinf(want).sum() == 4
+    got = back.double().cpu().numpy()
+    assert np.array_equal(got[0], want) and np.array_equal(got[1], -want)
