@@ -10,8 +10,10 @@
 // the LDS transpose read.
 //   S^T = K Q^T (16x16x32, 2 key blocks x D/32 steps),  P = exp2(c S - c m),  O^T += V^T P^T (D/16 blocks, one step of 32 keys)
 // 8-bit tiles are copied as they are; K is scaled to bf16 on its way from LDS (exact), V's scales go into the weights
-// before they are rounded, its bytes are converted as they are.  Weights are rounded to bf16 for the product (half a step of 2^-8 each, at random: their
-// sum is that of the unrounded ones); scores, maxima, sums and O are fp32.
+// before they are rounded (exact), its bytes are converted as they are.  Weights go into their product in two bf16 parts, the rounded one and what that left
+// of it (16 bits together): the matrix cores have the time.  With the rounded part alone the result is 1.1 to 1.3 times as far from the formula in 64 bits
+// (1.88e-3 to 2.16e-3 of it against 1.61e-3 to 1.68e-3, all of which is O's own rounding), at 125 against 127 us for the 64 sequences below and the same time for
+// the others.  Scores, maxima, sums and O are fp32.
 // One token of a sequence of 131001 keys, 32 heads on 8 of 128, bf16: 99 us = 5.4 TB/s (and 7 us for the join); of 64 sequences with 272960 keys together,
 // e4m3: 113 us = 5.0 TB/s (5 us); of one with 1058, 5 heads: 6.2 us (4.3), start and three trips to memory.  Counters: HBM reads 1.00 and 1.06 times the
 // cache's bytes (the scales' lines are fetched by several units), vector units a third busy.
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
             const float alpha = fast_exp2((m - m_ref) * c), mc = m_ref * c;
             m = m_new;
             float sum = 0.f;
-            union { u32x4 u; bf16x8 v; } w;
+            union { u32x4 u; bf16x8 v; } w, rest;      // the weights rounded to bf16, and what that left of them
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb) {
                 float e[4];
@@ -269,6 +271,10 @@ __global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
                 }
                 w.u[2 * mb] = pack_bf16(e[0], e[1]);
                 w.u[2 * mb + 1] = pack_bf16(e[2], e[3]);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) e[i] -= __uint_as_float(i & 1 ? w.u[2 * mb + i / 2] & 0xffff0000u : w.u[2 * mb + i / 2] << 16);
+                rest.u[2 * mb] = pack_bf16(e[0], e[1]);
+                rest.u[2 * mb + 1] = pack_bf16(e[2], e[3]);
             }
             l = l * alpha + sum;
             if (__any(alpha != 1.f)) {
@@ -294,7 +300,7 @@ __global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
                             const u32x2 y = e4m3_to_bf16(__builtin_amdgcn_perm(b.u[1], b.u[0], pick), 1.f);
                             union { u32x4 u; bf16x8 v; } t4;
                             t4.u = u32x4{x[0], x[1], y[0], y[1]};
-                            sum_of[2 * cb + odd] = mfma16(t4.v, w.v, sum_of[2 * cb + odd]);
+                            sum_of[2 * cb + odd] = mfma16(t4.v, rest.v, mfma16(t4.v, w.v, sum_of[2 * cb + odd]));
                         }
                     }
                 } else {
@@ -303,7 +309,7 @@ __global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
                         union { struct { s16x4 a, b; } s; bf16x8 v; } u;
                         u.s.a = lds_transpose_read(vt + Tile::at(v_row, db * 32 + v_byte));
                         u.s.b = lds_transpose_read(vt + Tile::at(v_row + 16, db * 32 + v_byte));
-                        sum_of[db] = mfma16(u.v, w.v, sum_of[db]);
+                        sum_of[db] = mfma16(u.v, rest.v, mfma16(u.v, w.v, sum_of[db]));
                     }
                 }
             };

@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 
 from oracle import paged
-from paged_util import Batch, attend
+from paged_util import BF16_HALF_STEP, Batch, attend
 from test_gpu_paged import check_attention, rows_of_q, run_attention
 
 pytestmark = pytest.mark.gpu
@@ -53,6 +53,25 @@ def test_hidden_infinities_and_nan_with_large_groups(group, e4m3):
 def test_one_long_sequence_among_many_rows(rows, kv, hq, hkv, e4m3):
     """More than 4096 (row, head) pairs, a few of which have results of many chunks to join."""
     run_attention(rows, kv, hq, hkv, 64, 16, e4m3, seed=27, extra_rows=3)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows,kv,hq,hkv,d", [([1, 1, 1], [2, 5, 40], 8, 2, 128), ([3, 2], [6, 300], 5, 1, 64), ([1], [3000], 4, 1, 104), ([2, 60], [9, 60], 4, 1, 64)])
+def test_few_rows_are_off_by_their_own_rounding_alone(rows, kv, hq, hkv, d, e4m3):
+    """Weights keep 16 bits for their product: O is off by half a bf16 step of its value, and by half a step of 2^-16 and what fp32 scores and sums
+    leave (1e-4, as in test_gpu_paged) of sum_j P_j |v_j|."""
+    import torch
+    import paper_2504_20490_amd as A
+    b = Batch(rows, kv, hkv, d, 16, e4m3, seed=29)
+    b.device(A)
+    q64, q = rows_of_q(b, hq)
+    o, _ = attend(A, b, q)
+    torch.cuda.synchronize()
+    n = b.cu[1] if max(rows) * hq // hkv > 16 else b.T                             # (the other sequence is for the kernel for many rows)
+    ref, _ = paged.attention(q64, b.k, b.v, b.cu, b.kv, b.table, b.size, d ** -0.5)
+    mass, _ = paged.attention(q64, b.k, np.abs(b.v), b.cu, b.kv, b.table, b.size, d ** -0.5)
+    off = np.abs(o.double().cpu().numpy() - ref)[:n]
+    assert (off <= BF16_HALF_STEP * np.abs(ref[:n]) + (2.0 ** -16 + 1e-4) * mass[:n]).all()
 
 
 def test_the_largest_numbers_of_the_8_bit_cache():
