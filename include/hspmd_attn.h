@@ -496,7 +496,7 @@ typedef struct {
  * lies in slot p % page_size of page page_table[s * table_width + p / page_size].
  * All three arrays are DEVICE memory and are read when the kernels run: a captured graph replays with the lengths and pages
  * that it finds there.  The host therefore cannot check them; the kernels do, and no value in them leads out of the pool or the
- * tensors: rows of a sequence are clamped to 0 .. total_rows, its length to table_width * page_size.
+ * tensors: rows of a sequence are clamped to 0 .. total_rows, its length to table_width * page_size and to 2^31 - 256.
  * A row whose position is negative (n > kv_lens[s]) has no place in the cache: a write skips it, a read gives zeros, the
  * attention gives O = 0 and LSE = -inf.  A page number outside 0 .. num_pages-1 is not followed: a write skips the row, a read
  * gives NaN, the attention gives NaN to rows that would see a key of that page.  Rows that belong to no sequence (behind

@@ -4,8 +4,8 @@ import numpy as np
 import pytest
 
 from oracle import paged
-from paged_util import BF16_HALF_STEP, Batch, attend
-from test_gpu_paged import check_attention, rows_of_q, run_attention
+from paged_util import BF16_HALF_STEP, Batch, attend, bf16
+from test_gpu_paged import LSE_ABS, check_attention, rows_of_q, run_attention
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +97,74 @@ def test_the_largest_numbers_of_the_8_bit_cache():
     assert np.isinf(want[3:5, 0, [0, 7]]).all() and np.isinf(want).sum() == 4
     got = back.double().cpu().numpy()
     assert np.array_equal(got[0], want) and np.array_equal(got[1], -want)
+
+
+@pytest.mark.parametrize("e4m3", [False, True])
+@pytest.mark.parametrize("rows", [1, 40])
+def test_lengths_next_to_two_to_the_31(rows, e4m3):
+    """The longest sequence that there can be, one page of 1024 tokens over and over: every row sees whole rounds of it, the last one's keys up to
+    its own beside them."""
+    import torch
+    import paper_2504_20490_amd as A
+    size, d, width = 1024, 16, 1 << 21
+    kv = (1 << 31) - 2 * size + 5
+    b = Batch([size], [size], 1, d, size, e4m3, seed=30, extra_pages=0, extra_width=0)
+    b.device(A)
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")
+    b.batch = A.KVBatch(i32(0, rows), i32(kv), torch.zeros(1, width, dtype=torch.int32, device="cuda"), rows)
+    q64 = bf16(b.rng.standard_normal((rows, 2, d)))
+    q64[:, 0] = 0.0                                                                 # (all weights 1: the sums count the keys)
+    o, lse = attend(A, b, torch.from_numpy(q64).to(torch.bfloat16).cuda())
+    back = torch.empty(2, rows, 1, d, dtype=torch.bfloat16, device="cuda")
+    A.kv_cache_read(b.cache, b.batch, back[0], back[1])
+    torch.cuda.synchronize()
+    k, v = b.k[b.table[0, 0], 0], b.v[b.table[0, 0], 0]
+    pos = kv - rows + np.arange(rows)
+    assert np.array_equal(back[0, :, 0].double().cpu().numpy(), k[pos % size]) and np.array_equal(back[1, :, 0].double().cpu().numpy(), v[pos % size])
+    times = (pos[:, None] + size - np.arange(size)) // size                        # how often a row sees each key
+    s = np.einsum("thd,kd->htk", q64, k) / np.sqrt(d)
+    top = s.max(-1, keepdims=True)
+    w = times * np.exp(s - top)
+    total = w.sum(-1, keepdims=True)
+    ref, mass = w / total @ v, w / total @ np.abs(v)
+    got = o.double().cpu().numpy().transpose(1, 0, 2)
+    # A share of at most 2^22 keys is summed up tile by tile (32 keys, or 64): at most 2^16 sums one after the other, rounded by 2^-24 of them each, in O and
+    # in the weights; 2^-7 of the mass together.  Weights of 1 are summed up exactly in a share, and in at most 2048 shares to 2^-13.
+    assert (np.abs(got - ref) <= BF16_HALF_STEP * np.abs(ref) + (BF16_HALF_STEP + 2.0 ** -7 + 1e-4) * mass).all()
+    off = np.abs(lse.double().cpu().numpy() - (top + np.log(total))[..., 0])
+    assert (off[0] <= 2.0 ** -13 + 1e-5).all() and (off[1] <= 2.0 ** -8 + LSE_ABS).all()
+
+
+def test_as_many_rows_as_there_can_be():
+    """2^25 tokens through the axes rotation, the write and the read, and as many sequences of one token through the attention."""
+    import torch
+    import paper_2504_20490_amd as A
+    T, d = 1 << 25, 8
+    i32 = lambda x: x.to(torch.int32).cuda()
+    x = torch.randn(T, 1, d, device="cuda").bfloat16()
+    pool = torch.zeros(2, T // 1024, 1, 1024, d, dtype=torch.bfloat16, device="cuda")
+    cache = A.KVCache(pool[0], pool[1])
+    pages = i32(torch.randperm(T // 1024))[None]
+    batch = A.KVBatch(i32(torch.tensor([0, T])), i32(torch.tensor([T])), pages)
+    A.kv_cache_write(cache, batch, x, -x)
+    back = torch.empty(2, T, 1, d, dtype=torch.bfloat16, device="cuda")
+    A.kv_cache_read(cache, batch, back[0], back[1])
+    assert torch.equal(back[0], x) and torch.equal(back[1], -x) and torch.equal(pool[0, pages[0].long()].view(T, 1, d), x)
+    table = torch.empty(4, d // 2, 2, device="cuda")
+    A.rope_table(table, 4, d)
+    turned, again = torch.empty_like(x), torch.empty_like(x)
+    rope = A.RopeAxes(table, 4, i32(torch.arange(T) % 4))
+    A.rope_axes_qk(rope, x, None, turned, None)
+    part = A.RopeAxes(table, 4, i32(torch.arange(T - 1000, T) % 4))
+    A.rope_axes_qk(part, x[-1000:], None, again[-1000:], None)
+    assert torch.equal(turned[-1000:], again[-1000:]) and torch.equal(turned[::4], x[::4])
+    # sequence s: one token, in slot 0 of a page of 16 (of 2^21): O is its value
+    cache = A.KVCache(pool[0].view(-1, 1, 16, d), pool[1].view(-1, 1, 16, d))
+    table = i32(torch.arange(T) % (T // 16))[:, None]
+    batch = A.KVBatch(i32(torch.arange(T + 1)), torch.ones(T, dtype=torch.int32, device="cuda"), table, 1)
+    o, lse = torch.empty_like(x), torch.empty(1, T, device="cuda")
+    A.attn_paged_fwd(cache, batch, x, o, lse, torch.empty(A.attn_paged_workspace_bytes(cache, batch, T, 1), dtype=torch.uint8, device="cuda"))
+    first = pool.view(2, -1, 16, d)[:, :, 0]
+    assert torch.equal(o[:, 0], first[1][table[:, 0].long()])
+    score = (x[:, 0].float() * first[0][table[:, 0].long()].float()).sum(-1) / d ** 0.5
+    assert (lse[0] - score).abs().max() <= 1e-4
