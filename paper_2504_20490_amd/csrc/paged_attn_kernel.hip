@@ -12,11 +12,11 @@
 // 8-bit tiles are copied as they are; K is scaled to bf16 on its way from LDS (exact), V's scales go into the weights
 // before they are rounded (exact), its bytes are converted as they are.  Weights go into their product in two bf16 parts, the rounded one and what that left
 // of it (16 bits together): the matrix cores have the time.  With the rounded part alone the result is 1.1 to 1.3 times as far from the formula in 64 bits
-// (1.88e-3 to 2.16e-3 of it against 1.61e-3 to 1.68e-3, all of which is O's own rounding), at 125 against 127 us for the 64 sequences below and the same time for
-// the others.  Scores, maxima, sums and O are fp32.
-// One token of a sequence of 131001 keys, 32 heads on 8 of 128, bf16: 99 us = 5.4 TB/s (and 7 us for the join); of 64 sequences with 272960 keys together,
-// e4m3: 113 us = 5.0 TB/s (5 us); of one with 1058, 5 heads: 6.2 us (4.3), start and three trips to memory.  Counters: HBM reads 1.00 and 1.06 times the
-// cache's bytes (the scales' lines are fetched by several units), vector units a third busy.
+// (1.88e-3 to 2.16e-3 of it against 1.61e-3 to 1.68e-3, all of which is O's own rounding), at 126 against 127 us for the 64 sequences below and the same time for
+// the others (with the join).  Scores, maxima, sums and O are fp32.
+// One token of a sequence of 131001 keys, 32 heads on 8 of 128, bf16: 101 us = 5.3 TB/s (and 7 us for the join); of 64 sequences with 272960 keys together,
+// e4m3: 118 us = 4.8 TB/s (5 us); of one with 1058, 5 heads: 6.3 us (4), start and three trips to memory.  Counters: HBM reads 1.00 and 1.06 times the
+// cache's bytes (the scales' lines are fetched by several units), matrix cores a tenth busy.
 #include "paged_item.hpp"
 
 namespace hspmd {
@@ -587,6 +587,8 @@ hipError_t launch_paged_attn(const PagedAttnParams& p, const PagedSizes& sizes, 
         if (const hipError_t e = launch_paged_many(p, sizes.many_grid, e4m3, stream)) return e;
     }
     if (!sizes.join) return hipSuccess;
+    // Chosen by the pairs of the call and the width of the table: the host does not know how many chunks a pair has.  (A few pairs of very many chunks in a large call wait for
+    // one team's walk over them: a token over 131001 keys, 32 heads, 110 us by itself, 172 in a batch padded to 256 rows.)
     // up to 4096 pairs: a workgroup each (64 rows of 32 heads, 5 to 30 chunks 7 us); long contexts: several, 32 columns each (one row of 32
     // heads, 256 chunks 10 -> 7 us, but 5 heads of 34 chunks 3.7 -> 4.9); more: teams (22784 pairs of 2 or 3 chunks 11 us,
     // 19 us with a workgroup for 6), and as many pairs per wave as keep 8192 waves busy (131072 with nothing to join 4.7 us, 12.4 with one per team)

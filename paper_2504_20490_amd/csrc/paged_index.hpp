@@ -35,6 +35,8 @@ HSPMD_INDEX SeqRows seq_rows(int cu, int cu_next, int kv_len, int total_rows, in
 
 // Row tiles of a (sequence, KV head), and units of keys.  The kernel for few rows takes sequences with up to `few_limit` rows
 // (new tokens x query heads of a KV head), the one for many the others.
+// Every row tile counts all keys of its sequence.  It walks those up to its last row only: the same but for the sequence's own new tokens, so exact for single tokens and close behind a long
+// prefix; in a prompt without one the last chunks of the first tiles are empty and the last tiles have up to twice the mean (one of 2048, 16 heads: 52 us, the packed forward 34).
 struct SeqTiles {
     int tiles, units;
 };

@@ -7,9 +7,12 @@
 // in one page (16 tokens at least), so its base is a scalar, worked out from page numbers that the workgroup keeps in LDS.
 // 8-bit tiles go through registers: fetched an iteration ahead, scaled to bf16 (exact) and written to the tile, in the same places of the
 // schedule where the 16-bit copies are issued; the tile and all that follows is the same.
-// 2048 tokens behind 27034, 32 heads on 8 of 128: bf16 877 to 923 us on five cards = 1020 to 1070 TFLOP/s of the visible pairs (a large bf16 matrix product here:
-// 1330), e4m3 926 (the conversions are vector work beside the softmax).  8 prompts of 2048, 16 heads: 188 us = 730 TFLOP/s: items of 2 to 32 tiles, whose start
-// (lengths, page numbers, first tiles) and masked tiles weigh more.
+// Weights are rounded to bf16 for their product with the values, as in the packed forward (O 2.3e-3 from the formula in 64 bits, 1.7e-3 of it its own rounding); two
+// bf16 parts, as for few rows, take half as many matrix instructions again: 902 -> 1238 us for the first case below.
+// 2048 tokens behind 27034, 32 heads on 8 of 128: bf16 877 to 923 us on six cards = 1020 to 1070 TFLOP/s of the visible pairs (a large bf16 matrix product here:
+// 1330), e4m3 926 to 943 (the conversions are vector work beside the softmax).  8 prompts of 2048, 16 heads: 182 us = 757 TFLOP/s, the packed forward 151: items of 2 to 32 tiles, whose start
+// (lengths, page numbers, first tiles) and masked tiles weigh more, dealt out as if each had all keys (seq_tiles).  16 sequences of 4 tokens, 64 heads on 8, 16000 keys (32 rows per
+// KV head): bf16 202 us = 5.2 TB/s, e4m3 126 us = 4.2.
 #include "fwd_iteration.hpp"
 #include "paged_item.hpp"
 
