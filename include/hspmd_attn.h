@@ -549,7 +549,7 @@ hspmd_status hspmd_kv_cache_read(const hspmd_kv_cache* cache, const hspmd_kv_bat
  * part in its result, whatever they hold, infinities and NaN included, nor does what the pages hold behind a sequence's last token.
  * An infinity or NaN in a key that a row sees may make that row NaN; in a value, its column.
  * Scores, sums and O are fp32 until the one rounding to bf16.  For their product with the values the weights are rounded to bf16, as in
- * hspmd_attn_varlen_fwd; in sequences of up to 16 rows per KV head (new tokens x query heads of a group) they keep 16 bits, if there are
+ * hspmd_attn_varlen_fwd; in sequences of up to 16 rows per KV head (new tokens x query heads of a group) they keep 15 bits, if there are
  * several sequences or max_rows says that none has more.
  * hspmd_attn_paged_workspace_bytes is 0 for bad arguments (hspmd_last_error says which) and where there is nothing to do.  Per-kernel timing
  * (hspmd_profile_enable) does not record the calls of this section.

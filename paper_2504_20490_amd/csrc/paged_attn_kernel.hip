@@ -10,10 +10,10 @@
 // the LDS transpose read.
 //   S^T = K Q^T (16x16x32, 2 key blocks x D/32 steps),  P = exp2(c S - c m),  O^T += V^T P^T (D/16 blocks, one step of 32 keys)
 // 8-bit tiles are copied as they are; K is scaled to bf16 on its way from LDS (exact), V's scales go into the weights
-// before they are rounded (exact), its bytes are converted as they are.  Weights go into their product in two bf16 parts, the rounded one and what that left
-// of it (16 bits together): the matrix cores have the time.  With the rounded part alone the result is 1.1 to 1.3 times as far from the formula in 64 bits
-// (1.88e-3 to 2.16e-3 of it against 1.61e-3 to 1.68e-3, all of which is O's own rounding), at 126 against 127 us for the 64 sequences below and the same time for
-// the others (with the join).  Scores, maxima, sums and O are fp32.
+// (exact), its bytes are converted as they are.  Weights go into their product in two bf16 parts, their upper 8 bits and the rest rounded (15 bits or more together):
+// the matrix cores have the time.  Rounded to one part they leave the result 1.1 to 1.3 times as far from the formula in 64 bits (1.88e-3 to 2.16e-3 of it against
+// 1.61e-3 to 1.68e-3, all of which is O's own rounding), at 127 against 129 us for the 64 sequences below and the same time for the others (with the join).
+// Scores, maxima, sums and O are fp32.
 // One token of a sequence of 131001 keys, 32 heads on 8 of 128, bf16: 101 us = 5.3 TB/s (and 7 us for the join); of 64 sequences with 272960 keys together,
 // e4m3: 118 us = 4.8 TB/s (5 us); of one with 1058, 5 heads: 6.3 us (4), start and three trips to memory.  Counters: HBM reads 1.00 and 1.06 times the
 // cache's bytes (the scales' lines are fetched by several units), matrix cores a tenth busy.
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
             const float alpha = fast_exp2((m - m_ref) * c), mc = m_ref * c;
             m = m_new;
             float sum = 0.f;
-            union { u32x4 u; bf16x8 v; } w, rest;      // the weights rounded to bf16, and what that left of them
+            union { u32x4 u; bf16x8 v; } w, rest;      // the weights cut to bf16, and what is left of them
 #pragma unroll
             for (int mb = 0; mb < 2; ++mb) {
                 float e[4];
@@ -269,10 +269,12 @@ __global__ __launch_bounds__(kWave) void paged_few_kernel(PagedAttnParams p) {
                         if (masked) e[i] = 16 * mb + i > seen ? 0.f : e[i];
                     }
                 }
-                w.u[2 * mb] = pack_bf16(e[0], e[1]);
-                w.u[2 * mb + 1] = pack_bf16(e[2], e[3]);
+                // (the upper halves of two words.  What is left is positive for every weight above 2^-102: 2^-24 of the weight is added, so that a value which
+                // is infinite stays so in both products)
+                w.u[2 * mb] = __builtin_amdgcn_perm(__float_as_uint(e[1]), __float_as_uint(e[0]), 0x07060302u);
+                w.u[2 * mb + 1] = __builtin_amdgcn_perm(__float_as_uint(e[3]), __float_as_uint(e[2]), 0x07060302u);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) e[i] -= __uint_as_float(i & 1 ? w.u[2 * mb + i / 2] & 0xffff0000u : w.u[2 * mb + i / 2] << 16);
+                for (int i = 0; i < 4; ++i) e[i] = fmaf(e[i], 0x1p-24f, e[i] - __uint_as_float(__float_as_uint(e[i]) & 0xffff0000u));
                 rest.u[2 * mb] = pack_bf16(e[0], e[1]);
                 rest.u[2 * mb + 1] = pack_bf16(e[2], e[3]);
             }

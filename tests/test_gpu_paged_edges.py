@@ -58,8 +58,8 @@ def test_one_long_sequence_among_many_rows(rows, kv, hq, hkv, e4m3):
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("rows,kv,hq,hkv,d", [([1, 1, 1], [2, 5, 40], 8, 2, 128), ([3, 2], [6, 300], 5, 1, 64), ([1], [3000], 4, 1, 104), ([2, 60], [9, 60], 4, 1, 64)])
 def test_few_rows_are_off_by_their_own_rounding_alone(rows, kv, hq, hkv, d, e4m3):
-    """Weights keep 16 bits for their product: O is off by half a bf16 step of its value, and by half a step of 2^-16 and what fp32 scores and sums
-    leave (1e-4, as in test_gpu_paged) of sum_j P_j |v_j|."""
+    """Weights go into their product as their upper 8 bits and a rest (below 2^-7 of the weight) rounded to 8: O is off by half a bf16 step of its value, and
+    by 2^-8 of 2^-7 and what fp32 scores and sums leave (1e-4, as in test_gpu_paged) of sum_j P_j |v_j|."""
     import torch
     import paper_2504_20490_amd as A
     b = Batch(rows, kv, hkv, d, 16, e4m3, seed=29)
@@ -71,7 +71,33 @@ def test_few_rows_are_off_by_their_own_rounding_alone(rows, kv, hq, hkv, d, e4m3
     ref, _ = paged.attention(q64, b.k, b.v, b.cu, b.kv, b.table, b.size, d ** -0.5)
     mass, _ = paged.attention(q64, b.k, np.abs(b.v), b.cu, b.kv, b.table, b.size, d ** -0.5)
     off = np.abs(o.double().cpu().numpy() - ref)[:n]
-    assert (off <= BF16_HALF_STEP * np.abs(ref[:n]) + (2.0 ** -16 + 1e-4) * mass[:n]).all()
+    assert (off <= BF16_HALF_STEP * np.abs(ref[:n]) + (2.0 ** -15 + 1e-4) * mass[:n]).all()
+
+
+@pytest.mark.parametrize("rows", [[1], [7], [90]])
+def test_infinite_values_make_infinite_results(rows):
+    """An infinity of a value that a row sees stands in that column of its result, with the value's sign, whatever its weight (one key: 1)."""
+    import torch
+    import paper_2504_20490_amd as A
+    b = Batch([1] + rows, [1, 120], 2, 64, 16, False, seed=31)
+    for s, p, col, value in ((0, 0, 3, np.inf), (0, 0, 4, -np.inf), *((1, p, p % 61, (-1) ** p * np.inf) for p in range(0, 120, 3))):
+        b.v[b.table[s, p // 16], :, p % 16, col] = value
+    b.device(A)
+    q64, q = rows_of_q(b, 4)
+    o, lse = attend(A, b, q)
+    torch.cuda.synchronize()
+    o, k = o.double().cpu().numpy(), 0
+    for s, (n, kv) in enumerate(zip(b.rows, b.kv)):
+        for r in range(n):
+            seen = b.v[b.table[s, np.arange(kv - n + r + 1) // 16], :, np.arange(kv - n + r + 1) % 16]          # [keys, heads, d]
+            for h in range(4):
+                v = seen[:, h // 2]
+                up, down = np.isposinf(v).any(0), np.isneginf(v).any(0)
+                got = o[k, h]
+                assert np.isposinf(got[up & ~down]).all() and np.isneginf(got[down & ~up]).all() and np.isnan(got[up & down]).all()
+                assert np.isfinite(got[~up & ~down]).all()
+            k += 1
+    assert k == len(o) and not torch.isnan(lse).any()
 
 
 def test_the_largest_numbers_of_the_8_bit_cache():
