@@ -563,6 +563,85 @@ hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_ba
                                   size_t workspace_bytes, void* stream);
 
 /*
+ * ---- Linear attention with a decay for each head ----
+ * For models that put such layers between those of softmax attention, over the same packs and the same shares of the heads.  Per sequence and KV
+ * head, with g_t <= 0 the logarithm of a token's decay and a state S of head_dim x head_dim (rows: columns of k, columns: columns of v):
+ *     S_t = exp(g_t) S_{t-1} + k_t v_t^T,    o_t = scale S_t^T q_t   for each query head of the group,
+ * S_0 the sequence's initial state, or zero.  Packed sequences do not see each other.  Three calls: the chunked form for prompts and training
+ * packs, its gradients, and the recurrent form for one token per sequence.
+ *
+ * The rows of a call: as hspmd_kv_batch, sequence s brings the packed rows cu_rows[s] .. cu_rows[s+1]-1, none among them.  cu_rows and the slots are
+ * DEVICE memory, read when the kernels run (a captured graph replays with what it finds there) and never trusted: rows are clamped to
+ * 0 .. total_rows, slots outside a pool are not followed.  Rows behind cu_rows[num_seqs] are left as they were, in every output.
+ */
+typedef struct {
+    const int32_t* cu_rows;        /* device, [num_seqs + 1], non-decreasing; hspmd_linear_attn_step does not look at it                  */
+    const int32_t* initial_slots;  /* device, [num_seqs]: the slot of a sequence's initial state, negative: it starts from zeros.  NULL: slot s   */
+    const int32_t* final_slots;    /* device, [num_seqs]: where its final state goes, negative: nowhere.  NULL: slot s                     */
+    int32_t num_seqs;              /* >= 0; num_seqs * local_kv_heads at most 2^22                                                        */
+    int32_t total_rows;            /* rows of the call's tensors, 0 .. 2^25; total_rows * local_q_heads at most 2^25                       */
+    int32_t max_rows;              /* the most rows of a sequence (0: unknown).  Chooses how sequences are cut; longer ones are computed all the same, slower */
+    int32_t local_q_heads, local_kv_heads, head_dim;
+} hspmd_linear_batch;
+
+/* A pool of states: fp32, slot i, head h at data + i * slot_stride + h * head_dim^2. */
+typedef struct {
+    float* data;                   /* device, 16-byte aligned */
+    int64_t slot_stride;           /* elements, a multiple of 4, >= local_kv_heads * head_dim^2 */
+    int32_t num_slots;             /* >= 1; >= num_seqs where the batch has no slots for it */
+} hspmd_linear_states;
+
+/*
+ * o of all rows, and the final states.
+ *   q, k, v    bf16 [total_rows, heads, head_dim], 16-byte aligned; token strides in elements, multiples of 8, >= heads*head_dim, at most 2^24
+ *   log_decay  fp32, g of row t and KV head h at t * decay_token_stride + h: >= local_kv_heads, or 0 for one decay per KV head.  -infinity and
+ *              anything below -110 forgets all; values above 0 are taken as they are, as long as no product of them along 64 rows overflows
+ *   scale      as softmax_scale of hspmd_attn_varlen_fwd
+ *   initial    NULL: every sequence starts from zeros.  A slot outside the pool gives NaN to its sequence's rows
+ *   final      NULL: not kept.  A slot outside the pool is not written.  No two sequences may name the same slot.  The pool may be the initial one: a sequence may
+ *              write the slot that it read; one that another sequence of the call reads must not be written.  A sequence without rows passes its state on
+ *   o          bf16 [total_rows, local_q_heads, head_dim], contiguous, written
+ *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 0) bytes, 16-byte aligned; nothing in it outlives the call
+ * States are fp32 throughout; where they, and the weights of pairs, enter a product on the matrix cores they do so in two bf16 parts, which leaves an error of
+ * 2^-17 of each factor.  No atomics: results are run-to-run bit-identical.  Rows are not changed by later ones of their sequence, whatever
+ * those hold; an infinity or NaN in a row of k or v is in the state from there on and may make all of it NaN.
+ */
+size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward);   /* 0 on bad arguments, and where none is needed */
+hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
+                                   int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,
+                                   const hspmd_linear_states* initial, const hspmd_linear_states* final, void* o, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * The gradients, from the forward's inputs alone (the states are computed again).  final_slots are not looked at.
+ *   d_o        bf16 [total_rows, local_q_heads, head_dim], contiguous
+ *   initial    as in the forward
+ *   d_final    fp32 [num_seqs, local_kv_heads, head_dim, head_dim], 16-byte aligned: the gradient of the sequences' final states; NULL: zeros
+ *   dq, dk, dv as in hspmd_attn_varlen_bwd: contiguous, bf16 or fp32; dk, dv summed over the group
+ *   d_log_decay  fp32, written; NULL: not wanted.  [total_rows, local_kv_heads], or, with decay_token_stride 0, [local_kv_heads]: the sum over all rows
+ *   d_initial  like d_final, written: the gradient of the sequences' initial states (by sequence: where several share a slot the caller adds
+ *              them up); NULL: not wanted.  Not d_final itself: other workgroups still read it
+ *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 1) bytes, 16-byte aligned
+ */
+hspmd_status hspmd_linear_attn_bwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
+                                   const void* d_o, int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,
+                                   const hspmd_linear_states* initial, const float* d_final, void* dq, void* dk, void* dv,
+                                   hspmd_grad_dtype grad_dtype, float* d_log_decay, float* d_initial, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
+/*
+ * One row per sequence (total_rows == num_seqs), arguments as in hspmd_linear_attn_fwd; all arithmetic in fp32, o rounded once.  A row whose slots
+ * are negative is computed from a state of zeros and leaves nothing behind, as the rows of a batch that is padded to a fixed size may be.
+ *
+ * Errors of these calls: INVALID_ARG for NULL / misaligned pointers, bad strides or counts; UNSUPPORTED for a head_dim outside the supported set
+ * or an unknown dtype; WORKSPACE_TOO_SMALL.  Nothing is launched on error.  num_seqs == 0 returns OK (a fixed decay's gradient is then zero); total_rows == 0
+ * passes states on.  Per-kernel timing (hspmd_profile_enable) does not record them.
+ */
+hspmd_status hspmd_linear_attn_step(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
+                                    int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,
+                                    const hspmd_linear_states* initial, const hspmd_linear_states* final, void* o, void* stream);
+
+/*
  * Per-kernel timing for measurement (the evidence the kernels are tuned against; not part of
  * the paper's method).  While enabled, every kernel launch made by forward / backward on the
  * calling process is bracketed by a pair of HIP events recorded on the launch stream.

@@ -13,4 +13,5 @@ from .binding import (  # noqa: F401
     attn_varlen_bwd_static_ws, STATIC_WORKSPACE_BYTES, probe_mfma_rate, PROBE_MODES,
     RopeAxes, rope_axes_qk, CACHE_BF16, CACHE_E4M3, KVCache, KVBatch, kv_cache_row, kv_cache_write, kv_cache_read,
     attn_paged_workspace_bytes, attn_paged_fwd,
+    LinearBatch, linear_attn_workspace_bytes, linear_attn_fwd, linear_attn_bwd, linear_attn_step,
 )

@@ -52,6 +52,16 @@ class _KVBatchArgs(ctypes.Structure):
                 ("max_rows", ctypes.c_int32)]
 
 
+class _LinearBatchArgs(ctypes.Structure):
+    _fields_ = [("cu_rows", ctypes.c_void_p), ("initial_slots", ctypes.c_void_p), ("final_slots", ctypes.c_void_p),
+                ("num_seqs", ctypes.c_int32), ("total_rows", ctypes.c_int32), ("max_rows", ctypes.c_int32),
+                ("local_q_heads", ctypes.c_int32), ("local_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class _LinearStatesArgs(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("slot_stride", ctypes.c_int64), ("num_slots", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -162,6 +172,17 @@ def load_library():
     lib.hspmd_attn_paged_workspace_bytes.argtypes = [cache_p, batch_p, i32]
     lib.hspmd_attn_paged_fwd.restype = ctypes.c_int
     lib.hspmd_attn_paged_fwd.argtypes = [cache_p, batch_p, vp, i64, i32, ctypes.c_float, vp, vp, vp, ctypes.c_size_t, vp]
+    linear_p, states_p = ctypes.POINTER(_LinearBatchArgs), ctypes.POINTER(_LinearStatesArgs)
+    rows = [vp, vp, vp, vp]                                  # q, k, v, log_decay
+    strides = [i64, i64, i64, ctypes.c_float]
+    lib.hspmd_linear_attn_workspace_bytes.restype = ctypes.c_size_t
+    lib.hspmd_linear_attn_workspace_bytes.argtypes = [linear_p, i32]
+    lib.hspmd_linear_attn_fwd.restype = ctypes.c_int
+    lib.hspmd_linear_attn_fwd.argtypes = [linear_p, *rows, *strides, states_p, states_p, vp, vp, ctypes.c_size_t, vp]
+    lib.hspmd_linear_attn_bwd.restype = ctypes.c_int
+    lib.hspmd_linear_attn_bwd.argtypes = [linear_p, *rows, vp, *strides, states_p, vp, vp, vp, vp, ctypes.c_int, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.hspmd_linear_attn_step.restype = ctypes.c_int
+    lib.hspmd_linear_attn_step.argtypes = [linear_p, *rows, *strides, states_p, states_p, vp, vp]
     lib.hspmd_probe_scratch_bytes.restype = ctypes.c_size_t
     lib.hspmd_probe_scratch_bytes.argtypes = []
     lib.hspmd_probe_mfma_tflops.restype = ctypes.c_int
@@ -769,3 +790,143 @@ def attn_paged_fwd(cache: KVCache, batch: KVBatch, q, o, lse, workspace, softmax
     handle = _stream_of(q.get_device(), devices, stream)
     _check(load_library().hspmd_attn_paged_fwd(cache._ref, batch._with_rows(T), q.data_ptr(), stride, hq, softmax_scale, o.data_ptr(), lse_ptr,
                                                workspace.data_ptr(), workspace.numel() * workspace.element_size(), handle))
+
+
+# ------------------------------------------------- linear attention with a decay for each head
+class LinearBatch:
+    """The rows of a call and where its states are: device int32 cu_rows [num_seqs + 1] (None for linear_attn_step: one row per sequence),
+    initial_slots, final_slots [num_seqs] (None: slot s for sequence s; negative entries: no state); max_rows: the most rows of a
+    sequence (0: unknown).  The calls read the tensors when their kernels run."""
+
+    def __init__(self, cu_rows=None, max_rows: int = 0, initial_slots=None, final_slots=None):
+        import torch
+        self.tensors = tuple(x for x in (cu_rows, initial_slots, final_slots) if x is not None)   # (kept alive)
+        if any(x.dtype is not torch.int32 or not x.is_contiguous() or x.dim() != 1 for x in self.tensors):
+            raise _bad("cu_rows and the slots have to be contiguous int32 tensors of one dimension")
+        self.num_seqs = None
+        if cu_rows is not None:
+            self.num_seqs = cu_rows.numel() - 1
+            if self.num_seqs < 0:
+                raise _bad("cu_rows has to have one entry more than there are sequences")
+            _count(self.num_seqs, "num_seqs")
+        for x in (initial_slots, final_slots):
+            if x is not None:
+                if self.num_seqs is not None and x.numel() != self.num_seqs:
+                    raise _bad("the slots have to have one entry per sequence")
+                self.num_seqs = x.numel()
+        self.max_rows = _count(max_rows, "max_rows")
+        self.has_cu = cu_rows is not None
+        self.devices = tuple(x.get_device() for x in self.tensors)
+        where = lambda x: None if x is None else x.data_ptr() or None
+        self._pointers = (where(cu_rows), where(initial_slots), where(final_slots))
+
+    def _args(self, rows: int, q_heads: int, kv_heads: int, head_dim: int):
+        n = rows if self.num_seqs is None else self.num_seqs
+        return ctypes.byref(_LinearBatchArgs(*self._pointers, n, rows, self.max_rows, q_heads, kv_heads, head_dim))
+
+
+def _linear_states(x, kv_heads: int, d: int, what: str, devices: list):
+    """The pool x, fp32 [num_slots, kv_heads, d, d] with contiguous slots, as the library takes it; None: none."""
+    import torch
+    if x is None:
+        return None
+    if x.dtype is not torch.float32 or x.dim() != 4 or tuple(x.shape[1:]) != (kv_heads, d, d):
+        raise _bad(f"{what} has to be [num_slots, {kv_heads}, {d}, {d}] of torch.float32")
+    if any(a != b and n > 1 for a, b, n in zip(x.stride()[1:], (d * d, d, 1), x.shape[1:])):
+        raise _bad(f"{what}: the heads, rows and columns of a slot have to be contiguous")
+    devices.append(x.get_device())
+    return ctypes.byref(_LinearStatesArgs(x.data_ptr(), x.stride(0) if x.shape[0] > 1 else kv_heads * d * d, _count(x.shape[0], "num_slots")))
+
+
+def _linear_dense(x, shape, dtype, what: str, devices: list):
+    if x is None:
+        return None
+    if tuple(x.shape) != tuple(shape) or x.dtype is not dtype or not x.is_contiguous():
+        raise _bad(f"{what} has to be a contiguous tensor {list(shape)} of {dtype}")
+    devices.append(x.get_device())
+    return x.data_ptr()
+
+
+def _linear_rows(batch: LinearBatch, q, k, v, log_decay):
+    """(shape, arguments q .. log_decay, strides, devices) of a call's rows."""
+    import torch
+    if q.dim() != 3 or k.dim() != 3:
+        raise _bad("q, k, v have to be [T, heads, head_dim]")
+    T, hq, d = q.shape
+    hkv, bf16 = k.shape[1], torch.bfloat16
+    qs, ks = _rows_stride(q, hq, d, bf16, "q", T), _rows_stride(k, hkv, d, bf16, "k", T)
+    if _rows_stride(v, hkv, d, bf16, "v", T) != ks:
+        raise _bad("k and v have to have the same token stride")
+    fixed = log_decay.dim() == 1
+    if log_decay.dtype is not torch.float32 or tuple(log_decay.shape) != ((hkv,) if fixed else (T, hkv)) or log_decay.stride(-1) != 1 and hkv > 1:
+        raise _bad("log_decay has to be [T, kv_heads] or [kv_heads] of torch.float32 with contiguous heads")
+    gs = 0 if fixed else log_decay.stride(0) if T > 1 else hkv
+    devices = [k.get_device(), v.get_device(), log_decay.get_device(), *batch.devices]
+    return (T, hq, hkv, d), (q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr()), (qs, ks, gs), devices
+
+
+def linear_attn_workspace_bytes(batch: LinearBatch, total_rows: int, q_heads: int, kv_heads: int, head_dim: int, backward: bool = False) -> int:
+    """Bytes of workspace that linear_attn_fwd (or, backward, linear_attn_bwd) takes; 0 where none is needed."""
+    lib, counts = load_library(), [_count(x, "a count") for x in (total_rows, q_heads, kv_heads, head_dim)]
+    # (the library answers 0 to what it refuses as well: its backward takes some wherever there is a sequence)
+    if int(lib.hspmd_linear_attn_workspace_bytes(batch._args(*counts), 1)) == 0 and (batch.num_seqs or counts[0]):
+        raise HspmdError(1, lib.hspmd_last_error().decode())
+    return int(lib.hspmd_linear_attn_workspace_bytes(batch._args(*counts), 1 if backward else 0))
+
+
+def linear_attn_fwd(batch: LinearBatch, q, k, v, log_decay, o, workspace, initial=None, final=None, scale: float = 0.0, stream=None) -> None:
+    """o (bf16 like q, contiguous) of the packed rows q [T, q_heads, d], k, v [T, kv_heads, d] with log decays fp32 [T, kv_heads], or [kv_heads] where
+    they are fixed; initial, final: pools of states, fp32 [num_slots, kv_heads, d, d], the latter written; workspace: any device
+    tensor of linear_attn_workspace_bytes(...) bytes, None where that is 0."""
+    import torch
+    if not batch.has_cu:
+        raise _bad("the batch has no cu_rows")
+    (T, hq, hkv, d), rows, strides, devices = _linear_rows(batch, q, k, v, log_decay)
+    before, after = _linear_states(initial, hkv, d, "initial", devices), _linear_states(final, hkv, d, "final", devices)
+    o_ptr = _linear_dense(o, (T, hq, d), torch.bfloat16, "o", devices)
+    ws, size = _linear_workspace(workspace, devices)
+    handle = _stream_of(q.get_device(), devices, stream)
+    _check(load_library().hspmd_linear_attn_fwd(batch._args(T, hq, hkv, d), *rows, *strides, scale, before, after, o_ptr, ws, size, handle))
+
+
+def _linear_workspace(workspace, devices: list):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous():
+        raise _bad("the workspace has to be contiguous")
+    devices.append(workspace.get_device())
+    return workspace.data_ptr() or None, workspace.numel() * workspace.element_size()
+
+
+def linear_attn_bwd(batch: LinearBatch, q, k, v, log_decay, d_o, dq, dk, dv, workspace, initial=None, d_final=None, d_log_decay=None,
+                    d_initial=None, scale: float = 0.0, stream=None) -> None:
+    """dq, dk, dv (all bf16 or all fp32, contiguous), d_log_decay (fp32, log_decay's shape; [kv_heads] where its token stride is 0) and d_initial
+    (fp32 [num_seqs, kv_heads, d, d]) from d_o and d_final (like d_initial); the last three may be None."""
+    import torch
+    if not batch.has_cu:
+        raise _bad("the batch has no cu_rows")
+    (T, hq, hkv, d), rows, strides, devices = _linear_rows(batch, q, k, v, log_decay)
+    f32, n = torch.float32, batch.num_seqs
+    before = _linear_states(initial, hkv, d, "initial", devices)
+    do_ptr = _linear_dense(d_o, (T, hq, d), torch.bfloat16, "d_o", devices)
+    t = dq.dtype
+    if t is not torch.bfloat16 and t is not f32:
+        raise _bad("the gradients have to be bf16 or fp32")
+    grads = [_linear_dense(x, (T, h, d), t, name, devices) for x, h, name in ((dq, hq, "dq"), (dk, hkv, "dk"), (dv, hkv, "dv"))]
+    dg_ptr = _linear_dense(d_log_decay, (T, hkv) if strides[2] else (hkv,), f32, "d_log_decay", devices)
+    end_ptr, start_ptr = (_linear_dense(x, (n, hkv, d, d), f32, name, devices) for x, name in ((d_final, "d_final"), (d_initial, "d_initial")))
+    ws, size = _linear_workspace(workspace, devices)
+    handle = _stream_of(q.get_device(), devices, stream)
+    _check(load_library().hspmd_linear_attn_bwd(batch._args(T, hq, hkv, d), *rows, do_ptr, *strides, scale, before, end_ptr, *grads,
+                                                GRAD_F32 if t is f32 else GRAD_BF16, dg_ptr, start_ptr, ws, size, handle))
+
+
+def linear_attn_step(batch: LinearBatch, q, k, v, log_decay, o, initial=None, final=None, scale: float = 0.0, stream=None) -> None:
+    """The same for one row per sequence: o of the rows q [num_seqs, q_heads, d], states read from `initial` and written to `final` (which may be one
+    pool) at the batch's slots.  The batch's cu_rows are not looked at."""
+    import torch
+    (T, hq, hkv, d), rows, strides, devices = _linear_rows(batch, q, k, v, log_decay)
+    before, after = _linear_states(initial, hkv, d, "initial", devices), _linear_states(final, hkv, d, "final", devices)
+    o_ptr = _linear_dense(o, (T, hq, d), torch.bfloat16, "o", devices)
+    handle = _stream_of(q.get_device(), devices, stream)
+    _check(load_library().hspmd_linear_attn_step(batch._args(T, hq, hkv, d), *rows, *strides, scale, before, after, o_ptr, handle))

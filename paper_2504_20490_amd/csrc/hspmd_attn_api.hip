@@ -15,6 +15,7 @@
 
 #include "../../include/hspmd_attn.h"
 #include "kernels.hpp"
+#include "linear.hpp"
 #include "paged.hpp"
 #include "schedule.hpp"
 
@@ -1346,6 +1347,208 @@ hspmd_status hspmd_attn_paged_fwd(const hspmd_kv_cache* cache, const hspmd_kv_ba
     p.few_limit = sizes.few_limit;
     const hipError_t e = hspmd::launch_paged_attn(p, sizes, cache->dtype == HSPMD_CACHE_E4M3, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return fail_hip(e, "paged attention launch");
+    return HSPMD_OK;
+}
+
+// ---- linear attention -------------------------------------------------------------------------------------------
+
+// States of a call: a grid holds fewer than 2^32 threads, and the backward has three workgroups of 256 for each
+static constexpr int64_t kMaxStates = (int64_t)1 << 22, kMaxLinearStride = (int64_t)1 << 24;
+
+static hspmd_status check_linear_batch(const hspmd_linear_batch* batch) {
+    if (!batch) return fail(HSPMD_ERR_INVALID_ARG, "batch is NULL");
+    if (!supported_head_dim(batch->head_dim)) return fail(HSPMD_ERR_UNSUPPORTED, "head_dim must be a multiple of 8 between 8 and 128");
+    if (batch->local_kv_heads < 1 || batch->local_kv_heads > (1 << 16)) return fail(HSPMD_ERR_INVALID_ARG, "local_kv_heads must be 1 .. 65536");
+    if (batch->local_q_heads < 1 || batch->local_q_heads % batch->local_kv_heads != 0 || batch->local_q_heads > (1 << 16))
+        return fail(HSPMD_ERR_INVALID_ARG, "local_q_heads must be a positive multiple of local_kv_heads, at most 65536");
+    if (batch->num_seqs < 0 || batch->max_rows < 0) return fail(HSPMD_ERR_INVALID_ARG, "negative count in the batch");
+    if ((int64_t)batch->num_seqs * batch->local_kv_heads > kMaxStates) return fail(HSPMD_ERR_INVALID_ARG, "num_seqs * local_kv_heads must not exceed 2^22");
+    if (batch->total_rows < 0 || batch->total_rows > kMaxRows) return fail(HSPMD_ERR_INVALID_ARG, "total_rows must be 0 .. 2^25");
+    if ((int64_t)batch->total_rows * batch->local_q_heads > kMaxRowHeads)
+        return fail(HSPMD_ERR_INVALID_ARG, "total_rows * local_q_heads must not exceed 2^25");
+    return HSPMD_OK;
+}
+
+static hspmd_status check_linear_stride(int64_t stride, int64_t heads, int32_t head_dim, const char* what) {
+    if (stride > kMaxLinearStride) return fail(HSPMD_ERR_INVALID_ARG, std::string(what) + " must not exceed 2^24");
+    return check_stride(stride, heads, head_dim, what);
+}
+
+// rows of q, k, v and the decays, where there are rows
+static hspmd_status check_linear_rows(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
+                                      int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride) {
+    if (!q || !k || !v || !log_decay) return fail(HSPMD_ERR_INVALID_ARG, "null tensor pointer");
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v)) return fail(HSPMD_ERR_INVALID_ARG, "q, k, v must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(log_decay) & 3u) return fail(HSPMD_ERR_INVALID_ARG, "log_decay must be 4-byte aligned");
+    if (hspmd_status rc = check_linear_stride(q_token_stride, batch->local_q_heads, batch->head_dim, "q_token_stride")) return rc;
+    if (hspmd_status rc = check_linear_stride(kv_token_stride, batch->local_kv_heads, batch->head_dim, "kv_token_stride")) return rc;
+    if (decay_token_stride != 0 && decay_token_stride < batch->local_kv_heads)
+        return fail(HSPMD_ERR_INVALID_ARG, "decay_token_stride must be 0 or >= local_kv_heads");
+    return HSPMD_OK;
+}
+
+static hspmd_status check_linear_states(const hspmd_linear_batch* batch, const hspmd_linear_states* states, const int32_t* slots, const char* what,
+                                        hspmd::LinearStates* out) {
+    *out = hspmd::LinearStates{};
+    if (!states) return HSPMD_OK;
+    const std::string name = what;
+    if (!states->data || !aligned16(states->data)) return fail(HSPMD_ERR_INVALID_ARG, name + ": data must be non-NULL and 16-byte aligned");
+    if (states->num_slots < 1) return fail(HSPMD_ERR_INVALID_ARG, name + ": the pool has no slot");
+    if (states->slot_stride < (int64_t)batch->local_kv_heads * batch->head_dim * batch->head_dim || states->slot_stride % 4 != 0)
+        return fail(HSPMD_ERR_INVALID_ARG, name + ": slot_stride must be a multiple of 4 and hold the heads' states");
+    if (!slots && states->num_slots < batch->num_seqs) return fail(HSPMD_ERR_INVALID_ARG, name + ": fewer slots than sequences, and none are named");
+    if (reinterpret_cast<uintptr_t>(slots) & 3u) return fail(HSPMD_ERR_INVALID_ARG, name + ": the slots must be 4-byte aligned");
+    *out = hspmd::LinearStates{states->data, slots, states->slot_stride, states->num_slots};
+    return HSPMD_OK;
+}
+
+// shape and workspace of a chunked call
+static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward, void* workspace, size_t workspace_bytes, hspmd::LinearParams* p) {
+    const hspmd::LinearSizes sizes = hspmd::linear_sizes(batch->total_rows, batch->num_seqs, batch->max_rows, batch->local_q_heads, batch->local_kv_heads,
+                                                         batch->head_dim, backward);
+    const size_t need = sizes.total_bytes(backward);
+    if (need > 0 && (!workspace || !aligned16(workspace))) return fail(HSPMD_ERR_INVALID_ARG, "workspace must be non-NULL and 16-byte aligned");
+    if (workspace_bytes < need) return fail(HSPMD_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than hspmd_linear_attn_workspace_bytes");
+    p->shape = hspmd::LinearShape{batch->cu_rows, batch->num_seqs, batch->total_rows, batch->local_q_heads, batch->local_kv_heads,
+                                  batch->local_q_heads / batch->local_kv_heads, batch->head_dim, sizes.seg_rows, (int32_t)sizes.slots,
+                                  (int32_t)sizes.entries, (int32_t)sizes.windows};
+    char* at = static_cast<char*>(workspace);
+    const auto take = [&at](size_t bytes) {
+        float* const r = reinterpret_cast<float*>(at);
+        at += bytes;
+        return r;
+    };
+    p->states = take(sizes.state_bytes);
+    p->seg_decay = take(sizes.decay_bytes);
+    if (backward) {
+        p->d_states = take(sizes.state_bytes);
+        p->q_near = take(sizes.q_row_bytes);
+        p->q_far = take(sizes.q_row_bytes);
+        p->k_near = take(sizes.k_row_bytes);
+        p->k_far = take(sizes.k_row_bytes);
+        p->across = take(sizes.slot_bytes);
+        p->decay_sums = take(sizes.slot_bytes);
+    }
+    return HSPMD_OK;
+}
+
+size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward) {
+    if (check_linear_batch(batch) || batch->num_seqs == 0) return 0;
+    return hspmd::linear_sizes(batch->total_rows, batch->num_seqs, batch->max_rows, batch->local_q_heads, batch->local_kv_heads, batch->head_dim,
+                               backward != 0).total_bytes(backward != 0);
+}
+
+static hspmd_status check_linear_cu(const hspmd_linear_batch* batch) {
+    if (!batch->cu_rows || (reinterpret_cast<uintptr_t>(batch->cu_rows) & 3u)) return fail(HSPMD_ERR_INVALID_ARG, "cu_rows must be non-NULL and 4-byte aligned");
+    return HSPMD_OK;
+}
+
+hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
+                                   int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,
+                                   const hspmd_linear_states* initial, const hspmd_linear_states* final, void* o, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    hspmd::LinearParams p{};
+    if (hspmd_status rc = check_linear_batch(batch)) return rc;
+    if (hspmd_status rc = resolve_scale(scale, batch->head_dim, &p.scale)) return rc;
+    if (hspmd_status rc = check_linear_states(batch, initial, batch->initial_slots, "initial", &p.initial)) return rc;
+    if (hspmd_status rc = check_linear_states(batch, final, batch->final_slots, "final", &p.final)) return rc;
+    if (batch->num_seqs == 0) return HSPMD_OK;
+    if (hspmd_status rc = check_linear_cu(batch)) return rc;
+    if (batch->total_rows > 0) {
+        if (hspmd_status rc = check_linear_rows(batch, q, k, v, log_decay, q_token_stride, kv_token_stride, decay_token_stride)) return rc;
+        if (!o || !aligned16(o)) return fail(HSPMD_ERR_INVALID_ARG, "o must be non-NULL and 16-byte aligned");
+    } else if (!final) {
+        return HSPMD_OK;
+    }
+    if (hspmd_status rc = linear_shape(batch, false, workspace, workspace_bytes, &p)) return rc;
+    p.q = static_cast<const uint16_t*>(q);
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.log_decay = log_decay;
+    p.q_stride = q_token_stride;
+    p.kv_stride = kv_token_stride;
+    p.decay_stride = decay_token_stride;
+    p.o = o;
+    const hipError_t e = hspmd::launch_linear_fwd(p, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip(e, "linear attention launch (forward)");
+    return HSPMD_OK;
+}
+
+hspmd_status hspmd_linear_attn_bwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
+                                   const void* d_o, int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,
+                                   const hspmd_linear_states* initial, const float* d_final, void* dq, void* dk, void* dv,
+                                   hspmd_grad_dtype grad_dtype, float* d_log_decay, float* d_initial, void* workspace,
+                                   size_t workspace_bytes, void* stream) {
+    hspmd::LinearParams p{};
+    if (grad_dtype != HSPMD_GRAD_BF16 && grad_dtype != HSPMD_GRAD_F32) return fail(HSPMD_ERR_UNSUPPORTED, "grad_dtype must be bf16 or fp32");
+    if (hspmd_status rc = check_linear_batch(batch)) return rc;
+    if (hspmd_status rc = resolve_scale(scale, batch->head_dim, &p.scale)) return rc;
+    if (hspmd_status rc = check_linear_states(batch, initial, batch->initial_slots, "initial", &p.initial)) return rc;
+    if (!aligned16(d_final) || !aligned16(d_initial)) return fail(HSPMD_ERR_INVALID_ARG, "d_final and d_initial must be 16-byte aligned");
+    if (reinterpret_cast<uintptr_t>(d_log_decay) & 3u) return fail(HSPMD_ERR_INVALID_ARG, "d_log_decay must be 4-byte aligned");
+    const bool fixed_sum = d_log_decay && decay_token_stride == 0;     // written whether there are rows or not
+    if (batch->num_seqs > 0) {
+        if (hspmd_status rc = check_linear_cu(batch)) return rc;
+        if (batch->total_rows > 0) {
+            if (hspmd_status rc = check_linear_rows(batch, q, k, v, log_decay, q_token_stride, kv_token_stride, decay_token_stride)) return rc;
+            if (!d_o || !dq || !dk || !dv) return fail(HSPMD_ERR_INVALID_ARG, "null tensor pointer");
+            if (!aligned16(d_o) || !aligned16(dq) || !aligned16(dk) || !aligned16(dv))
+                return fail(HSPMD_ERR_INVALID_ARG, "d_o, dq, dk, dv must be 16-byte aligned");
+        }
+        if (batch->total_rows > 0 || d_initial || fixed_sum) {
+            if (hspmd_status rc = linear_shape(batch, true, workspace, workspace_bytes, &p)) return rc;
+        }
+    }
+    if (!fixed_sum && (batch->num_seqs == 0 || (batch->total_rows == 0 && !d_initial))) return HSPMD_OK;
+    p.shape.kv_heads = batch->local_kv_heads;
+    p.q = static_cast<const uint16_t*>(q);
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.d_o = static_cast<const uint16_t*>(d_o);
+    p.log_decay = log_decay;
+    p.q_stride = q_token_stride;
+    p.kv_stride = kv_token_stride;
+    p.do_stride = (int64_t)batch->local_q_heads * batch->head_dim;
+    p.decay_stride = decay_token_stride;
+    p.final = hspmd::LinearStates{const_cast<float*>(d_final), nullptr, (int64_t)batch->local_kv_heads * batch->head_dim * batch->head_dim, batch->num_seqs};
+    p.dq = dq;
+    p.dk = dk;
+    p.dv = dv;
+    p.grad_f32 = grad_dtype == HSPMD_GRAD_F32;
+    p.d_log_decay = d_log_decay;
+    p.d_initial = d_initial;
+    const hipError_t e = hspmd::launch_linear_bwd(p, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip(e, "linear attention launch (backward)");
+    return HSPMD_OK;
+}
+
+hspmd_status hspmd_linear_attn_step(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
+                                    int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,
+                                    const hspmd_linear_states* initial, const hspmd_linear_states* final, void* o, void* stream) {
+    hspmd::LinearStepParams p{};
+    if (hspmd_status rc = check_linear_batch(batch)) return rc;
+    if (batch->total_rows != batch->num_seqs) return fail(HSPMD_ERR_INVALID_ARG, "a step has one row per sequence");
+    if (hspmd_status rc = resolve_scale(scale, batch->head_dim, &p.scale)) return rc;
+    if (hspmd_status rc = check_linear_states(batch, initial, batch->initial_slots, "initial", &p.initial)) return rc;
+    if (hspmd_status rc = check_linear_states(batch, final, batch->final_slots, "final", &p.final)) return rc;
+    if (batch->num_seqs == 0) return HSPMD_OK;
+    if (hspmd_status rc = check_linear_rows(batch, q, k, v, log_decay, q_token_stride, kv_token_stride, decay_token_stride)) return rc;
+    if (!o || !aligned16(o)) return fail(HSPMD_ERR_INVALID_ARG, "o must be non-NULL and 16-byte aligned");
+    p.q = static_cast<const uint16_t*>(q);
+    p.k = static_cast<const uint16_t*>(k);
+    p.v = static_cast<const uint16_t*>(v);
+    p.log_decay = log_decay;
+    p.q_stride = q_token_stride;
+    p.kv_stride = kv_token_stride;
+    p.decay_stride = decay_token_stride;
+    p.o = static_cast<uint16_t*>(o);
+    p.num_seqs = batch->num_seqs;
+    p.q_heads = batch->local_q_heads;
+    p.kv_heads = batch->local_kv_heads;
+    p.group = batch->local_q_heads / batch->local_kv_heads;
+    p.head_dim = batch->head_dim;
+    const hipError_t e = hspmd::launch_linear_step(p, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return fail_hip(e, "linear attention launch (step)");
     return HSPMD_OK;
 }
 

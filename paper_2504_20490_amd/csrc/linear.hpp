@@ -1,0 +1,83 @@
+// Kernel parameter blocks and host-callable launchers of the linear attention (internal to the library).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/hspmd_attn.h"
+#include "linear_index.hpp"
+
+namespace hspmd {
+
+// The rows of a call and what they are cut into
+struct LinearShape {
+    const int32_t* cu_rows;
+    int32_t num_seqs, total_rows;
+    int32_t q_heads, kv_heads, group, head_dim;
+    int32_t seg_rows;              // 0: every sequence is one segment, slot = sequence
+    int32_t slots, entries, windows;
+};
+
+// A pool of states, or one state per sequence
+struct LinearStates {
+    float* data;                   // NULL: none
+    const int32_t* slots;          // NULL: sequence s has slot s
+    int64_t slot_stride;
+    int32_t num_slots;
+};
+
+struct LinearParams {
+    LinearShape shape;
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    const uint16_t* d_o;           // backward only
+    const float* log_decay;
+    int64_t q_stride, kv_stride, do_stride, decay_stride;
+    float scale;
+    LinearStates initial, final;   // backward: `final` is the gradient that comes in (read)
+    void* o;                       // forward: bf16
+    void* dq;
+    void* dk;
+    void* dv;
+    int32_t grad_f32;
+    float* d_initial;              // may be NULL
+    float* d_log_decay;            // may be NULL
+    // workspace
+    float* states;                 // [entries][kv_heads][d][d]: the state at a segment's start
+    float* d_states;               // its gradient at a segment's end
+    float* seg_decay;              // [entries][kv_heads]: log2 of a segment's decay
+    float* q_near;                 // [q_heads][total_rows]: <q, dq> from the own chunk's other tokens ...
+    float* q_far;                  // ... and from before the chunk
+    float* k_near;                 // [kv_heads][total_rows], likewise
+    float* k_far;
+    float* across;                 // [slots][kv_heads]: <S, dS> at a segment's end
+    float* decay_sums;             // [slots][kv_heads]: a segment's share of a fixed decay's gradient
+};
+
+struct LinearSizes {
+    int32_t seg_rows;              // as in LinearShape
+    int64_t slots, entries, windows;
+    size_t state_bytes, decay_bytes, q_row_bytes, k_row_bytes, slot_bytes;
+    size_t total_bytes(bool backward) const {
+        return backward ? 2 * state_bytes + decay_bytes + 2 * q_row_bytes + 2 * k_row_bytes + 2 * slot_bytes : state_bytes + decay_bytes;
+    }
+};
+LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                         bool backward);
+hipError_t launch_linear_fwd(const LinearParams& p, hipStream_t stream);
+hipError_t launch_linear_bwd(const LinearParams& p, hipStream_t stream);
+
+struct LinearStepParams {
+    const uint16_t* q;
+    const uint16_t* k;
+    const uint16_t* v;
+    const float* log_decay;
+    int64_t q_stride, kv_stride, decay_stride;
+    float scale;
+    LinearStates initial, final;
+    uint16_t* o;
+    int32_t num_seqs, q_heads, kv_heads, group, head_dim;
+};
+hipError_t launch_linear_step(const LinearStepParams& p, hipStream_t stream);
+
+}  // namespace hspmd

@@ -1,0 +1,123 @@
+// Device code shared by the kernels of the linear attention: where a workgroup's tokens are, decays along a chunk, two-part operands.
+#pragma once
+#include "attn_device.hpp"
+#include "linear.hpp"
+
+namespace hspmd {
+
+// A decay of 2^-160 or less leaves nothing of any fp32 number, and infinities would make differences of sums NaN.
+constexpr float kForgetLog2 = -160.f;
+__device__ __forceinline__ float decay_log2(float log_decay) {
+    const float g = log_decay * kLog2e;
+    return g < kForgetLog2 ? kForgetLog2 : g;      // (NaN stays)
+}
+
+// inclusive sum over the lanes 0 .. lane of a wave, and over the lanes lane .. 63
+__device__ __forceinline__ float sum_up_to(float x, int lane) {
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) {
+        const float y = __shfl_up(x, step, 64);
+        x += lane >= step ? y : 0.f;
+    }
+    return x;
+}
+__device__ __forceinline__ float sum_from(float x, int lane) {
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) {
+        const float y = __shfl_down(x, step, 64);
+        x += lane + step < 64 ? y : 0.f;
+    }
+    return x;
+}
+__device__ __forceinline__ float wave_sum(float x) {
+#pragma unroll
+    for (int step = 1; step < 64; step *= 2) x += __shfl_xor(x, step, 64);
+    return x;
+}
+
+// A segment of a sequence: what a workgroup computes for one KV head.
+struct Segment {
+    int seq, index, count;   // of the sequence's segments
+    int start, rows;         // its first token in the packed tensors, tokens of it (0: an empty sequence)
+    int entry;               // first entry of the sequence (count > 1)
+};
+
+// by a whole wave, the same slot in every lane; false: the slot is none
+__device__ __forceinline__ bool find_segment(const LinearShape& p, int slot, Segment& out) {
+    const int lane = threadIdx.x & 63;
+    int seq = slot;
+    if (p.seg_rows > 0) {
+        // the last sequence whose first slot is not behind this one, 64 of them at a time
+        int lo = 0, n = p.num_seqs;
+        while (n > 1) {
+            const int step = (n + 63) / 64, at = lane * step;
+            bool before = false;
+            if (at < n) before = linear_first_slot(linear_rows(p.cu_rows[lo + at], 0, p.total_rows).start, lo + at, p.seg_rows) <= slot;
+            const uint64_t m = __ballot(before);
+            const int found = m ? 63 - __builtin_clzll(m) : 0;
+            lo += found * step;
+            n = min(step, n - found * step);
+        }
+        seq = lo;
+    }
+    const LinearRows r = linear_rows(p.cu_rows[seq], p.cu_rows[seq + 1], p.total_rows);
+    out.seq = seq;
+    out.count = 1;
+    out.index = 0;
+    out.start = r.start;
+    out.rows = r.n;
+    out.entry = 0;
+    if (p.seg_rows > 0) {
+        out.count = linear_segments(r.n, p.seg_rows);
+        out.index = slot - linear_first_slot(r.start, seq, p.seg_rows);
+        if (out.index < 0 || out.index >= out.count) return false;
+        out.entry = linear_first_entry(r.start, p.seg_rows);
+        out.start = r.start + out.index * p.seg_rows;
+        out.rows = min(r.n - out.index * p.seg_rows, p.seg_rows);
+    }
+    return true;
+}
+
+// A state of a pool: *exists = false where there is none (no pool, a negative slot: a state of zeros), NULL with *exists where the
+// slot is outside the pool (it is not followed)
+__device__ __forceinline__ float* state_of(const LinearStates& s, int seq, int head, int head_dim, bool* exists) {
+    *exists = false;
+    if (s.data == nullptr) return nullptr;
+    const int slot = s.slots ? s.slots[seq] : seq;
+    if (slot < 0) return nullptr;
+    *exists = true;
+    return slot < s.num_slots ? s.data + slot * s.slot_stride + (int64_t)head * head_dim * head_dim : nullptr;
+}
+
+// x as two bf16 values, the second the rest that the first leaves: 16 to 17 bits together (relative error up to 2^-17.5)
+struct TwoParts {
+    bf16x8 hi, lo;
+};
+__device__ __forceinline__ TwoParts two_parts(const float (&x)[8]) {
+    union { u32x4 u; bf16x8 v; } hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        hi.u[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+        const float a = __uint_as_float(hi.u[i] << 16), b = __uint_as_float(hi.u[i] & 0xffff0000u);
+        lo.u[i] = pack_bf16(x[2 * i] - a, x[2 * i + 1] - b);
+    }
+    return TwoParts{hi.v, lo.v};
+}
+
+// read_transposed_frag with the 16 columns of a lane group in another order: result row 16 g + 8 hi + 4 mid + low (MFMA M index) is column
+// 16 g + 8 mid + 4 hi + low.  An accumulator of a product with such an A operand then holds, in registers 8 t .. 8 t + 7 of
+// lane half hh, the columns 16 t + 8 hh + {0 .. 7}: the k order that an operand read along a row has.
+template <int D>
+__device__ __forceinline__ bf16x8 read_transposed_frag_in_order(const char* tile, int cb, int t, int lane) {
+    const int c16 = lane & 15, c = c16 & 3;
+    const int col = cb * 32 + (((lane >> 4) & 1) << 4) + (((c & 1) << 1 | c >> 1) << 2);
+    const int row = t * 16 + ((lane >> 5) << 2) + (c16 >> 2);
+    const s16x4 lo = lds_transpose_read(tile + tile_offset<D>(row, col));
+    const s16x4 hi = lds_transpose_read(tile + tile_offset<D>(row + 8, col));
+    union { struct { s16x4 a, b; } s; bf16x8 v; } u;
+    u.s.a = lo;
+    u.s.b = hi;
+    return u.v;
+}
+
+}  // namespace hspmd

@@ -1,0 +1,47 @@
+// Which tokens, states and workspace entries a workgroup of the linear attention takes.  Plain index arithmetic, usable on the host as
+// well: that every segment is taken once and that nothing leads out of the grid or the workspace is tested there.
+#pragma once
+#include <stdint.h>
+
+namespace hspmd {
+
+#if defined(__HIPCC__)
+#define HSPMD_LINEAR_INDEX __host__ __device__ __forceinline__ constexpr
+#else
+#define HSPMD_LINEAR_INDEX constexpr inline
+#endif
+
+constexpr int kLinearChunk = 64;     // tokens whose pairs are formed; states pass from chunk to chunk
+
+// A sequence's rows as the device array gives them, clamped to what there is.
+struct LinearRows {
+    int start, n;
+};
+HSPMD_LINEAR_INDEX LinearRows linear_rows(int cu, int cu_next, int total_rows) {
+    const int start = cu < 0 ? 0 : cu > total_rows ? total_rows : cu;
+    const int end = cu_next < start ? start : cu_next > total_rows ? total_rows : cu_next;
+    return LinearRows{start, end - start};
+}
+
+// A sequence is cut into segments of seg_rows tokens (a multiple of the chunk), at least one.  Segment b of sequence s is slot
+// start / seg_rows + s + b of the launch: the next sequence's first slot, (start + n) / seg_rows + s + 1, is never less than that of the
+// last segment plus one, so every slot is taken once at most, by a rule that needs no sums over the sequences.
+HSPMD_LINEAR_INDEX int linear_first_slot(int start, int seq, int seg_rows) { return start / seg_rows + seq; }
+HSPMD_LINEAR_INDEX int linear_segments(int n, int seg_rows) { return n <= seg_rows ? 1 : (n + seg_rows - 1) / seg_rows; }
+HSPMD_LINEAR_INDEX int64_t linear_slots(int64_t total_rows, int64_t num_seqs, int64_t seg_rows) { return total_rows / seg_rows + num_seqs; }
+
+// Sequences of several segments have an entry in the workspace for each (the state that reaches it): from 2 start / seg_rows on.  With n >
+// seg_rows the next sequence's first entry is at least 2 (segments - 1) further, which is never less than the number of segments.
+HSPMD_LINEAR_INDEX int linear_first_entry(int start, int seg_rows) { return (int)(2 * (int64_t)start / seg_rows); }
+HSPMD_LINEAR_INDEX int64_t linear_entries(int64_t total_rows, int64_t seg_rows) { return 2 * total_rows / seg_rows + 1; }
+
+// The sequence of several segments that starts in window w (tokens w * seg_rows .. + seg_rows - 1), if there is one, is the last that
+// starts there; windows are what the launch that passes states from segment to segment goes by.
+HSPMD_LINEAR_INDEX int64_t linear_windows(int64_t total_rows, int64_t seg_rows) { return total_rows / seg_rows + 1; }
+
+// Workgroups go to the 8 XCDs in turn; a range of consecutive items per XCD keeps the heads of a segment, which share lines of the decays
+// and the edges of rows, in one L2.  The grid is 8 * linear_share(items); items from `items` on are none.
+HSPMD_LINEAR_INDEX int64_t linear_share(int64_t items) { return (items + 7) / 8; }
+HSPMD_LINEAR_INDEX int64_t linear_item(int64_t block, int64_t items) { return block % 8 * linear_share(items) + block / 8; }
+
+}  // namespace hspmd
