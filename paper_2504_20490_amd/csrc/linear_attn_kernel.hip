@@ -51,14 +51,17 @@ struct TileLoad {
     static constexpr int kThreadsHere = D / 32 * 64, kRowsPerPass = kThreadsHere / (D / 8), kPasses = kLinearChunk / kRowsPerPass;
     u32x4 r[kPasses];
     __device__ __forceinline__ void issue(const uint16_t* first_row, int64_t stride, int rows, int head_dim) {
-        const int row = threadIdx.x / (D / 8), col = threadIdx.x % (D / 8) * 8;
+        const int row = threadIdx.x / (D / 8), col = threadIdx.x % (D / 8) * 8, there = col < head_dim ? rows : 0;
+        const uint32_t off = (uint32_t)(row * (int)stride + col) * 2u;
         const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(first_row), 0, 0x7fffffff, 0x00020000);
 #pragma unroll
-        for (int i = 0; i < kPasses; ++i) {
-            const int at = row + i * kRowsPerPass;
-            const uint32_t off = at < rows && col < head_dim ? (uint32_t)(at * (int)stride + col) * 2u : 0x80000000u;
-            r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off, 0, 0);
-        }
+        for (int i = 0; i < kPasses; ++i)
+            r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, row + i * kRowsPerPass < there ? off : 0x80000000u, i * kRowsPerPass * (int)stride * 2, 0);
+    }
+    // ends the life of what was put: a load that is not always made again would else keep its registers throughout the loop
+    __device__ __forceinline__ void drop() {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) r[i] = u32x4{};
     }
     __device__ __forceinline__ void put(char* tile) const {
         const int row = threadIdx.x / (D / 8), col = threadIdx.x % (D / 8) * 8;
@@ -132,34 +135,49 @@ struct State {
     }
 };
 
-// A hidden pair has the weight 0, and 0 times an infinity or NaN is NaN: such elements of the sources are left out of the product (set
-// to zero here) and added for the targets that see them, see add_not_finite.  true: there are none in the wave's columns, as hardly ever there are.
-__device__ __forceinline__ bool only_finite(const bf16x8 (&x)[4], bf16x8 (&finite)[4]) {
+// A hidden pair has the weight 0, and 0 times an infinity or NaN is NaN: sources that hold one are left out of the products, element by element, and
+// added for the targets that see them.
+__device__ __forceinline__ bool all_finite(const bf16x8 (&x)[4]) {
     typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
     u16x2 most{};
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
         union { bf16x8 v; u32x4 u; } c;
-        c.v = finite[t] = x[t];
+        c.v = x[t];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t m = c.u[i] & 0x7fff7fffu;
             most = __builtin_elementwise_max(most, *reinterpret_cast<const u16x2*>(&m));
         }
     }
-    if (!__any(most[0] >= 0x7f80 || most[1] >= 0x7f80)) return true;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-        union { bf16x8 v; uint16_t h[8]; } c;
-        c.v = x[t];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) c.h[i] = (c.h[i] & 0x7f80) == 0x7f80 ? 0 : c.h[i];
-        finite[t] = c.v;
-    }
-    return false;
+    return !__any(most[0] >= 0x7f80 || most[1] >= 0x7f80);
 }
-template <int D, bool LATER>
-__device__ __forceinline__ void add_not_finite(const char* lds, int wave, int lane, f32x16 (&out)[2]) {
+__device__ __forceinline__ bf16x8 finite_part(bf16x8 x) {
+    union { bf16x8 v; u32x4 u; } c;
+    c.v = x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        c.u[i] = (c.u[i] & 0x7f80u) == 0x7f80u ? c.u[i] & 0xffff0000u : c.u[i];
+        c.u[i] = (c.u[i] & 0x7f800000u) == 0x7f800000u ? c.u[i] & 0xffffu : c.u[i];
+    }
+    return c.v;
+}
+
+// What the sources of the own chunk give: weights times c, (source block, target block) of 32 x 32 pairs by their number, see kPairs
+template <int D, bool LATER, bool FINITE>
+__device__ __forceinline__ void add_own_chunk(const char* lds, const bf16x8 (&sources)[4], int wave, int lane, f32x16 (&out)[2]) {
+    const char* const weights = lds + Lds<D>::kP + lane * 16;
+#pragma unroll
+    for (int blk = 0; blk < 3; ++blk) {
+        const int sb = LATER ? (blk > 0) : blk >> 1, tb = LATER ? blk >> 1 : (blk > 0);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+            const bf16x8 c = FINITE ? sources[2 * sb + tt] : finite_part(sources[2 * sb + tt]);
+            out[tb] = mfma(c, *reinterpret_cast<const bf16x8*>(weights + (blk * 4 + tt * 2) * 1024), out[tb]);
+            out[tb] = mfma(c, *reinterpret_cast<const bf16x8*>(weights + (blk * 4 + tt * 2 + 1) * 1024), out[tb]);
+        }
+    }
+    if (FINITE) return;
     const char* const tile = lds + Lds<D>::kC;
     const int t32 = lane & 31, hh = lane >> 5;
 #pragma unroll 1
@@ -169,9 +187,8 @@ __device__ __forceinline__ void add_not_finite(const char* lds, int wave, int la
         for (int tb = 0; tb < 2; ++tb) {
             if (LATER ? sb < tb : sb > tb) continue;
             const bool sees = sb != tb || (LATER ? r >= t32 : r <= t32);
-            // the weight of (s, t32) as it was laid out for the product: lane 32 (r / 4 % 2) + t32, element 4 (r / 8 % 2) + r % 4 of step r / 16
-            const int blk = sb + tb;      // (0, 0), (0, 1) or (1, 0), (1, 1)
-            const char* const at = lds + Lds<D>::kP + (blk * 4 + (r / 16) * 2) * 1024 + (32 * (r / 4 % 2) + t32) * 16 + (4 * (r / 8 % 2) + r % 4) * 2;
+            // the weight of (s, t32) as it was laid out for the products: lane 32 (r / 4 % 2) + t32, element 4 (r / 8 % 2) + r % 4 of step r / 16
+            const char* const at = lds + Lds<D>::kP + ((sb + tb) * 4 + (r / 16) * 2) * 1024 + (32 * (r / 4 % 2) + t32) * 16 + (4 * (r / 8 % 2) + r % 4) * 2;
             const float weight = (float)*reinterpret_cast<const __bf16*>(at) + (float)*reinterpret_cast<const __bf16*>(at + 1024);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
@@ -189,14 +206,17 @@ __device__ __forceinline__ void add_not_finite(const char* lds, int wave, int la
 //   OUT     outputs are wanted, not only the state
 //   DOTS    the dot products of the output with the tensor it is the gradient of, the part from the own chunk (without the token's own) and
 //           the part from the state apart
+//   ONE     a KV head has one query head
 // Returns the log2 of the segment's decay.
-template <int D, bool LATER, bool OUT, bool DOTS>
+template <int D, bool LATER, bool OUT, bool DOTS, bool ONE>
 __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, const Segment& seg, int kv_head, char* lds, State<D>& S) {
     using L = Lds<D>;
     constexpr int kWaves = L::kWaves;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int d = p.shape.head_dim, group = p.shape.group;
-    const int t32 = lane & 31, hh = lane >> 5;
+    const int d = p.shape.head_dim, group = ONE ? 1 : p.shape.group;
+    const int hh = lane >> 5;
+    TileReads<D> reads;
+    reads.init(lane);
     char* const tile_a = lds + L::kA;
     char* const tile_b = lds + L::kB;
     char* const tile_c = lds + L::kC;
@@ -214,31 +234,47 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
 
     TileLoad<D> la, lb, lc, le;
     float next_g = 0.f;
-    // the tiles of (chunk number n of the walk, query head h of the group)
+    const int first_target = LATER ? kv_head : kv_head * group, first_source = LATER ? kv_head * group : kv_head;
+    const uint16_t* const base_a = f.a + seg.start * f.a_stride + (int64_t)first_target * d;
+    const uint16_t* const base_e = f.e + seg.start * f.e_stride + (int64_t)first_target * d;
+    const uint16_t* const base_b = f.b + seg.start * f.b_stride + (int64_t)first_source * d;
+    const uint16_t* const base_c = f.c + seg.start * f.c_stride + (int64_t)first_source * d;
+    const float* const base_g = p.log_decay + seg.start * p.decay_stride + kv_head;
+    // the tiles of chunk number n of the walk and query head h of the group, if there is that chunk
     auto issue = [&](int n, int h) {
         const int chunk = LATER ? chunks - 1 - n : n;
-        const int first = chunk * kLinearChunk, rows = seg.rows - first;
-        const int64_t at = seg.start + first;
-        const int qh = kv_head * group + h;
-        const int target_head = LATER ? kv_head : qh, source_head = LATER ? qh : kv_head;
-        if (OUT && (!LATER || h == 0)) {
-            la.issue(f.a + at * f.a_stride + (int64_t)target_head * d, f.a_stride, rows, d);
-            if (DOTS) le.issue(f.e + at * f.e_stride + (int64_t)target_head * d, f.e_stride, rows, d);
+        const int first = n < chunks ? chunk * kLinearChunk : 0, rows = n < chunks ? seg.rows - first : 0;
+        if (OUT) {
+            if (ONE || !LATER || h == 0) {
+                la.issue(base_a + first * f.a_stride + h * d, f.a_stride, rows, d);
+                if (DOTS) le.issue(base_e + first * f.e_stride + h * d, f.e_stride, rows, d);
+            } else {
+                la.drop();
+                if (DOTS) le.drop();
+            }
         }
-        if (LATER || h == 0) {
-            lb.issue(f.b + at * f.b_stride + (int64_t)source_head * d, f.b_stride, rows, d);
-            lc.issue(f.c + at * f.c_stride + (int64_t)source_head * d, f.c_stride, rows, d);
+        if (ONE || LATER || h == 0) {
+            lb.issue(base_b + first * f.b_stride + h * d, f.b_stride, rows, d);
+            lc.issue(base_c + first * f.c_stride + h * d, f.c_stride, rows, d);
+        } else {
+            lb.drop();
+            lc.drop();
         }
-        if (h == 0) next_g = lane < rows ? p.log_decay[(at + lane) * p.decay_stride + kv_head] : 0.f;
+        if (ONE || h == 0) next_g = lane < rows ? base_g[(first + lane) * p.decay_stride] : 0.f;
     };
     if (chunks > 0) issue(0, 0);
     for (int n = 0; n < chunks; ++n) {
         const int chunk = LATER ? chunks - 1 - n : n;
         const int first = chunk * kLinearChunk;
-        f32x16 out[2];
+        f32x16 out_of_heads[2];            // LATER: summed over the heads
         float chunk_decay = 0.f;
         for (int h = 0; h < group; ++h) {
+            f32x16 out_of_head[2];
+            f32x16 (&out)[2] = LATER ? out_of_heads : out_of_head;
             const bool first_head = h == 0, last_head = h == group - 1;
+            int t32 = lane & 31;
+            asm volatile("" : "+v"(t32));      // (as reads.fresh(): or the mask of every hidden pair is kept in registers)
+            reads.fresh();
             if (OUT && (!LATER || first_head)) {
                 la.put(tile_a);
                 if (DOTS) le.put(tile_e);
@@ -259,9 +295,6 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                 }
             }
             __syncthreads();
-            if (h + 1 < group) issue(n, h + 1);
-            else if (n + 1 < chunks) issue(n + 1, 0);
-
             if constexpr (OUT) {
                 // pairs of sources (along the rows) and targets (along the lanes): of the four blocks of 32 x 32, the three that are not all hidden
 #pragma unroll 1
@@ -270,12 +303,12 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                     f32x16 w{};
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk)
-                        w = mfma(read_rowmajor_frag<D>(tile_b, sb, kk, lane), read_rowmajor_frag<D>(tile_a, tb, kk, lane), w);
+                        w = mfma(reads.along(tile_b, sb, kk), reads.along(tile_a, tb, kk), w);
                     f32x16 y{};
                     if constexpr (DOTS) {
 #pragma unroll
                         for (int kk = 0; kk < D / 16; ++kk)
-                            y = mfma(read_rowmajor_frag<D>(tile_c, sb, kk, lane), read_rowmajor_frag<D>(tile_e, tb, kk, lane), y);
+                            y = mfma(reads.along(tile_c, sb, kk), reads.along(tile_e, tb, kk), y);
                     }
                     const float target_sum = sums[tb * 32 + t32];
                     float dot = 0.f;
@@ -317,7 +350,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                         const TwoParts parts = two_parts(x);
 #pragma unroll
                         for (int tb = 0; tb < 2; ++tb) {
-                            const bf16x8 a = read_rowmajor_frag<D>(tile_a, tb, kk, lane);
+                            const bf16x8 a = reads.along(tile_a, tb, kk);
                             out[tb] = mfma(parts.hi, a, out[tb]);
                             out[tb] = mfma(parts.lo, a, out[tb]);
                         }
@@ -345,24 +378,13 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                 __syncthreads();
             }
 
+            bf16x8 sources[4];     // c, 16 sources at a time down the operand's k
             if (has_columns) {
-                bf16x8 sources[4];     // c, 16 sources at a time down the operand's k
 #pragma unroll
-                for (int t = 0; t < 4; ++t) sources[t] = read_transposed_frag<D>(tile_c, wave, t, lane);
+                for (int t = 0; t < 4; ++t) sources[t] = reads.down(tile_c, wave, t);
                 if constexpr (OUT) {
-                    bf16x8 finite[4];
-                    const bool all_finite = only_finite(sources, finite);
-#pragma unroll
-                    for (int blk = 0; blk < 3; ++blk) {
-                        const int sb = LATER ? (blk > 0) : blk >> 1, tb = LATER ? blk >> 1 : (blk > 0);
-#pragma unroll
-                        for (int tt = 0; tt < 2; ++tt) {
-                            const char* const at = lds + L::kP + (blk * 4 + tt * 2) * 1024 + lane * 16;
-                            out[tb] = mfma(finite[2 * sb + tt], *reinterpret_cast<const bf16x8*>(at), out[tb]);
-                            out[tb] = mfma(finite[2 * sb + tt], *reinterpret_cast<const bf16x8*>(at + 1024), out[tb]);
-                        }
-                    }
-                    if (!all_finite) add_not_finite<D, LATER>(lds, wave, lane, out);
+                    if (all_finite(sources)) add_own_chunk<D, LATER, true>(lds, sources, wave, lane, out);
+                    else add_own_chunk<D, LATER, false>(lds, sources, wave, lane, out);
                     if (!LATER || last_head) {
                         const int target_head = LATER ? kv_head : kv_head * group + h;
 #pragma unroll
@@ -378,6 +400,11 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                         }
                     }
                 }
+            }
+            // the next tiles: behind the outputs, whose registers they take, and in front of the state's products, which hide some of their way
+            if (h + 1 < group) issue(n, h + 1);
+            else issue(n + 1, 0);
+            if (has_columns) {
                 if (LATER || last_head) {
                     if (!LATER || first_head) {
                         const float left = fast_exp2(chunk_decay);
@@ -401,7 +428,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                         const TwoParts parts = two_parts(x);
 #pragma unroll
                         for (int db = 0; db < D / 32; ++db) {
-                            const bf16x8 rows = read_transposed_frag_in_order<D>(tile_b, db, t, lane);
+                            const bf16x8 rows = reads.down_ordered(tile_b, db, t);
                             S.x[db] = mfma(rows, parts.hi, S.x[db]);
                             S.x[db] = mfma(rows, parts.lo, S.x[db]);
                         }
@@ -440,7 +467,7 @@ __device__ __forceinline__ const float* reaching_state(const LinearParams& p, co
     return m;
 }
 
-template <int D, bool LATER, bool DOTS>
+template <int D, bool LATER, bool DOTS, bool ONE>
 __device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine& f, const Segment& seg, int slot, int kv_head, char* lds) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = p.shape.head_dim;
     State<D> S;
@@ -448,7 +475,7 @@ __device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine&
     const float* const from = reaching_state<LATER>(p, seg, kv_head, &bad);
     if (from) S.load(from, d, f.transposed, wave, lane);
     else S.clear(bad ? __builtin_nanf("") : 0.f);
-    walk<D, LATER, true, DOTS>(p, f, seg, kv_head, lds, S);
+    walk<D, LATER, true, DOTS, ONE>(p, f, seg, kv_head, lds, S);
     if (!LATER && DOTS) {
         // <S, dS> behind the segment's last token: what the gradient of its decays starts from
         const float* const d_end = reaching_state<true>(p, seg, kv_head, &bad);
@@ -497,24 +524,24 @@ __device__ __forceinline__ Routine dv_routine(const LinearParams& p) {
     return Routine{p.k, p.q, p.d_o, nullptr, p.kv_stride, p.q_stride, p.do_stride, 0, 1.f, p.scale, p.dv, p.grad_f32 != 0, false, nullptr, nullptr};
 }
 
-template <int D>
+template <int D, bool ONE>
 __global__ __launch_bounds__(D / 32 * 64, 2) void linear_fwd_kernel(LinearParams p) {
     __shared__ __align__(16) char lds[Lds<D>::bytes(true, false)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block(p.shape, 1, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
-    outputs_of<D, false, false>(p, forward_routine(p), seg, slot, kv_head, lds);
+    outputs_of<D, false, false, ONE>(p, forward_routine(p), seg, slot, kv_head, lds);
 }
 
-template <int D>
+template <int D, bool ONE>
 __global__ __launch_bounds__(D / 32 * 64, 2) void linear_bwd_kernel(LinearParams p) {
     __shared__ __align__(16) char lds[Lds<D>::bytes(true, true)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
-    if (role == 0) outputs_of<D, false, true>(p, dq_routine(p), seg, slot, kv_head, lds);
-    else if (role == 1) outputs_of<D, true, true>(p, dk_routine(p), seg, slot, kv_head, lds);
-    else outputs_of<D, true, false>(p, dv_routine(p), seg, slot, kv_head, lds);
+    if (role == 0) outputs_of<D, false, true, ONE>(p, dq_routine(p), seg, slot, kv_head, lds);
+    else if (role == 1) outputs_of<D, true, true, ONE>(p, dk_routine(p), seg, slot, kv_head, lds);
+    else outputs_of<D, true, false, ONE>(p, dv_routine(p), seg, slot, kv_head, lds);
 }
 
 // What a segment adds to the state, into the entry of the segment that it reaches next; `roles` 2: also what it adds to the gradient.
@@ -529,8 +556,8 @@ __global__ __launch_bounds__(D / 32 * 64, 2) void linear_state_kernel(LinearPara
     if (role == 0 ? last : seg.index == 0) return;
     State<D> S;
     S.clear(0.f);
-    const float decay = role == 0 ? walk<D, false, false, false>(p, forward_routine(p), seg, kv_head, lds, S)
-                                  : walk<D, true, false, false>(p, dv_routine(p), seg, kv_head, lds, S);
+    const float decay = role == 0 ? walk<D, false, false, false, true>(p, forward_routine(p), seg, kv_head, lds, S)
+                                  : walk<D, true, false, false, false>(p, dv_routine(p), seg, kv_head, lds, S);
     const int64_t own = (int64_t)(seg.entry + seg.index) * p.shape.kv_heads + kv_head;
     float* const to = role == 0 ? p.states + (own + p.shape.kv_heads) * d * d : p.d_states + (own - p.shape.kv_heads) * d * d;
     S.store(to, d, wave, lane);
@@ -651,12 +678,14 @@ void launch_states(const LinearParams& p, int roles, hipStream_t stream) {
 template <int D>
 void launch_fwd(const LinearParams& p, hipStream_t stream) {
     launch_states<D>(p, 1, stream);
-    linear_fwd_kernel<D><<<grid_of(p, 1), D / 32 * 64, 0, stream>>>(p);
+    const auto kernel = p.shape.group == 1 ? linear_fwd_kernel<D, true> : linear_fwd_kernel<D, false>;
+    kernel<<<grid_of(p, 1), D / 32 * 64, 0, stream>>>(p);
 }
 template <int D>
 void launch_bwd(const LinearParams& p, hipStream_t stream) {
     launch_states<D>(p, 2, stream);
-    linear_bwd_kernel<D><<<grid_of(p, 3), D / 32 * 64, 0, stream>>>(p);
+    const auto kernel = p.shape.group == 1 ? linear_bwd_kernel<D, true> : linear_bwd_kernel<D, false>;
+    kernel<<<grid_of(p, 3), D / 32 * 64, 0, stream>>>(p);
 }
 
 }  // namespace

@@ -98,26 +98,50 @@ __device__ __forceinline__ TwoParts two_parts(const float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         hi.u[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+        asm("" : "+v"(hi.u[i]));     // (its halves are taken from the register: converting x again takes half as many conversions more)
         const float a = __uint_as_float(hi.u[i] << 16), b = __uint_as_float(hi.u[i] & 0xffff0000u);
         lo.u[i] = pack_bf16(x[2 * i] - a, x[2 * i + 1] - b);
     }
     return TwoParts{hi.v, lo.v};
 }
 
-// read_transposed_frag with the 16 columns of a lane group in another order: result row 16 g + 8 hi + 4 mid + low (MFMA M index) is column
-// 16 g + 8 mid + 4 hi + low.  An accumulator of a product with such an A operand then holds, in registers 8 t .. 8 t + 7 of
-// lane half hh, the columns 16 t + 8 hh + {0 .. 7}: the k order that an operand read along a row has.
+// Reads of a swizzled tile (see swizzle in attn_device.hpp).  Row and column take part in an address by different bits, and the swizzle is an exclusive
+// or of the column's with some of the row's: so an address is a lane's own part, exclusive or the part of the column, plus 32-row steps.
+// The lane's parts are values of their own in every round of a loop (`fresh`): derived addresses are then made where they are used, in one operation,
+// and not kept in dozens of registers across the loop.
 template <int D>
-__device__ __forceinline__ bf16x8 read_transposed_frag_in_order(const char* tile, int cb, int t, int lane) {
-    const int c16 = lane & 15, c = c16 & 3;
-    const int col = cb * 32 + (((lane >> 4) & 1) << 4) + (((c & 1) << 1 | c >> 1) << 2);
-    const int row = t * 16 + ((lane >> 5) << 2) + (c16 >> 2);
-    const s16x4 lo = lds_transpose_read(tile + tile_offset<D>(row, col));
-    const s16x4 hi = lds_transpose_read(tile + tile_offset<D>(row + 8, col));
-    union { struct { s16x4 a, b; } s; bf16x8 v; } u;
-    u.s.a = lo;
-    u.s.b = hi;
-    return u.v;
-}
+struct TileReads {
+    uint32_t row_part;          // row lane % 32, chunk lane / 32
+    uint32_t down_part;         // row 4 (lane / 32) + lane % 16 / 4, columns 16 (lane / 16 % 2) + 4 (lane % 4)
+    uint32_t ordered_part;      // the same with columns 16 (lane / 16 % 2) + 4 * (0, 2, 1, 3)[lane % 4]
+    __device__ __forceinline__ void init(int lane) {
+        row_part = tile_offset<D>(lane & 31, (lane >> 5) * 8);
+        const int row = ((lane >> 5) << 2) + ((lane & 15) >> 2), c = lane & 3, group = ((lane >> 4) & 1) << 4;
+        down_part = tile_offset<D>(row, group + c * 4);
+        ordered_part = tile_offset<D>(row, group + ((c & 1) << 1 | c >> 1) * 4);
+    }
+    __device__ __forceinline__ void fresh() { asm volatile("" : "+v"(row_part), "+v"(down_part), "+v"(ordered_part)); }
+    // an operand whose k runs along the rows: rows 32 rb .. + 31, columns 16 kk .. + 15
+    __device__ __forceinline__ bf16x8 along(const char* tile, int rb, int kk) const {
+        return *reinterpret_cast<const bf16x8*>(tile + (row_part ^ (kk << 5)) + rb * 32 * D * 2);
+    }
+    // an operand whose k runs down the rows: rows 16 t .. + 15 in the order of an accumulator (see read_transposed_frag), columns 32 cb .. + 31
+    __device__ __forceinline__ bf16x8 down(const char* tile, int cb, int t) const { return down_from(tile, down_part ^ (cb << 6), t); }
+    // the same with the columns in another order: result row (MFMA M index) 16 g + 8 hi + 4 mid + low is column 16 g + 8 mid + 4 hi + low.
+    // An accumulator of a product with such an A operand then holds, in registers 8 t .. 8 t + 7 of lane half hh, the columns
+    // 16 t + 8 hh + {0 .. 7}: the k order that an operand read along a row has.
+    __device__ __forceinline__ bf16x8 down_ordered(const char* tile, int cb, int t) const { return down_from(tile, ordered_part ^ (cb << 6), t); }
+
+private:
+    __device__ __forceinline__ static bf16x8 down_from(const char* tile, uint32_t at, int t) {
+        // eight rows further down: the row's bit 3 is bit 1 of the swizzle's (row / 4) % 4
+        const s16x4 lo = lds_transpose_read(tile + at + t * 16 * D * 2);
+        const s16x4 hi = lds_transpose_read(tile + (at ^ (2 << 4)) + t * 16 * D * 2 + 8 * D * 2);
+        union { struct { s16x4 a, b; } s; bf16x8 v; } u;
+        u.s.a = lo;
+        u.s.b = hi;
+        return u.v;
+    }
+};
 
 }  // namespace hspmd
