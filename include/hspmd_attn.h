@@ -594,7 +594,7 @@ typedef struct {
 /*
  * o of all rows, and the final states.
  *   q, k, v    bf16 [total_rows, heads, head_dim], 16-byte aligned; token strides in elements, multiples of 8, >= heads*head_dim, at most 2^24
- *   log_decay  fp32, g of row t and KV head h at t * decay_token_stride + h: >= local_kv_heads, or 0 for one decay per KV head.  -infinity and
+ *   log_decay  fp32, g of row t and KV head h at t * decay_token_stride + h: >= local_kv_heads and at most 2^23, or 0 for one decay per KV head.  -infinity and
  *              anything below -110 forgets all; values above 0 are taken as they are, as long as no product of them along 64 rows overflows
  *   scale      as softmax_scale of hspmd_attn_varlen_fwd
  *   initial    NULL: every sequence starts from zeros.  A slot outside the pool gives NaN to its sequence's rows

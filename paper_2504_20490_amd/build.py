@@ -9,9 +9,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIBRARY = os.path.join(HERE, "libhspmd_attn.so")
 SOURCES = ["hspmd_attn_api.hip", "schedule.cpp", "fwd_kernel.hip", "bwd_kernels.hip", "bwd_dkv_kernel.hip", "merge_kernel.hip", "probe.hip", "rope_kernel.hip",
            "rope_axes_kernel.hip", "kv_cache_kernel.hip", "paged_attn_kernel.hip", "paged_many_kernel.hip",
-           "linear_attn_kernel.hip", "linear_step_kernel.hip"]
+           "linear_fwd_kernel.hip", "linear_bwd_kernel.hip", "linear_state_kernel.hip", "linear_step_kernel.hip"]
 HEADERS = ["attn_device.hpp", "fwd_iteration.hpp", "fwd_tiles.hpp", "kernels.hpp", "schedule.hpp", "paged.hpp", "paged_device.hpp", "paged_index.hpp",
-           "paged_item.hpp", "linear.hpp", "linear_device.hpp", "linear_index.hpp", os.path.join("..", "..", "include", "hspmd_attn.h")]
+           "paged_item.hpp", "linear.hpp", "linear_device.hpp", "linear_walk.hpp", "linear_index.hpp", os.path.join("..", "..", "include", "hspmd_attn.h")]
 
 # Packed fp32 VALU forms are switched off for all device code of this library.
 HIPCC_FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",

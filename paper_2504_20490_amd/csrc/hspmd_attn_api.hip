@@ -1384,6 +1384,7 @@ static hspmd_status check_linear_rows(const hspmd_linear_batch* batch, const voi
     if (hspmd_status rc = check_linear_stride(kv_token_stride, batch->local_kv_heads, batch->head_dim, "kv_token_stride")) return rc;
     if (decay_token_stride != 0 && decay_token_stride < batch->local_kv_heads)
         return fail(HSPMD_ERR_INVALID_ARG, "decay_token_stride must be 0 or >= local_kv_heads");
+    if (decay_token_stride > (kMaxLinearStride >> 1)) return fail(HSPMD_ERR_INVALID_ARG, "decay_token_stride must not exceed 2^23");
     return HSPMD_OK;
 }
 
@@ -1418,6 +1419,7 @@ static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward,
         at += bytes;
         return r;
     };
+    p->scale_log2 = std::log2(p->scale);
     p->states = take(sizes.state_bytes);
     p->seg_decay = take(sizes.decay_bytes);
     if (backward) {

@@ -33,7 +33,7 @@ struct LinearParams {
     const uint16_t* d_o;           // backward only
     const float* log_decay;
     int64_t q_stride, kv_stride, do_stride, decay_stride;
-    float scale;
+    float scale, scale_log2;       // and its log2
     LinearStates initial, final;   // backward: `final` is the gradient that comes in (read)
     void* o;                       // forward: bf16
     void* dq;
@@ -64,6 +64,8 @@ struct LinearSizes {
 };
 LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                          bool backward);
+// states of sequences that are cut into segments; parts: of a source's bf16 values, 2 or 3
+void launch_linear_states(const LinearParams& p, bool backward, int parts, hipStream_t stream);
 hipError_t launch_linear_fwd(const LinearParams& p, hipStream_t stream);
 hipError_t launch_linear_bwd(const LinearParams& p, hipStream_t stream);
 

@@ -1,0 +1,99 @@
+// Linear attention with a decay for each head, chunked form: the gradients.
+#include "linear_walk.hpp"
+
+namespace hspmd {
+namespace {
+
+template <int D, bool ONE, int WEIGHT_PARTS>
+// (three parts of the weights leave room for one workgroup per compute unit)
+__global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2) void linear_bwd_kernel(LinearParams p) {
+    __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS>::bytes(true, true)];
+    int role, kv_head, slot;
+    Segment seg;
+    if (!item_of_block(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
+    if (role == 0) outputs_of<D, false, true, ONE, 3, WEIGHT_PARTS>(p, dq_routine(p), seg, slot, kv_head, lds);
+    else if (role == 1) outputs_of<D, true, true, ONE, 3, WEIGHT_PARTS>(p, dk_routine(p), seg, slot, kv_head, lds);
+    else outputs_of<D, true, false, ONE, 3, WEIGHT_PARTS>(p, dv_routine(p), seg, slot, kv_head, lds);
+}
+
+// Gradients of the log decays, one wave per segment and KV head, from its last chunk to its first.  g_t weighs every pair of a token from t on
+// and one before t.  Of these pairs, a chunk's own and those with a token on one side of the chunk come from the dot products;
+// those across the whole chunk, <e^{G_L} S, R>, are what is left of <S, dS> at its end without its own keys.
+__global__ __launch_bounds__(64) void linear_decay_kernel(LinearParams p) {
+    const LinearShape& sh = p.shape;
+    int role, kv_head, slot;
+    if (!item_of_block(sh, 1, role, kv_head, slot)) return;
+    const int lane = threadIdx.x & 63;
+    const int64_t item = (int64_t)slot * sh.kv_heads + kv_head;
+    const bool fixed = p.decay_stride == 0;
+    Segment seg;
+    if (!find_segment(sh, slot, seg)) {
+        if (fixed && lane == 0) p.decay_sums[item] = 0.f;
+        return;
+    }
+    float across = p.across[item], total = 0.f;
+    for (int chunk = (seg.rows + kLinearChunk - 1) / kLinearChunk - 1; chunk >= 0; --chunk) {
+        const int64_t row = seg.start + chunk * kLinearChunk + lane;
+        const bool there = chunk * kLinearChunk + lane < seg.rows;
+        float near = 0.f, far_q = 0.f, far_k = 0.f, g = 0.f;
+        if (there) {
+            g = decay_log2(p.log_decay[row * p.decay_stride + kv_head]);
+            far_k = p.k_far[(int64_t)kv_head * sh.total_rows + row];
+            for (int h = 0; h < sh.group; ++h) {
+                const int64_t at = (int64_t)(kv_head * sh.group + h) * sh.total_rows + row;
+                near += p.q_near[at];
+                far_q += p.q_far[at];
+            }
+            near -= p.k_near[(int64_t)kv_head * sh.total_rows + row];
+        }
+        const float all_k = wave_sum(far_k);
+        // (a decay that leaves nothing leaves no pairs across it either, not even rounding errors)
+        const float whole = fast_exp2(wave_sum(g)) == 0.f ? 0.f : across - all_k;
+        const float later = sum_from(near + far_q, lane);
+        const float grad = later + (sum_up_to(far_k) - far_k) + whole;
+        if (there) {
+            if (fixed) total += grad;
+            else p.d_log_decay[row * sh.kv_heads + kv_head] = grad;
+        }
+        across = whole + wave_sum(far_q);
+    }
+    if (fixed) {
+        total = wave_sum(total);
+        if (lane == 0) p.decay_sums[item] = total;
+    }
+}
+
+// A fixed decay's gradient is the sum over all tokens: one workgroup per KV head, in a fixed order.
+__global__ __launch_bounds__(256) void linear_decay_sum_kernel(LinearParams p) {
+    __shared__ float parts[4];
+    float sum = 0.f;
+    for (int64_t i = threadIdx.x; i < p.shape.slots; i += 256) sum += p.decay_sums[i * p.shape.kv_heads + blockIdx.x];
+    sum = wave_sum(sum);
+    if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) p.d_log_decay[blockIdx.x] = parts[0] + parts[1] + parts[2] + parts[3];
+}
+
+template <int D, bool ONE>
+void launch(const LinearParams& p, hipStream_t stream) {
+    const auto kernel = p.grad_f32 ? linear_bwd_kernel<D, ONE, 3> : linear_bwd_kernel<D, ONE, 2>;
+    kernel<<<grid_of(p, 3), D / 32 * 64, 0, stream>>>(p);
+}
+
+}  // namespace
+
+hipError_t launch_linear_bwd(const LinearParams& p, hipStream_t stream) {
+    if (p.shape.slots > 0) {
+        launch_linear_states(p, true, 3, stream);
+        const bool one = p.shape.group == 1;
+        if (p.shape.head_dim <= 64) one ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
+        else one ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+    }
+    if (p.d_log_decay) {
+        if (p.shape.slots > 0) linear_decay_kernel<<<grid_of(p, 1), 64, 0, stream>>>(p);
+        if (p.decay_stride == 0) linear_decay_sum_kernel<<<(unsigned)p.shape.kv_heads, 256, 0, stream>>>(p);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace hspmd

@@ -3,6 +3,8 @@
 #include "attn_device.hpp"
 #include "linear.hpp"
 
+#include <type_traits>
+
 namespace hspmd {
 
 // A decay of 2^-160 or less leaves nothing of any fp32 number, and infinities would make differences of sums NaN.
@@ -12,15 +14,21 @@ __device__ __forceinline__ float decay_log2(float log_decay) {
     return g < kForgetLog2 ? kForgetLog2 : g;      // (NaN stays)
 }
 
-// inclusive sum over the lanes 0 .. lane of a wave, and over the lanes lane .. 63
-__device__ __forceinline__ float sum_up_to(float x, int lane) {
-#pragma unroll
-    for (int step = 1; step < 64; step *= 2) {
-        const float y = __shfl_up(x, step, 64);
-        x += lane >= step ? y : 0.f;
-    }
+// inclusive sum over the lanes 0 .. lane of a wave (all lanes active): rows of 16 lanes, then their last lanes to the rows behind
+__device__ __forceinline__ float sum_up_to(float x) {
+    const auto moved = [](float v, auto ctrl, auto rows) {
+        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), decltype(ctrl)::value, decltype(rows)::value, 0xf, true));
+    };
+    using std::integral_constant;
+    x += moved(x, integral_constant<int, 0x111>{}, integral_constant<int, 0xf>{});      // row_shr 1, 2, 4, 8
+    x += moved(x, integral_constant<int, 0x112>{}, integral_constant<int, 0xf>{});
+    x += moved(x, integral_constant<int, 0x114>{}, integral_constant<int, 0xf>{});
+    x += moved(x, integral_constant<int, 0x118>{}, integral_constant<int, 0xf>{});
+    x += moved(x, integral_constant<int, 0x142>{}, integral_constant<int, 0xa>{});      // row_bcast 15: lane 15 of rows 0, 2 to rows 1, 3
+    x += moved(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});      // row_bcast 31: lane 31 to rows 2, 3
     return x;
 }
+// over the lanes lane .. 63
 __device__ __forceinline__ float sum_from(float x, int lane) {
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) {
@@ -89,21 +97,74 @@ __device__ __forceinline__ float* state_of(const LinearStates& s, int seq, int h
     return slot < s.num_slots ? s.data + slot * s.slot_stride + (int64_t)head * head_dim * head_dim : nullptr;
 }
 
-// x as two bf16 values, the second the rest that the first leaves: 16 to 17 bits together (relative error up to 2^-17.5)
-struct TwoParts {
-    bf16x8 hi, lo;
-};
-__device__ __forceinline__ TwoParts two_parts(const float (&x)[8]) {
-    union { u32x4 u; bf16x8 v; } hi, lo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        hi.u[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-        asm("" : "+v"(hi.u[i]));     // (its halves are taken from the register: converting x again takes half as many conversions more)
-        const float a = __uint_as_float(hi.u[i] << 16), b = __uint_as_float(hi.u[i] & 0xffff0000u);
-        lo.u[i] = pack_bf16(x[2 * i] - a, x[2 * i + 1] - b);
+typedef __attribute__((ext_vector_type(8))) float f32x8;
+
+// a - the low, or high, half of a pair of bf16 values, or 0 * both + a: one operation instead of unpacking and subtracting.  (The difference is exact where
+// the pair is a rounding of a; a pair with an infinity or NaN gives NaN.)
+struct PairOps {
+    uint32_t low, high, none;     // (-1, 0), (0, -1), (0, 0): in scalar registers, of which an inline constant would mean something else
+    __device__ __forceinline__ void init() {
+        low = 0x0000bf80u, high = 0xbf800000u, none = 0u;
+        asm("" : "+s"(low), "+s"(high), "+s"(none));
     }
-    return TwoParts{hi.v, lo.v};
+    static __device__ __forceinline__ float dot(uint32_t pair, uint32_t by, float a) {
+        union { uint32_t u; bf16x2 v; } x, y;
+        x.u = pair, y.u = by;
+        return __builtin_amdgcn_fdot2_f32_bf16(x.v, y.v, a, false);
+    }
+};
+
+// What eight values leave of their roundings to bf16, x kept: as PairOps::dot, which overwrites its third operand.  The operations are written out because
+// the compiler takes the overwriting form with a copy in front: one more for each value of a state.  A dot product's result may be read three operations
+// later by one of another kind; and x must not come from a matrix product just in front, whose results an instruction here would not wait for.
+__device__ __forceinline__ f32x8 rest_of_rounding(const f32x8& x, const u32x4& pairs, const PairOps& ops) {
+    f32x8 r;
+    float r0, r1, r2, r3, r4, r5, r6, r7;
+    asm volatile("v_dot2_f32_bf16 %0, %8, %20, %12\n\tv_dot2_f32_bf16 %1, %8, %21, %13\n\t"
+                 "v_dot2_f32_bf16 %2, %9, %20, %14\n\tv_dot2_f32_bf16 %3, %9, %21, %15\n\t"
+                 "v_dot2_f32_bf16 %4, %10, %20, %16\n\tv_dot2_f32_bf16 %5, %10, %21, %17\n\t"
+                 "v_dot2_f32_bf16 %6, %11, %20, %18\n\tv_dot2_f32_bf16 %7, %11, %21, %19\n\ts_nop 2"
+                 : "=&v"(r0), "=&v"(r1), "=&v"(r2), "=&v"(r3), "=&v"(r4), "=&v"(r5), "=&v"(r6), "=&v"(r7)
+                 : "v"(pairs[0]), "v"(pairs[1]), "v"(pairs[2]), "v"(pairs[3]), "v"(x[0]), "v"(x[1]), "v"(x[2]), "v"(x[3]), "v"(x[4]), "v"(x[5]), "v"(x[6]),
+                   "v"(x[7]), "s"(ops.low), "s"(ops.high));
+    r[0] = r0, r[1] = r1, r[2] = r2, r[3] = r3, r[4] = r4, r[5] = r5, r[6] = r6, r[7] = r7;
+    return r;
 }
+
+// fp32 values as sums of bf16 values, each the rounding of what those before it leave: two hold 16 to 17 bits (error 2^-17.5 at most), three all 24
+template <int PARTS>
+struct Parts {
+    bf16x8 part[PARTS];
+    // KEEP: x lives on (see rest_of_rounding)
+    template <bool KEEP = false>
+    __device__ __forceinline__ void of(f32x8 x, const PairOps& ops) {
+        if constexpr (KEEP) {
+            union { u32x4 u; bf16x8 v; } p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p.u[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+            part[0] = p.v;
+            Parts<PARTS - 1> others;
+            others.of(rest_of_rounding(x, p.u, ops), ops);
+#pragma unroll
+            for (int n = 1; n < PARTS; ++n) part[n] = others.part[n - 1];
+            return;
+        }
+#pragma unroll
+        for (int n = 0; n < PARTS; ++n) {
+            union { u32x4 u; bf16x8 v; } p;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                p.u[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
+                asm("" : "+v"(p.u[i]));      // (one register from here on: else both halves are converted a second time for the differences)
+                if (n + 1 < PARTS) {
+                    x[2 * i] = PairOps::dot(p.u[i], ops.low, x[2 * i]);
+                    x[2 * i + 1] = PairOps::dot(p.u[i], ops.high, x[2 * i + 1]);
+                }
+            }
+            part[n] = p.v;
+        }
+    }
+};
 
 // Reads of a swizzled tile (see swizzle in attn_device.hpp).  Row and column take part in an address by different bits, and the swizzle is an exclusive
 // or of the column's with some of the row's: so an address is a lane's own part, exclusive or the part of the column, plus 32-row steps.

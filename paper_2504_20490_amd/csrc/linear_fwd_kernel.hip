@@ -1,0 +1,58 @@
+// Linear attention with a decay for each head, chunked form: the forward.
+#include "linear_walk.hpp"
+
+namespace hspmd {
+namespace {
+
+template <int D, bool ONE, int PARTS>
+__global__ __launch_bounds__(D / 32 * 64, 2) void linear_fwd_kernel(LinearParams p) {
+    __shared__ __align__(16) char lds[Lds<D, 2>::bytes(true, false)];
+    int role, kv_head, slot;
+    Segment seg;
+    if (!item_of_block(p.shape, 1, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
+    outputs_of<D, false, false, ONE, PARTS, 2>(p, forward_routine(p), seg, slot, kv_head, lds);
+}
+
+template <int D, bool ONE>
+void launch(const LinearParams& p, hipStream_t stream) {
+    // (o is rounded to bf16: two parts of the state suffice for it, a final state that is kept takes three)
+    const auto kernel = p.final.data ? linear_fwd_kernel<D, ONE, 3> : linear_fwd_kernel<D, ONE, 2>;
+    kernel<<<grid_of(p, 1), D / 32 * 64, 0, stream>>>(p);
+}
+
+}  // namespace
+
+LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
+                         bool backward) {
+    LinearSizes s{};
+    const int64_t longest = max_rows > 0 && max_rows < total_rows ? max_rows : total_rows;
+    int64_t seg = ((int64_t)total_rows * kv_heads / 768 + kLinearChunk - 1) / kLinearChunk * kLinearChunk;
+    seg = seg < 256 ? 256 : seg > 4096 ? 4096 : seg;
+    s.seg_rows = longest <= seg ? 0 : (int32_t)seg;
+    if (s.seg_rows > 0) {
+        s.slots = linear_slots(total_rows, num_seqs, seg);
+        s.entries = linear_entries(total_rows, seg);
+        s.windows = linear_windows(total_rows, seg);
+    } else {
+        s.slots = num_seqs;
+    }
+    const auto rounded = [](int64_t bytes) { return (size_t)((bytes + 255) / 256 * 256); };
+    s.state_bytes = rounded(s.entries * kv_heads * head_dim * head_dim * 4);
+    s.decay_bytes = rounded(s.entries * kv_heads * 4);
+    s.q_row_bytes = rounded((int64_t)total_rows * q_heads * 4);
+    s.k_row_bytes = rounded((int64_t)total_rows * kv_heads * 4);
+    s.slot_bytes = rounded(s.slots * kv_heads * 4);
+    return s;
+}
+
+hipError_t launch_linear_fwd(const LinearParams& p, hipStream_t stream) {
+    if (p.shape.slots > 0) {
+        launch_linear_states(p, false, p.final.data ? 3 : 2, stream);
+        const bool one = p.shape.group == 1;
+        if (p.shape.head_dim <= 64) one ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
+        else one ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace hspmd

@@ -1,0 +1,585 @@
+// Linear attention with a decay for each head, chunked form, forward and backward.
+//
+// Per sequence and KV head, with G the running sum of the log decays from a chunk's start, S the state at that start and s the scale:
+//   o_t  = s e^{G_t} S^T q_t + s sum_{j <= t} e^{G_t - G_j} <q_t, k_j> v_j,      S' = e^{G_L} S + sum_j e^{G_L - G_j} k_j v_j^T.
+// The gradients are the same form with other tensors: dq looks backwards like o (targets dO, sources v and k, the transposed state),
+// dk and dv look forwards (targets v and k, sources dO, q and q, dO) with R, the gradient of the state at the chunk's end:
+//   dk_t = e^{G_L - G_t} R v_t + s sum_{i >= t} e^{G_i - G_t} <v_t, dO_i> q_i,    R' = e^{G_L} R + s sum_i e^{G_i} q_i dO_i^T.
+// So one routine does all four: targets a, sources b and c, state sum b c^T.
+#pragma once
+#include "linear_device.hpp"
+
+namespace hspmd {
+namespace {
+
+// Long sequences: segments of them go to different workgroups.  What each adds to the state is computed first (OUT false below), a small
+// launch passes the states from segment to segment, and then every segment starts with the state that reaches it.
+
+// What the routine below is given
+struct Routine {
+    const uint16_t* a;       // targets, [T, a_heads, d]
+    const uint16_t* b;       // sources
+    const uint16_t* c;
+    const uint16_t* e;       // DOTS: the tensor whose gradient the output is
+    int64_t a_stride, b_stride, c_stride, e_stride;
+    float scale_in, scale_state;   // of what the state gives to a target, of what a source gives to the state
+    void* out;
+    bool transposed;         // the state is b c^T transposed to how it lies in memory
+    float* near;             // DOTS: [heads][total_rows], see LinearParams
+    float* far;
+};
+
+// What a workgroup keeps in LDS.  WEIGHT_PARTS: bf16 values per weight of a pair
+template <int D, int WEIGHT_PARTS>
+struct Lds {
+    static constexpr int kWaves = D / 32;
+    static constexpr int kTile = kLinearChunk * D * 2;
+    static constexpr int kB = 0, kC = kTile;
+    static constexpr int kSums = 2 * kTile;                   // running sums of the log decays, weights of targets and of sources, the chunk's decay
+    static constexpr int kA = kSums + (3 * kLinearChunk + 4) * 4;
+    static constexpr int kWeights = kA + kTile;               // of pairs: [block][step of 16 sources][part][lane]
+    static constexpr int kNear = kWeights + 3 * 2 * WEIGHT_PARTS * 1024;
+    static constexpr int kFar = kNear + 3 * 32 * 4;
+    static constexpr int kE = kFar + kWaves * kLinearChunk * 4;
+    static constexpr int bytes(bool out, bool dots) { return dots ? kE + kTile : out ? kNear : kA; }
+    // where the weights of a block's step are, for lane 0
+    static constexpr int weights(int blk, int step, int part) { return kWeights + ((blk * 2 + step) * WEIGHT_PARTS + part) * 1024; }
+};
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// Memory from an address on, for accesses with 32-bit offsets: one at kNowhere reads zeros and writes nothing.  So the loops below hold no branches
+// around their loads and stores, and the compiler can wait for a load without waiting for the stores that follow it.
+constexpr uint32_t kNowhere = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t whole_memory(const void* from) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(from), 0, 0x7fffffff, 0x00020000);
+}
+
+// A tile of a chunk's rows on its way from memory to LDS.  Rows behind the segment's end and columns behind head_dim read as zeros
+// (an address outside the buffer resource), so that nothing behind a sequence ever meets a product.
+template <int D>
+struct TileLoad {
+    static constexpr int kThreadsHere = D / 32 * 64, kRowsPerPass = kThreadsHere / (D / 8), kPasses = kLinearChunk / kRowsPerPass;
+    u32x4 r[kPasses];
+    __device__ __forceinline__ void issue(const uint16_t* first_row, int64_t stride, int rows, int head_dim) {
+        const int row = threadIdx.x / (D / 8), col = threadIdx.x % (D / 8) * 8, there = col < head_dim ? rows : 0;
+        const uint32_t off = (uint32_t)(row * (int)stride + col) * 2u;
+        const __amdgpu_buffer_rsrc_t rsrc = whole_memory(first_row);
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i)
+            r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, row + i * kRowsPerPass < there ? off : kNowhere, i * kRowsPerPass * (int)stride * 2, 0);
+    }
+    // ends the life of what was put: a load that is not always made again would else keep its registers throughout the loop
+    __device__ __forceinline__ void drop() {
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) r[i] = u32x4{};
+    }
+    __device__ __forceinline__ void put(char* tile) const {
+        const int row = threadIdx.x / (D / 8), col = threadIdx.x % (D / 8) * 8;
+#pragma unroll
+        for (int i = 0; i < kPasses; ++i) *reinterpret_cast<u32x4*>(tile + tile_offset<D>(row + i * kRowsPerPass, col)) = r[i];
+    }
+};
+
+// The wave's 32 columns of a chunk's outputs: lane's token in a block of 32 along the columns of the accumulators, columns of the head along the rows.
+// row_stride: elements
+template <bool F32>
+__device__ __forceinline__ void store_rows(void* base, int64_t first, const f32x16 (&out)[2], int row_stride, int rows, int d, int wave, int lane) {
+    const __amdgpu_buffer_rsrc_t rsrc = whole_memory(static_cast<char*>(base) + first * (F32 ? 4 : 2));
+    const int row = lane & 31, col = wave * 32 + 4 * (lane >> 5);
+#pragma unroll
+    for (int tb = 0; tb < 2; ++tb) {
+        const uint32_t off = row + tb * 32 < rows ? (uint32_t)((row + tb * 32) * row_stride + col) * (F32 ? 4u : 2u) : kNowhere;
+#pragma unroll
+        for (int i4 = 0; i4 < 4; ++i4) {
+            const f32x4 x = {out[tb][4 * i4], out[tb][4 * i4 + 1], out[tb][4 * i4 + 2], out[tb][4 * i4 + 3]};
+            const uint32_t at = wave * 32 + 8 * i4 < d ? off + 8 * i4 * (F32 ? 4 : 2) : kNowhere;
+            if constexpr (F32) {
+                union { f32x4 f; u32x4 u; } y;
+                y.f = x;
+                __builtin_amdgcn_raw_buffer_store_b128(y.u, rsrc, at, 0, 0);
+            } else {
+                __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])}, rsrc, at, 0, 0);
+            }
+        }
+    }
+}
+
+// The wave's part of a state: columns 32 wave .. + 31 (of c) along the lanes, all D rows (of b) in registers; register i of
+// block db holds row 32 db + 16 (i / 8) + 8 (lane / 32) + i % 8.
+template <int D>
+struct State {
+    f32x16 x[D / 32];
+    __device__ __forceinline__ void clear(float value) {
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[db][i] = value;
+    }
+    // as `in memory`: [row][col], or [col][row]
+    __device__ __forceinline__ void load(const float* m, int d, bool transposed, int wave, int lane) {
+        const int col = wave * 32 + (lane & 31);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = db * 32 + h * 16 + (lane >> 5) * 8;
+                const bool there = row < d && col < d;
+                if (transposed) {
+                    f32x4 u{}, v{};
+                    if (there) {
+                        u = *reinterpret_cast<const f32x4*>(m + (int64_t)col * d + row);
+                        v = *reinterpret_cast<const f32x4*>(m + (int64_t)col * d + row + 4);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[db][8 * h + i] = u[i], x[db][8 * h + 4 + i] = v[i];
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[db][8 * h + i] = there ? m[(row + i) * d + col] : 0.f;
+                }
+            }
+    }
+    __device__ __forceinline__ void store(float* m, int d, int wave, int lane) const {
+        const int col = wave * 32 + (lane & 31);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = db * 32 + h * 16 + (lane >> 5) * 8;
+                if (row < d && col < d) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) m[(row + i) * d + col] = x[db][8 * h + i];
+                }
+            }
+    }
+    // this lane's share of the sum over all elements of this state times the one in memory
+    __device__ __forceinline__ float dot(const float* m, int d, bool transposed, int wave, int lane) const {
+        const int col = wave * 32 + (lane & 31);
+        float sum = 0.f;
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = db * 32 + h * 16 + (lane >> 5) * 8;
+                if (row < d && col < d) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) sum += x[db][8 * h + i] * (transposed ? m[(int64_t)col * d + row + i] : m[(row + i) * d + col]);
+                }
+            }
+        return sum;
+    }
+};
+
+// A hidden pair has the weight 0, and 0 times an infinity or NaN is NaN: sources that hold one are left out of the products, element by element, and
+// added for the targets that see them.
+__device__ __forceinline__ bool all_finite(const bf16x8 (&x)[4], const PairOps& ops) {
+    float zero[2] = {0.f, 0.f};              // 0 times an infinity or NaN is NaN
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+        union { bf16x8 v; u32x4 u; } c;
+        c.v = x[t];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) zero[i % 2] = PairOps::dot(c.u[i], ops.none, zero[i % 2]);
+    }
+    return !__any(zero[0] + zero[1] != 0.f);
+}
+__device__ __forceinline__ bf16x8 finite_part(bf16x8 x) {
+    union { bf16x8 v; u32x4 u; } c;
+    c.v = x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        c.u[i] = (c.u[i] & 0x7f80u) == 0x7f80u ? c.u[i] & 0xffff0000u : c.u[i];
+        c.u[i] = (c.u[i] & 0x7f800000u) == 0x7f800000u ? c.u[i] & 0xffffu : c.u[i];
+    }
+    return c.v;
+}
+
+// What the sources of the own chunk give: weights times c, (source block, target block) of 32 x 32 pairs by their number, see walk
+template <int D, bool LATER, int WEIGHT_PARTS>
+__device__ __forceinline__ void add_own_chunk(const char* lds, const bf16x8 (&sources)[4], int lane, f32x16 (&out)[2]) {
+    using L = Lds<D, WEIGHT_PARTS>;
+#pragma unroll
+    for (int part = 0; part < WEIGHT_PARTS; ++part)
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+            for (int blk = 0; blk < 3; ++blk) {
+                const int sb = LATER ? (blk > 0) : blk >> 1, tb = LATER ? blk >> 1 : (blk > 0);
+                out[tb] = mfma(sources[2 * sb + tt], *reinterpret_cast<const bf16x8*>(lds + L::weights(blk, tt, part) + lane * 16), out[tb]);
+            }
+}
+template <int D, bool LATER, int WEIGHT_PARTS>
+__device__ __forceinline__ void add_not_finite(const char* lds, int wave, int lane, f32x16 (&out)[2]) {
+    using L = Lds<D, WEIGHT_PARTS>;
+    const char* const tile = lds + L::kC;
+    const int t32 = lane & 31, hh = lane >> 5;
+#pragma unroll 1
+    for (int s = 0; s < kLinearChunk; ++s) {
+        const int sb = s / 32, r = s % 32;
+#pragma unroll
+        for (int tb = 0; tb < 2; ++tb) {
+            if (LATER ? sb < tb : sb > tb) continue;
+            const bool sees = sb != tb || (LATER ? r >= t32 : r <= t32);
+            // the weight of (s, t32) as it was laid out for the products: lane 32 (r / 4 % 2) + t32, element 4 (r / 8 % 2) + r % 4 of step r / 16
+            const char* const at = lds + L::weights(sb + tb, r / 16, 0) + (32 * (r / 4 % 2) + t32) * 16 + (4 * (r / 8 % 2) + r % 4) * 2;
+            float weight = 0.f;
+#pragma unroll
+            for (int part = 0; part < WEIGHT_PARTS; ++part) weight += (float)*reinterpret_cast<const __bf16*>(at + part * 1024);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int col = wave * 32 + 8 * (i / 4) + 4 * hh + i % 4;
+                const uint32_t raw = *reinterpret_cast<const uint16_t*>(tile + tile_offset<D>(s, col & ~3) + (col & 3) * 2);
+                if (sees && (raw & 0x7f80) == 0x7f80) out[tb][i] += weight * __uint_as_float(raw << 16);
+            }
+        }
+    }
+}
+
+// The state is held as 2^held times what the registers hold, and multiplied out when that is below 2^-16: decays near 1 cost no operation per element
+// and chunk.
+constexpr float kLeastHeld = -16.f;
+
+// Walks a segment's chunks, forwards or (LATER) backwards, with the state that reaches it in `S`.
+//   LATER   targets see the tokens from themselves on, and a KV head's sources are those of all its query heads (dk, dv); else they see the
+//           tokens up to themselves, and a KV head's targets are those of all its query heads (o, dq)
+//   OUT     outputs are wanted, not only the state
+//   DOTS    the dot products of the output with the tensor it is the gradient of, the part from the own chunk (without the token's own) and
+//           the part from the state apart
+//   ONE     a KV head has one query head
+//   PARTS, WEIGHT_PARTS   bf16 values that the state and its sources, and the weights of pairs, enter products as; three of the weights go with
+//           fp32 outputs, two with bf16
+// Returns the log2 of the segment's decay.
+template <int D, bool LATER, bool OUT, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS>
+__device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, const Segment& seg, int kv_head, char* lds, State<D>& S) {
+    constexpr bool OUT_F32 = WEIGHT_PARTS == 3;
+    using L = Lds<D, WEIGHT_PARTS>;
+    constexpr int kWaves = L::kWaves;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int d = p.shape.head_dim, group = ONE ? 1 : p.shape.group;
+    const int hh = lane >> 5;
+    TileReads<D> reads;
+    reads.init(lane);
+    PairOps ops;
+    ops.init();
+    char* const tile_a = lds + L::kA;
+    char* const tile_b = lds + L::kB;
+    char* const tile_c = lds + L::kC;
+    char* const tile_e = lds + L::kE;
+    float* const sums = reinterpret_cast<float*>(lds + L::kSums);
+    float* const in_weight = sums + kLinearChunk;
+    float* const out_weight = in_weight + kLinearChunk;
+    float* const whole = out_weight + kLinearChunk;
+    float* const near = reinterpret_cast<float*>(lds + L::kNear);
+    float* const far = reinterpret_cast<float*>(lds + L::kFar);
+
+    const int chunks = (seg.rows + kLinearChunk - 1) / kLinearChunk;
+    const int target_heads = LATER ? p.shape.kv_heads : p.shape.q_heads;
+    float all_decay = 0.f, held = 0.f;
+
+    TileLoad<D> la, lb, lc, le;
+    float next_g = 0.f;
+    const int first_target = LATER ? kv_head : kv_head * group, first_source = LATER ? kv_head * group : kv_head;
+    const uint16_t* const base_a = f.a + seg.start * f.a_stride + (int64_t)first_target * d;
+    const uint16_t* const base_e = f.e + seg.start * f.e_stride + (int64_t)first_target * d;
+    const uint16_t* const base_b = f.b + seg.start * f.b_stride + (int64_t)first_source * d;
+    const uint16_t* const base_c = f.c + seg.start * f.c_stride + (int64_t)first_source * d;
+    const float* const base_g = p.log_decay + seg.start * p.decay_stride + kv_head;
+    // the tiles of chunk number n of the walk and query head h of the group, if there is that chunk
+    auto issue = [&](int n, int h) {
+        const int chunk = LATER ? chunks - 1 - n : n;
+        const int first = n < chunks ? chunk * kLinearChunk : 0, rows = n < chunks ? seg.rows - first : 0;
+        if (OUT) {
+            if (ONE || !LATER || h == 0) {
+                la.issue(base_a + first * f.a_stride + h * d, f.a_stride, rows, d);
+                if (DOTS) le.issue(base_e + first * f.e_stride + h * d, f.e_stride, rows, d);
+            } else {
+                la.drop();
+                if (DOTS) le.drop();
+            }
+        }
+        if (ONE || LATER || h == 0) {
+            lb.issue(base_b + first * f.b_stride + h * d, f.b_stride, rows, d);
+            lc.issue(base_c + first * f.c_stride + h * d, f.c_stride, rows, d);
+        } else {
+            lb.drop();
+            lc.drop();
+        }
+        if (ONE || h == 0)
+            next_g = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(whole_memory(base_g + first * p.decay_stride),
+                                                                          lane < rows ? (uint32_t)(lane * (int)p.decay_stride * 4) : kNowhere, 0, 0));
+    };
+    auto issue_next = [&](int n, int h) {
+        if (h + 1 < group) issue(n, h + 1);
+        else issue(n + 1, 0);
+    };
+    if (chunks > 0) issue(0, 0);
+    for (int n = 0; n < chunks; ++n) {
+        const int chunk = LATER ? chunks - 1 - n : n;
+        const int first = chunk * kLinearChunk;
+        f32x16 out_of_heads[2];            // LATER: summed over the heads
+        float chunk_decay = 0.f;
+        for (int h = 0; h < group; ++h) {
+            f32x16 out_of_head[2];
+            f32x16 (&out)[2] = LATER ? out_of_heads : out_of_head;
+            const bool first_head = h == 0, last_head = h == group - 1;
+            int t32 = lane & 31;
+            asm volatile("" : "+v"(t32));      // (as reads.fresh(): or the mask of every hidden pair is kept in registers)
+            reads.fresh();
+            if (first_head && wave == kWaves - 1) {        // (the wave without a block of pairs)
+                const float sum = sum_up_to(lane < seg.rows - first ? decay_log2(next_g) : 0.f);
+                const float total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum), 63));
+                const float in = LATER ? total - sum : sum, out = LATER ? sum : total - sum;
+                const float next_held = held + total < kLeastHeld ? 0.f : held + total;
+                sums[lane] = sum;
+                in_weight[lane] = f.scale_in * fast_exp2(in + held);
+                out_weight[lane] = f.scale_state * fast_exp2(out - next_held);
+                if (lane == 0) whole[0] = total;
+            }
+            if (OUT && (!LATER || first_head)) {
+                la.put(tile_a);
+                if (DOTS) le.put(tile_e);
+            }
+            if (LATER || first_head) {
+                lb.put(tile_b);
+                lc.put(tile_c);
+            }
+            __syncthreads();
+            if (first_head) chunk_decay = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(whole[0])));
+
+            if (!OUT) issue_next(n, h);
+            if constexpr (OUT) {
+                // pairs of sources (along the rows) and targets (along the lanes): of the four blocks of 32 x 32, the three that are not all hidden
+#pragma unroll 1
+                for (int blk = wave; blk < 3; blk += kWaves) {
+                    const int sb = LATER ? (blk > 0) : blk >> 1, tb = LATER ? blk >> 1 : (blk > 0);
+                    f32x16 w{};
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) w = mfma(reads.along(tile_b, sb, kk), reads.along(tile_a, tb, kk), w);
+                    f32x16 y{};
+                    if constexpr (DOTS) {
+#pragma unroll
+                        for (int kk = 0; kk < D / 16; ++kk) y = mfma(reads.along(tile_c, sb, kk), reads.along(tile_e, tb, kk), y);
+                    }
+                    const float target_sum = LATER ? sums[tb * 32 + t32] - p.scale_log2 : sums[tb * 32 + t32] + p.scale_log2;
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const f32x4 source_sum = *reinterpret_cast<const f32x4*>(sums + sb * 32 + 8 * i4 + 4 * hh);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[4 * i4 + j] *= fast_exp2(LATER ? source_sum[j] - target_sum : target_sum - source_sum[j]);
+                    }
+                    if (sb == tb) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int s = 8 * (i / 4) + 4 * hh + i % 4;
+                            w[i] = (LATER ? s < t32 : s > t32) ? 0.f : w[i];
+                            if constexpr (DOTS) y[i] = (LATER ? s <= t32 : s >= t32) ? 0.f : y[i];
+                        }
+                    }
+                    if constexpr (DOTS) {
+                        float dot = 0.f;
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) dot += w[i] * y[i];
+                        dot += partner32(dot);
+                        if (lane < 32) near[blk * 32 + lane] = LATER && !first_head ? near[blk * 32 + lane] + dot : dot;
+                    }
+#pragma unroll
+                    for (int tt = 0; tt < 2; ++tt) {
+                        Parts<WEIGHT_PARTS> parts;
+                        f32x8 x;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = w[8 * tt + i];
+                        parts.of(x, ops);
+#pragma unroll
+                        for (int part = 0; part < WEIGHT_PARTS; ++part)
+                            *reinterpret_cast<bf16x8*>(lds + L::weights(0, tt, part) + blk * (2 * WEIGHT_PARTS * 1024) + lane * 16) = parts.part[part];
+                    }
+                }
+                issue_next(n, h);      // (in front of the pairs they would take registers that these need)
+                // what the state gives to the targets
+                if (!LATER || first_head) {
+                    out[0] = out[1] = f32x16{};
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk) {
+                        Parts<PARTS> parts;
+                        f32x8 x;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = S.x[kk / 2][8 * (kk % 2) + i];
+                        parts.template of<true>(x, ops);       // (the state's last products are two barriers behind)
+                        const bf16x8 a[2] = {reads.along(tile_a, 0, kk), reads.along(tile_a, 1, kk)};
+#pragma unroll
+                        for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                            for (int tb = 0; tb < 2; ++tb) out[tb] = mfma(parts.part[part], a[tb], out[tb]);
+                    }
+#pragma unroll
+                    for (int tb = 0; tb < 2; ++tb) {
+                        const float weight = in_weight[tb * 32 + t32];
+                        float dot = 0.f;
+#pragma unroll
+                        for (int i4 = 0; i4 < 4; ++i4) {
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) out[tb][4 * i4 + j] *= weight;
+                            if constexpr (DOTS) {
+                                const u32x2 e = *reinterpret_cast<const u32x2*>(tile_e + tile_offset<D>(tb * 32 + t32, wave * 32 + 8 * i4 + 4 * hh));
+                                dot += out[tb][4 * i4] * __uint_as_float(e[0] << 16) + out[tb][4 * i4 + 1] * __uint_as_float(e[0] & 0xffff0000u) +
+                                       out[tb][4 * i4 + 2] * __uint_as_float(e[1] << 16) + out[tb][4 * i4 + 3] * __uint_as_float(e[1] & 0xffff0000u);
+                            }
+                        }
+                        if constexpr (DOTS) {
+                            dot += partner32(dot);
+                            if (lane < 32) far[wave * kLinearChunk + tb * 32 + lane] = dot;
+                        }
+                    }
+                }
+                __syncthreads();
+            }
+
+            if constexpr (OUT) {
+                bf16x8 sources[4];     // c, 16 sources at a time down the operand's k
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sources[t] = reads.down(tile_c, wave, t);
+                const bool finite = all_finite(sources, ops);
+                if (!finite) {
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) sources[t] = finite_part(sources[t]);
+                }
+                add_own_chunk<D, LATER, WEIGHT_PARTS>(lds, sources, lane, out);
+                if (!finite) add_not_finite<D, LATER, WEIGHT_PARTS>(lds, wave, lane, out);
+                if (!LATER || last_head) {
+                    const int64_t at = (int64_t)(seg.start + first) * target_heads + (LATER ? kv_head : kv_head * group + h);
+                    store_rows<OUT_F32>(f.out, at * d, out, target_heads * d, seg.rows - first, d, wave, lane);
+                }
+                if constexpr (DOTS) {
+                    if (!LATER || last_head) {
+                        const int64_t at = (int64_t)(LATER ? kv_head : kv_head * group + h) * p.shape.total_rows + seg.start + first;
+                        // blocks 0 | 1, 2 of the pairs have targets 0 .. 31 | 32 .. 63, or (LATER) 0, 1 | 2
+                        const float near_sum = LATER ? (lane < 32 ? near[lane] + near[32 + lane] : near[32 + lane])
+                                                     : (lane < 32 ? near[lane] : near[lane] + near[32 + lane]);
+                        float far_sum = 0.f;
+#pragma unroll
+                        for (int w = 0; w < kWaves; ++w) far_sum += far[w * kLinearChunk + lane];
+                        const uint32_t off = wave == 0 && lane < seg.rows - first ? lane * 4 : kNowhere;
+                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(near_sum), whole_memory(f.near + at), off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(far_sum), whole_memory(f.far + at), off, 0, 0);
+                    }
+                }
+            }
+            if (LATER || last_head) {
+                if ((!LATER || first_head) && held + chunk_decay < kLeastHeld) {
+                    const float left = fast_exp2(held + chunk_decay);
+#pragma unroll
+                    for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) S.x[db][i] *= left;
+                }
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const f32x4 w0 = *reinterpret_cast<const f32x4*>(out_weight + 16 * t + 4 * hh);
+                    const f32x4 w1 = *reinterpret_cast<const f32x4*>(out_weight + 16 * t + 8 + 4 * hh);
+                    union { bf16x8 v; u32x4 u; } c;
+                    c.v = reads.down(tile_c, wave, t);
+                    f32x8 x;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x[2 * i] = __uint_as_float(c.u[i] << 16) * (i < 2 ? w0[2 * i] : w1[2 * i - 4]);
+                        x[2 * i + 1] = __uint_as_float(c.u[i] & 0xffff0000u) * (i < 2 ? w0[2 * i + 1] : w1[2 * i - 3]);
+                    }
+                    Parts<PARTS> parts;
+                    parts.of(x, ops);
+                    bf16x8 rows[D / 32];
+#pragma unroll
+                    for (int db = 0; db < D / 32; ++db) rows[db] = reads.down_ordered(tile_b, db, t);
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part)
+#pragma unroll
+                        for (int db = 0; db < D / 32; ++db) S.x[db] = mfma(rows[db], parts.part[part], S.x[db]);
+                }
+            }
+            __syncthreads();
+        }
+        all_decay += chunk_decay;
+        held = held + chunk_decay < kLeastHeld ? 0.f : held + chunk_decay;
+    }
+    if (held != 0.f) {
+        const float left = fast_exp2(held);
+#pragma unroll
+        for (int db = 0; db < D / 32; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) S.x[db][i] *= left;
+    }
+    return all_decay;
+}
+
+// the state at a segment's start (LATER: the gradient at its end) as it lies in memory; NULL: zeros.  *bad: it is one that does not exist
+template <bool LATER>
+__device__ __forceinline__ const float* reaching_state(const LinearParams& p, const Segment& seg, int kv_head, bool* bad) {
+    const int d = p.shape.head_dim;
+    *bad = false;
+    if (seg.count > 1) return (LATER ? p.d_states : p.states) + ((int64_t)(seg.entry + seg.index) * p.shape.kv_heads + kv_head) * d * d;
+    bool exists;
+    const float* m = state_of(LATER ? p.final : p.initial, seg.seq, kv_head, d, &exists);
+    *bad = exists && m == nullptr;
+    return m;
+}
+
+template <int D, bool LATER, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS>
+__device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine& f, const Segment& seg, int slot, int kv_head, char* lds) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = p.shape.head_dim;
+    State<D> S;
+    bool bad;
+    const float* const from = reaching_state<LATER>(p, seg, kv_head, &bad);
+    if (from) S.load(from, d, f.transposed, wave, lane);
+    else S.clear(bad ? __builtin_nanf("") : 0.f);
+    walk<D, LATER, true, DOTS, ONE, PARTS, WEIGHT_PARTS>(p, f, seg, kv_head, lds, S);
+    if (!LATER && DOTS) {
+        // <S, dS> behind the segment's last token: what the gradient of its decays starts from
+        const float* const d_end = reaching_state<true>(p, seg, kv_head, &bad);
+        float sum = d_end ? wave_sum(S.dot(d_end, d, f.transposed, wave, lane)) : 0.f;
+        float* const parts = reinterpret_cast<float*>(lds);
+        if (lane == 0) parts[wave] = sum;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            sum = 0.f;
+            for (int w = 0; w < D / 32; ++w) sum += parts[w];
+            p.across[(int64_t)slot * p.shape.kv_heads + kv_head] = sum;
+        }
+    }
+    if (!DOTS && !f.transposed) {
+        float* to = nullptr;
+        if (LATER) {
+            if (seg.index == 0 && p.d_initial) to = p.d_initial + ((int64_t)seg.seq * p.shape.kv_heads + kv_head) * d * d;
+        } else if (seg.index == seg.count - 1) {
+            bool exists;
+            to = state_of(p.final, seg.seq, kv_head, d, &exists);
+        }
+        if (to) S.store(to, d, wave, lane);
+    }
+}
+
+// what a workgroup works on: item -> (role, KV head, slot), roles innermost
+__device__ __forceinline__ bool item_of_block(const LinearShape& shape, int roles, int& role, int& kv_head, int& slot) {
+    const int64_t items = (int64_t)shape.slots * shape.kv_heads * roles, item = linear_item(blockIdx.x, items);
+    if ((int64_t)blockIdx.x / 8 >= linear_share(items) || item >= items) return false;
+    role = (int)(item % roles);
+    kv_head = (int)(item / roles % shape.kv_heads);
+    slot = (int)(item / roles / shape.kv_heads);
+    return true;
+}
+
+__device__ __forceinline__ Routine forward_routine(const LinearParams& p) {
+    return Routine{p.q, p.k, p.v, nullptr, p.q_stride, p.kv_stride, p.kv_stride, 0, p.scale, 1.f, p.o, false, nullptr, nullptr};
+}
+__device__ __forceinline__ Routine dq_routine(const LinearParams& p) {
+    return Routine{p.d_o, p.v, p.k, p.q, p.do_stride, p.kv_stride, p.kv_stride, p.q_stride, p.scale, 1.f, p.dq, true, p.q_near, p.q_far};
+}
+__device__ __forceinline__ Routine dk_routine(const LinearParams& p) {
+    return Routine{p.v, p.d_o, p.q, p.k, p.kv_stride, p.do_stride, p.q_stride, p.kv_stride, 1.f, p.scale, p.dk, true, p.k_near, p.k_far};
+}
+__device__ __forceinline__ Routine dv_routine(const LinearParams& p) {
+    return Routine{p.k, p.q, p.d_o, nullptr, p.kv_stride, p.q_stride, p.do_stride, 0, 1.f, p.scale, p.dv, false, nullptr, nullptr};
+}
+
+unsigned grid_of(const LinearParams& p, int roles) { return (unsigned)(8 * linear_share((int64_t)p.shape.slots * p.shape.kv_heads * roles)); }
+
+}  // namespace
+}  // namespace hspmd
