@@ -10,7 +10,7 @@ __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2)
     __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS>::bytes(true, true)];
     int role, kv_head, slot;
     Segment seg;
-    if (!item_of_block(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
+    if (!item_of_block<true>(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
     if (role == 0) outputs_of<D, false, true, ONE, 3, WEIGHT_PARTS>(p, dq_routine(p), seg, slot, kv_head, lds);
     else if (role == 1) outputs_of<D, true, true, ONE, 3, WEIGHT_PARTS>(p, dk_routine(p), seg, slot, kv_head, lds);
     else outputs_of<D, true, false, ONE, 3, WEIGHT_PARTS>(p, dv_routine(p), seg, slot, kv_head, lds);

@@ -9,7 +9,7 @@ __global__ __launch_bounds__(D / 32 * 64, 2) void linear_fwd_kernel(LinearParams
     __shared__ __align__(16) char lds[Lds<D, 2>::bytes(true, false)];
     int role, kv_head, slot;
     Segment seg;
-    if (!item_of_block(p.shape, 1, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
+    if (!item_of_block<true>(p.shape, 1, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
     outputs_of<D, false, false, ONE, PARTS, 2>(p, forward_routine(p), seg, slot, kv_head, lds);
 }
 

@@ -397,6 +397,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                 issue_next(n, h);      // (in front of the pairs they would take registers that these need)
                 // what the state gives to the targets
                 if (!LATER || first_head) {
+                    __builtin_amdgcn_s_setprio(1);     // (products before the other workgroup's vector operations)
                     out[0] = out[1] = f32x16{};
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk) {
@@ -411,6 +412,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
 #pragma unroll
                             for (int tb = 0; tb < 2; ++tb) out[tb] = mfma(parts.part[part], a[tb], out[tb]);
                     }
+                    __builtin_amdgcn_s_setprio(0);
 #pragma unroll
                     for (int tb = 0; tb < 2; ++tb) {
                         const float weight = in_weight[tb * 32 + t32];
@@ -472,6 +474,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
 #pragma unroll
                         for (int i = 0; i < 16; ++i) S.x[db][i] *= left;
                 }
+                __builtin_amdgcn_s_setprio(1);
 #pragma unroll
                 for (int t = 0; t < 4; ++t) {
                     const f32x4 w0 = *reinterpret_cast<const f32x4*>(out_weight + 16 * t + 4 * hh);
@@ -494,6 +497,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
 #pragma unroll
                         for (int db = 0; db < D / 32; ++db) S.x[db] = mfma(rows[db], parts.part[part], S.x[db]);
                 }
+                __builtin_amdgcn_s_setprio(0);
             }
             __syncthreads();
         }
@@ -556,10 +560,14 @@ __device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine&
     }
 }
 
-// what a workgroup works on: item -> (role, KV head, slot), roles innermost
+// what a workgroup works on: item -> (role, KV head, slot), roles innermost.  LAST_FIRST: the last slots start first, whose keys and values the launch in
+// front has read last
+template <bool LAST_FIRST = false>
 __device__ __forceinline__ bool item_of_block(const LinearShape& shape, int roles, int& role, int& kv_head, int& slot) {
-    const int64_t items = (int64_t)shape.slots * shape.kv_heads * roles, item = linear_item(blockIdx.x, items);
+    const int64_t items = (int64_t)shape.slots * shape.kv_heads * roles;
+    int64_t item = linear_item(blockIdx.x, items);
     if ((int64_t)blockIdx.x / 8 >= linear_share(items) || item >= items) return false;
+    if (LAST_FIRST) item = items - 1 - item;
     role = (int)(item % roles);
     kv_head = (int)(item / roles % shape.kv_heads);
     slot = (int)(item / roles / shape.kv_heads);
