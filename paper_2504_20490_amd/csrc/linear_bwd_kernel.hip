@@ -16,25 +16,28 @@ __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2)
     else outputs_of<D, true, false, ONE, 3, WEIGHT_PARTS>(p, dv_routine(p), seg, slot, kv_head, lds);
 }
 
-// Gradients of the log decays, one wave per segment and KV head, from its last chunk to its first.  g_t weighs every pair of a token from t on
-// and one before t.  Of these pairs, a chunk's own and those with a token on one side of the chunk come from the dot products;
+// Gradients of the log decays, a workgroup per segment and KV head, from its last chunk to its first, a chunk per wave.  g_t weighs every pair of a
+// token from t on and one before t.  Of these pairs, a chunk's own and those with a token on one side of the chunk come from the dot products;
 // those across the whole chunk, <e^{G_L} S, R>, are what is left of <S, dS> at its end without its own keys.
-__global__ __launch_bounds__(64) void linear_decay_kernel(LinearParams p) {
+constexpr int kDecayWaves = 4;
+__global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearParams p) {
+    __shared__ float keys[kDecayWaves], queries[kDecayWaves], dead[kDecayWaves], totals[kDecayWaves];
     const LinearShape& sh = p.shape;
     int role, kv_head, slot;
     if (!item_of_block(sh, 1, role, kv_head, slot)) return;
-    const int lane = threadIdx.x & 63;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t item = (int64_t)slot * sh.kv_heads + kv_head;
     const bool fixed = p.decay_stride == 0;
     Segment seg;
     if (!find_segment(sh, slot, seg)) {
-        if (fixed && lane == 0) p.decay_sums[item] = 0.f;
+        if (fixed && threadIdx.x == 0) p.decay_sums[item] = 0.f;
         return;
     }
     float across = p.across[item], total = 0.f;
-    for (int chunk = (seg.rows + kLinearChunk - 1) / kLinearChunk - 1; chunk >= 0; --chunk) {
+    for (int last = (seg.rows + kLinearChunk - 1) / kLinearChunk - 1; last >= 0; last -= kDecayWaves) {
+        const int chunk = last - wave;
         const int64_t row = seg.start + chunk * kLinearChunk + lane;
-        const bool there = chunk * kLinearChunk + lane < seg.rows;
+        const bool there = chunk >= 0 && chunk * kLinearChunk + lane < seg.rows;
         float near = 0.f, far_q = 0.f, far_k = 0.f, g = 0.f;
         if (there) {
             g = decay_log2(p.log_decay[row * p.decay_stride + kv_head]);
@@ -46,20 +49,33 @@ __global__ __launch_bounds__(64) void linear_decay_kernel(LinearParams p) {
             }
             near -= p.k_near[(int64_t)kv_head * sh.total_rows + row];
         }
-        const float all_k = wave_sum(far_k);
-        // (a decay that leaves nothing leaves no pairs across it either, not even rounding errors)
-        const float whole = fast_exp2(wave_sum(g)) == 0.f ? 0.f : across - all_k;
-        const float later = sum_from(near + far_q, lane);
-        const float grad = later + (sum_up_to(far_k) - far_k) + whole;
+        const float all_k = wave_sum(far_k), all_q = wave_sum(far_q), all_g = wave_sum(g);
+        __syncthreads();                       // (the others have read the round before)
+        if (lane == 0) {
+            keys[wave] = all_k;
+            queries[wave] = all_q;
+            // a decay that leaves nothing leaves no pairs across it either, not even rounding errors
+            dead[wave] = fast_exp2(all_g) == 0.f ? 1.f : 0.f;
+        }
+        __syncthreads();
+        float whole = 0.f, mine = 0.f;
+#pragma unroll
+        for (int w = 0; w < kDecayWaves; ++w) {
+            whole = dead[w] != 0.f ? 0.f : across - keys[w];
+            if (w == wave) mine = whole;
+            across = whole + queries[w];
+        }
+        const float grad = sum_from(near + far_q, lane) + (sum_up_to(far_k) - far_k) + mine;
         if (there) {
             if (fixed) total += grad;
             else p.d_log_decay[row * sh.kv_heads + kv_head] = grad;
         }
-        across = whole + wave_sum(far_q);
     }
     if (fixed) {
         total = wave_sum(total);
-        if (lane == 0) p.decay_sums[item] = total;
+        if (lane == 0) totals[wave] = total;
+        __syncthreads();
+        if (threadIdx.x == 0) p.decay_sums[item] = totals[0] + totals[1] + totals[2] + totals[3];
     }
 }
 
@@ -90,7 +106,7 @@ hipError_t launch_linear_bwd(const LinearParams& p, hipStream_t stream) {
         else one ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
     }
     if (p.d_log_decay) {
-        if (p.shape.slots > 0) linear_decay_kernel<<<grid_of(p, 1), 64, 0, stream>>>(p);
+        if (p.shape.slots > 0) linear_decay_kernel<<<grid_of(p, 1), kDecayWaves * 64, 0, stream>>>(p);
         if (p.decay_stride == 0) linear_decay_sum_kernel<<<(unsigned)p.shape.kv_heads, 256, 0, stream>>>(p);
     }
     return hipGetLastError();

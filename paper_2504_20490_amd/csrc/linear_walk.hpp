@@ -254,6 +254,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
     constexpr bool OUT_F32 = WEIGHT_PARTS == 3;
     using L = Lds<D, WEIGHT_PARTS>;
     constexpr int kWaves = L::kWaves;
+    constexpr bool kEarly = !DOTS || ONE;      // when the next tiles are loaded: four of them, beside outputs kept over several heads, are too many
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int d = p.shape.head_dim, group = ONE ? 1 : p.shape.group;
     const int hh = lane >> 5;
@@ -394,7 +395,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                             *reinterpret_cast<bf16x8*>(lds + L::weights(0, tt, part) + blk * (2 * WEIGHT_PARTS * 1024) + lane * 16) = parts.part[part];
                     }
                 }
-                issue_next(n, h);      // (in front of the pairs they would take registers that these need)
+                if (kEarly) issue_next(n, h);      // (in front of the pairs they would take registers that these need)
                 // what the state gives to the targets
                 if (!LATER || first_head) {
                     __builtin_amdgcn_s_setprio(1);     // (products before the other workgroup's vector operations)
@@ -466,6 +467,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                     }
                 }
             }
+            if (OUT && !kEarly) issue_next(n, h);
             if (LATER || last_head) {
                 if ((!LATER || first_head) && held + chunk_decay < kLeastHeld) {
                     const float left = fast_exp2(held + chunk_decay);
