@@ -80,8 +80,9 @@ __device__ __forceinline__ bool find_segment(const LinearShape& p, int slot, Seg
         out.index = slot - linear_first_slot(r.start, seq, p.seg_rows);
         if (out.index < 0 || out.index >= out.count) return false;
         out.entry = linear_first_entry(r.start, p.seg_rows);
-        out.start = r.start + out.index * p.seg_rows;
-        out.rows = min(r.n - out.index * p.seg_rows, p.seg_rows);
+        const int rows = linear_segment_rows(r.n, out.count);
+        out.start = r.start + out.index * rows;
+        out.rows = min(r.n - out.index * rows, rows);
     }
     return true;
 }

@@ -23,11 +23,15 @@ HSPMD_LINEAR_INDEX LinearRows linear_rows(int cu, int cu_next, int total_rows) {
     return LinearRows{start, end - start};
 }
 
-// A sequence is cut into segments of seg_rows tokens (a multiple of the chunk), at least one.  Segment b of sequence s is slot
+// A sequence is cut into segments of at most seg_rows tokens (a multiple of the chunk, at least four), as few as that takes, of equal length in chunks but
+// for the last, which is never empty; at least one.  Segment b of sequence s is slot
 // start / seg_rows + s + b of the launch: the next sequence's first slot, (start + n) / seg_rows + s + 1, is never less than that of the
 // last segment plus one, so every slot is taken once at most, by a rule that needs no sums over the sequences.
 HSPMD_LINEAR_INDEX int linear_first_slot(int start, int seq, int seg_rows) { return start / seg_rows + seq; }
 HSPMD_LINEAR_INDEX int linear_segments(int n, int seg_rows) { return n <= seg_rows ? 1 : (n + seg_rows - 1) / seg_rows; }
+HSPMD_LINEAR_INDEX int linear_segment_rows(int n, int count) {
+    return ((n + kLinearChunk - 1) / kLinearChunk + count - 1) / count * kLinearChunk;
+}
 HSPMD_LINEAR_INDEX int64_t linear_slots(int64_t total_rows, int64_t num_seqs, int64_t seg_rows) { return total_rows / seg_rows + num_seqs; }
 
 // Sequences of several segments have an entry in the workspace for each (the state that reaches it): from 2 start / seg_rows on.  With n >
@@ -39,9 +43,13 @@ HSPMD_LINEAR_INDEX int64_t linear_entries(int64_t total_rows, int64_t seg_rows) 
 // starts there; windows are what the launch that passes states from segment to segment goes by.
 HSPMD_LINEAR_INDEX int64_t linear_windows(int64_t total_rows, int64_t seg_rows) { return total_rows / seg_rows + 1; }
 
-// Workgroups go to the 8 XCDs in turn; a range of consecutive items per XCD keeps the heads of a segment, which share lines of the decays
-// and the edges of rows, in one L2.  The grid is 8 * linear_share(items); items from `items` on are none.
-HSPMD_LINEAR_INDEX int64_t linear_share(int64_t items) { return (items + 7) / 8; }
-HSPMD_LINEAR_INDEX int64_t linear_item(int64_t block, int64_t items) { return block % 8 * linear_share(items) + block / 8; }
+// Workgroups go to the 8 XCDs in turn.  Items do so four heads at a time (`granule` items: four heads, all that is computed for them): neighbouring heads share
+// lines of the decays and the edges of rows, which then meet in one L2, and every XCD has as many items as another but for one granule.  (All heads of a slot
+// on one XCD, ranges of slots, left some with a round of workgroups more.)  The grid is 8 * granule * rounds; items from `items` on are none.
+HSPMD_LINEAR_INDEX int64_t linear_grid(int64_t items, int granule) { return (items + 8 * granule - 1) / (8 * granule) * 8 * granule; }
+HSPMD_LINEAR_INDEX int64_t linear_item(int64_t block, int granule) {
+    const int64_t i = block / 8;
+    return (i / granule * 8 + block % 8) * granule + i % granule;
+}
 
 }  // namespace hspmd

@@ -567,8 +567,8 @@ __device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine&
 template <bool LAST_FIRST = false>
 __device__ __forceinline__ bool item_of_block(const LinearShape& shape, int roles, int& role, int& kv_head, int& slot) {
     const int64_t items = (int64_t)shape.slots * shape.kv_heads * roles;
-    int64_t item = linear_item(blockIdx.x, items);
-    if ((int64_t)blockIdx.x / 8 >= linear_share(items) || item >= items) return false;
+    int64_t item = linear_item(blockIdx.x, 4 * roles);
+    if (item >= items) return false;
     if (LAST_FIRST) item = items - 1 - item;
     role = (int)(item % roles);
     kv_head = (int)(item / roles % shape.kv_heads);
@@ -589,7 +589,7 @@ __device__ __forceinline__ Routine dv_routine(const LinearParams& p) {
     return Routine{p.k, p.q, p.d_o, nullptr, p.kv_stride, p.q_stride, p.do_stride, 0, 1.f, p.scale, p.dv, false, nullptr, nullptr};
 }
 
-unsigned grid_of(const LinearParams& p, int roles) { return (unsigned)(8 * linear_share((int64_t)p.shape.slots * p.shape.kv_heads * roles)); }
+unsigned grid_of(const LinearParams& p, int roles) { return (unsigned)linear_grid((int64_t)p.shape.slots * p.shape.kv_heads * roles, 4 * roles); }
 
 }  // namespace
 }  // namespace hspmd

@@ -22,6 +22,8 @@ extern "C" int check(const int* cu, int num_seqs, int total_rows, int seg, int s
         const int count = linear_segments(r.n, seg), first = linear_first_slot(r.start, s, seg), entry = linear_first_entry(r.start, seg);
         if (count < 1 || (long)count * seg < r.n || (count > 1 && (long)(count - 1) * seg >= r.n)) return __LINE__;
         if (entry < 0 || (count > 1 && entry + count > entries)) return __LINE__;
+        const int rows = linear_segment_rows(r.n, count);
+        if (rows > seg || (r.n > 0 && ((long)(count - 1) * rows >= r.n || (long)count * rows < r.n || rows % kLinearChunk))) return __LINE__;
         if (!sane) continue;
         for (int b = 0; b < count; ++b) {
             if (first + b >= slots || slot_of[first + b] >= 0) return __LINE__;
@@ -45,12 +47,11 @@ extern "C" int check(const int* cu, int num_seqs, int total_rows, int seg, int s
     }
     return 0;
 }
-extern "C" int check_items(long items) {
+extern "C" int check_items(long items, int granule) {
     std::vector<char> met(items, 0);
-    const long share = linear_share(items);
     long n = 0;
-    for (long b = 0; b < 8 * share; ++b) {
-        const long i = linear_item(b, items);
+    for (long b = 0; b < linear_grid(items, granule); ++b) {
+        const long i = linear_item(b, granule);
         if (i < 0) return __LINE__;
         if (i >= items) continue;
         if (met[i]++) return __LINE__;
@@ -67,7 +68,7 @@ def lib(tmp_path_factory):
     (d / "shim.cpp").write_text(SHIM)
     subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wall", "-Werror", f"-I{lib_build.CSRC}", "-o", str(d / "shim.so"), str(d / "shim.cpp")], check=True)
     so = ctypes.CDLL(str(d / "shim.so"))
-    so.check_items.argtypes = [ctypes.c_long]
+    so.check_items.argtypes = [ctypes.c_long, ctypes.c_int]
     return so
 
 
@@ -78,7 +79,7 @@ def check(lib, cu, total, seg, sane=True):
 def test_every_segment_has_a_place_of_its_own(lib):
     rng = random.Random(1)
     for _ in range(3000):
-        seg = 64 * rng.randint(1, 20)
+        seg = 64 * rng.randint(4, 20)
         lengths = [rng.choice([0, 1, seg - 1, seg, seg + 1, 2 * seg, 2 * seg + 1, rng.randint(0, 5 * seg)]) for _ in range(rng.randint(1, 12))]
         cu = [0]
         for n in lengths:
@@ -89,17 +90,18 @@ def test_every_segment_has_a_place_of_its_own(lib):
 def test_nothing_in_cu_rows_leads_out(lib):
     rng = random.Random(2)
     for _ in range(3000):
-        seg, total = 64 * rng.randint(1, 20), rng.randint(0, 20000)
+        seg, total = 64 * rng.randint(4, 20), rng.randint(0, 20000)
         cu = [rng.choice([0, total, rng.randint(-5, total + 5), -2 ** 31, 2 ** 31 - 1, rng.randint(-2 ** 31, 2 ** 31 - 1)]) for _ in range(rng.randint(2, 12))]
         assert check(lib, cu, total, seg, False) == 0, (cu, total, seg)
 
 
 def test_the_largest_counts_fit(lib):
     top = 1 << 25
-    assert check(lib, [0, top], top, 64) == 0
+    assert check(lib, [0, top], top, 256) == 0
     assert check(lib, [0, 5, top - 7, top], top, 256) == 0
 
 
 @pytest.mark.parametrize("items", [0, 1, 7, 8, 9, 100, 1001, 65536])
 def test_items_are_dealt_out_once(lib, items):
-    assert lib.check_items(items) == 0
+    for granule in (4, 8, 12):
+        assert lib.check_items(items, granule) == 0
