@@ -578,7 +578,7 @@ def _rows_stride(x, heads: int, head_dim: int, dtype, what: str, tokens: int) ->
     """The token stride of a [tokens, heads, head_dim] tensor of the given type whose rows are contiguous."""
     if (tokens | heads) >> 31 > 0:
         raise _bad(f"{what}: its tokens or heads do not fit 32 bits")
-    if x.dtype is not dtype or tuple(x.shape) != (tokens, heads, head_dim):
+    if x.dtype is not dtype or x.shape != (tokens, heads, head_dim):
         raise _bad(f"{what} has to be [{tokens}, {heads}, {head_dim}] of {dtype}")
     s = x.stride()
     if (s[2] != 1 or s[1] != head_dim and heads > 1) and x.numel():
@@ -800,25 +800,23 @@ class LinearBatch:
 
     def __init__(self, cu_rows=None, max_rows: int = 0, initial_slots=None, final_slots=None):
         import torch
-        self.tensors = tuple(x for x in (cu_rows, initial_slots, final_slots) if x is not None)   # (kept alive)
-        if any(x.dtype is not torch.int32 or not x.is_contiguous() or x.dim() != 1 for x in self.tensors):
-            raise _bad("cu_rows and the slots have to be contiguous int32 tensors of one dimension")
-        self.num_seqs = None
-        if cu_rows is not None:
-            self.num_seqs = cu_rows.numel() - 1
-            if self.num_seqs < 0:
-                raise _bad("cu_rows has to have one entry more than there are sequences")
-            _count(self.num_seqs, "num_seqs")
-        for x in (initial_slots, final_slots):
-            if x is not None:
-                if self.num_seqs is not None and x.numel() != self.num_seqs:
-                    raise _bad("the slots have to have one entry per sequence")
-                self.num_seqs = x.numel()
-        self.max_rows = _count(max_rows, "max_rows")
-        self.has_cu = cu_rows is not None
-        self.devices = tuple(x.get_device() for x in self.tensors)
-        where = lambda x: None if x is None else x.data_ptr() or None
-        self._pointers = (where(cu_rows), where(initial_slots), where(final_slots))
+        i32, n, pointers, devices = torch.int32, None, [], []
+        for x in (cu_rows, initial_slots, final_slots):
+            if x is None:
+                pointers.append(None)
+                continue
+            if x.dtype is not i32 or x.dim() != 1 or not x.is_contiguous():
+                raise _bad("cu_rows and the slots have to be contiguous int32 tensors of one dimension")
+            count = x.shape[0] - (x is cu_rows)
+            if n is not None and count != n or count < 0:
+                raise _bad("cu_rows has to have one entry more than there are sequences, the slots as many")
+            n = count
+            pointers.append(x.data_ptr() or None)
+            devices.append(x.get_device())
+        self.num_seqs = n if n is None else _count(n, "num_seqs")
+        self.max_rows, self.has_cu = _count(max_rows, "max_rows"), cu_rows is not None
+        self.tensors = (cu_rows, initial_slots, final_slots)      # (kept alive)
+        self.devices, self._pointers = devices, pointers
 
     def _args(self, rows: int, q_heads: int, kv_heads: int, head_dim: int):
         n = rows if self.num_seqs is None else self.num_seqs
@@ -830,18 +828,20 @@ def _linear_states(x, kv_heads: int, d: int, what: str, devices: list):
     import torch
     if x is None:
         return None
-    if x.dtype is not torch.float32 or x.dim() != 4 or tuple(x.shape[1:]) != (kv_heads, d, d):
+    shape, inner = x.shape, (d * d, d, 1)
+    if x.dtype is not torch.float32 or len(shape) != 4 or shape[1:] != (kv_heads, d, d):
         raise _bad(f"{what} has to be [num_slots, {kv_heads}, {d}, {d}] of torch.float32")
-    if any(a != b and n > 1 for a, b, n in zip(x.stride()[1:], (d * d, d, 1), x.shape[1:])):
+    s = x.stride()
+    if s[1:] != inner and any(a != b and n > 1 for a, b, n in zip(s[1:], inner, shape[1:])):
         raise _bad(f"{what}: the heads, rows and columns of a slot have to be contiguous")
     devices.append(x.get_device())
-    return ctypes.byref(_LinearStatesArgs(x.data_ptr(), x.stride(0) if x.shape[0] > 1 else kv_heads * d * d, _count(x.shape[0], "num_slots")))
+    return ctypes.byref(_LinearStatesArgs(x.data_ptr(), s[0] if shape[0] > 1 else kv_heads * d * d, _count(shape[0], "num_slots")))
 
 
 def _linear_dense(x, shape, dtype, what: str, devices: list):
     if x is None:
         return None
-    if tuple(x.shape) != tuple(shape) or x.dtype is not dtype or not x.is_contiguous():
+    if x.shape != shape or x.dtype is not dtype or not x.is_contiguous():
         raise _bad(f"{what} has to be a contiguous tensor {list(shape)} of {dtype}")
     devices.append(x.get_device())
     return x.data_ptr()
@@ -857,10 +857,10 @@ def _linear_rows(batch: LinearBatch, q, k, v, log_decay):
     qs, ks = _rows_stride(q, hq, d, bf16, "q", T), _rows_stride(k, hkv, d, bf16, "k", T)
     if _rows_stride(v, hkv, d, bf16, "v", T) != ks:
         raise _bad("k and v have to have the same token stride")
-    fixed = log_decay.dim() == 1
-    if log_decay.dtype is not torch.float32 or tuple(log_decay.shape) != ((hkv,) if fixed else (T, hkv)) or log_decay.stride(-1) != 1 and hkv > 1:
+    s, shape = log_decay.stride(), log_decay.shape
+    if log_decay.dtype is not torch.float32 or shape != (T, hkv) and shape != (hkv,) or s[-1] != 1 and hkv > 1:
         raise _bad("log_decay has to be [T, kv_heads] or [kv_heads] of torch.float32 with contiguous heads")
-    gs = 0 if fixed else log_decay.stride(0) if T > 1 else hkv
+    gs = 0 if len(s) == 1 else s[0] if T > 1 else hkv
     devices = [k.get_device(), v.get_device(), log_decay.get_device(), *batch.devices]
     return (T, hq, hkv, d), (q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr()), (qs, ks, gs), devices
 

@@ -4,7 +4,7 @@
 namespace hspmd {
 namespace {
 
-template <int D, bool ONE, int WEIGHT_PARTS>
+template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS>
 // (three parts of the weights leave room for one workgroup per compute unit)
 __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2) void linear_bwd_kernel(LinearParams p) {
     __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS>::bytes(true, true)];
@@ -13,7 +13,7 @@ __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2)
     if (!item_of_block<true>(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
     if (role == 0) outputs_of<D, false, true, ONE, 3, WEIGHT_PARTS>(p, dq_routine(p), seg, slot, kv_head, lds);
     else if (role == 1) outputs_of<D, true, true, ONE, 3, WEIGHT_PARTS>(p, dk_routine(p), seg, slot, kv_head, lds);
-    else outputs_of<D, true, false, ONE, 3, WEIGHT_PARTS>(p, dv_routine(p), seg, slot, kv_head, lds);
+    else outputs_of<D, true, false, ONE, V_PARTS, WEIGHT_PARTS>(p, dv_routine(p), seg, slot, kv_head, lds);
 }
 
 // Gradients of the log decays, a workgroup per segment and KV head, from its last chunk to its first, a chunk per wave.  g_t weighs every pair of a
@@ -92,7 +92,8 @@ __global__ __launch_bounds__(256) void linear_decay_sum_kernel(LinearParams p) {
 
 template <int D, bool ONE>
 void launch(const LinearParams& p, hipStream_t stream) {
-    const auto kernel = p.grad_f32 ? linear_bwd_kernel<D, ONE, 3> : linear_bwd_kernel<D, ONE, 2>;
+    // dv rounded to bf16 needs two parts of the gradient of the state; that gradient itself, where it goes out, three
+    const auto kernel = p.grad_f32 ? linear_bwd_kernel<D, ONE, 3, 3> : p.d_initial ? linear_bwd_kernel<D, ONE, 2, 3> : linear_bwd_kernel<D, ONE, 2, 2>;
     kernel<<<grid_of(p, 3), D / 32 * 64, 0, stream>>>(p);
 }
 

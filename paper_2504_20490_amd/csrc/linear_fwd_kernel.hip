@@ -25,12 +25,15 @@ void launch(const LinearParams& p, hipStream_t stream) {
 LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
                          bool backward) {
     LinearSizes s{};
-    // Segments that make 1024 workgroups, two rounds of what the device holds, where there is that much: fewer leave it idle at the end, more cost states.
-    // (One document of 131000 tokens, 8 KV heads: 967 us in segments of 1024, 1017 of 1408; ten prompts, 16 heads: 175 of 384, 196 of 640.)  Sequences that are
-    // not twice as long stay whole: two rounds of them take less than a second reading of their keys and values.
+    // As many segments as make one round of workgroups, 512 (a sequence ends in half a segment on average); fewer leave the device idle, more cost states
+    // and a second round's end.  (The headline pack, 24 heads: 345 us in segments of 1024, 328 of 1856, 417 of 3072; ten prompts, 16 heads: 158 of 1024,
+    // 131 of 640, 168 of 384.)  The backward, three workgroups for each, takes some more.  Sequences of up to two segments stay whole: that takes less
+    // than a second reading of their keys and values.
     const int64_t longest = max_rows > 0 && max_rows < total_rows ? max_rows : total_rows;
-    int64_t seg = ((int64_t)total_rows * kv_heads / 1024 + kLinearChunk - 1) / kLinearChunk * kLinearChunk;
-    seg = seg < 256 ? 256 : seg > 4096 ? 4096 : seg;
+    const int64_t round = (backward ? 576 : 512) - (int64_t)num_seqs * kv_heads / 2;
+    int64_t seg = (int64_t)total_rows * kv_heads / (round < 256 ? 256 : round);
+    seg = (seg + kLinearChunk - 1) / kLinearChunk * kLinearChunk;
+    seg = seg < 256 ? 256 : seg > 16384 ? 16384 : seg;
     s.seg_rows = longest <= 2 * seg ? 0 : (int32_t)seg;
     if (s.seg_rows > 0) {
         s.slots = linear_slots(total_rows, num_seqs, seg);
