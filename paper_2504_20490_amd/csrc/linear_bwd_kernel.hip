@@ -19,7 +19,7 @@ __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2)
 // Gradients of the log decays, a workgroup per segment and KV head, from its last chunk to its first, a chunk per wave.  g_t weighs every pair of a
 // token from t on and one before t.  Of these pairs, a chunk's own and those with a token on one side of the chunk come from the dot products;
 // those across the whole chunk, <e^{G_L} S, R>, are what is left of <S, dS> at its end without its own keys.
-constexpr int kDecayWaves = 4;
+constexpr int kDecayWaves = 8;
 __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearParams p) {
     __shared__ float keys[kDecayWaves], queries[kDecayWaves], dead[kDecayWaves], totals[kDecayWaves];
     const LinearShape& sh = p.shape;
@@ -75,7 +75,12 @@ __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearPa
         total = wave_sum(total);
         if (lane == 0) totals[wave] = total;
         __syncthreads();
-        if (threadIdx.x == 0) p.decay_sums[item] = totals[0] + totals[1] + totals[2] + totals[3];
+        if (threadIdx.x == 0) {
+            total = 0.f;
+#pragma unroll
+            for (int w = 0; w < kDecayWaves; ++w) total += totals[w];
+            p.decay_sums[item] = total;
+        }
     }
 }
 

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(D / 32 * 64, 2) void linear_state_kernel(LinearPara
 
 // Passes states from segment to segment, elementwise: entry b holds what segment b - 1 adds and receives the state at the start of segment b.
 // blockIdx.y: 0 states, forwards; 1 their gradients, backwards.
-constexpr int kPassThreads = 256;
+constexpr int kPassThreads = 256, kPassAhead = 4;
 __global__ __launch_bounds__(kPassThreads) void linear_pass_kernel(LinearParams p, int parts) {
     const LinearShape& sh = p.shape;
     const int part = blockIdx.x % parts, kv_head = blockIdx.x / parts % sh.kv_heads, window = blockIdx.x / parts / sh.kv_heads;
@@ -59,11 +59,24 @@ __global__ __launch_bounds__(kPassThreads) void linear_pass_kernel(LinearParams 
     if (from) s = *reinterpret_cast<const f32x4*>(from + e);
     else if (exists) s = s + __builtin_nanf("");
     *reinterpret_cast<f32x4*>(base + (later ? count - 1 : 0) * step) = s;
-    for (int i = 1; i < count; ++i) {
-        const int to = later ? count - 1 - i : i, over = later ? to + 1 : i - 1;     // the entry, and the segment that is passed over
-        f32x4* const at = reinterpret_cast<f32x4*>(base + to * step);
-        s = s * fast_exp2(decay[(int64_t)over * sh.kv_heads]) + *at;
-        *at = s;
+    // number i of the way: entry i, or (later) count - 1 - i; the segment passed over between numbers i - 1 and i is that of number i - 1
+    const int64_t way = later ? -1 : 1, begin = later ? count - 1 : 0;
+    for (int i = 1; i < count; i += kPassAhead) {
+        f32x4 x[kPassAhead];
+        float g[kPassAhead];
+#pragma unroll
+        for (int j = 0; j < kPassAhead; ++j) {
+            const int k = i + j;          // (all read before any is written)
+            if (k >= count) break;
+            x[j] = *reinterpret_cast<const f32x4*>(base + (begin + k * way) * step);
+            g[j] = decay[(begin + (k - 1) * way) * sh.kv_heads];
+        }
+#pragma unroll
+        for (int j = 0; j < kPassAhead; ++j) {
+            if (i + j >= count) break;
+            s = s * fast_exp2(g[j]) + x[j];
+            *reinterpret_cast<f32x4*>(base + (begin + (i + j) * way) * step) = s;
+        }
     }
 }
 

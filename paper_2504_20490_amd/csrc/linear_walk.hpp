@@ -61,13 +61,15 @@ template <int D>
 struct TileLoad {
     static constexpr int kThreadsHere = D / 32 * 64, kRowsPerPass = kThreadsHere / (D / 8), kPasses = kLinearChunk / kRowsPerPass;
     u32x4 r[kPasses];
-    __device__ __forceinline__ void issue(const uint16_t* first_row, int64_t stride, int rows, int head_dim) {
+    __device__ __forceinline__ void issue(const uint16_t* first_row, int64_t token_stride, int rows, int head_dim) {
+        int stride = (int)token_stride;
+        asm volatile("" : "+s"(stride));      // (its multiples are made here, and not kept in scalar registers across the loop)
         const int row = threadIdx.x / (D / 8), col = threadIdx.x % (D / 8) * 8, there = col < head_dim ? rows : 0;
-        const uint32_t off = (uint32_t)(row * (int)stride + col) * 2u;
+        const uint32_t off = (uint32_t)(row * stride + col) * 2u;
         const __amdgpu_buffer_rsrc_t rsrc = whole_memory(first_row);
 #pragma unroll
         for (int i = 0; i < kPasses; ++i)
-            r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, row + i * kRowsPerPass < there ? off : kNowhere, i * kRowsPerPass * (int)stride * 2, 0);
+            r[i] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, row + i * kRowsPerPass < there ? off : kNowhere, i * kRowsPerPass * stride * 2, 0);
     }
     // ends the life of what was put: a load that is not always made again would else keep its registers throughout the loop
     __device__ __forceinline__ void drop() {
