@@ -237,9 +237,9 @@ __device__ __forceinline__ void add_not_finite(const char* lds, int wave, int la
     }
 }
 
-// The state is held as 2^held times what the registers hold, and multiplied out when that is below 2^-16: decays near 1 cost no operation per element
-// and chunk.
-constexpr float kLeastHeld = -16.f;
+// The state is held as 2^held times what the registers hold, and multiplied out when that leaves 2^-16 .. 2^16: decays near 1 cost no operation per element
+// and chunk.  (false for NaN, which is multiplied out into the state)
+__device__ __forceinline__ bool can_hold(float log2) { return __builtin_fabsf(log2) <= 16.f; }
 
 // Walks a segment's chunks, forwards or (LATER) backwards, with the state that reaches it in `S`.
 //   LATER   targets see the tokens from themselves on, and a KV head's sources are those of all its query heads (dk, dv); else they see the
@@ -307,6 +307,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             lb.drop();
             lc.drop();
         }
+        next_g = 0.f;
         if (ONE || h == 0)
             next_g = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(whole_memory(base_g + first * p.decay_stride),
                                                                           lane < rows ? (uint32_t)(lane * (int)p.decay_stride * 4) : kNowhere, 0, 0));
@@ -319,6 +320,25 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
     for (int n = 0; n < chunks; ++n) {
         const int chunk = LATER ? chunks - 1 - n : n;
         const int first = chunk * kLinearChunk;
+        if (wave == kWaves - 1) {        // (the wave without a block of pairs)
+            const float sum = sum_up_to(lane < seg.rows - first ? decay_log2(next_g) : 0.f);
+            const float total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum), 63));
+            const float in = LATER ? total - sum : sum, out = LATER ? sum : total - sum;
+            const float next_held = can_hold(held + total) ? held + total : 0.f;
+            sums[lane] = sum;
+            in_weight[lane] = f.scale_in * fast_exp2(in + held);
+            out_weight[lane] = f.scale_state * fast_exp2(out - next_held);
+            if (lane == 0) whole[0] = total;
+        }
+        // tiles of the chunk; those of a head follow in the loop over them
+        if (LATER && OUT) {
+            la.put(tile_a);
+            if (DOTS) le.put(tile_e);
+        }
+        if (!LATER) {
+            lb.put(tile_b);
+            lc.put(tile_c);
+        }
         f32x16 out_of_heads[2];            // LATER: summed over the heads
         float chunk_decay = 0.f;
         for (int h = 0; h < group; ++h) {
@@ -328,21 +348,11 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             int t32 = lane & 31;
             asm volatile("" : "+v"(t32));      // (as reads.fresh(): or the mask of every hidden pair is kept in registers)
             reads.fresh();
-            if (first_head && wave == kWaves - 1) {        // (the wave without a block of pairs)
-                const float sum = sum_up_to(lane < seg.rows - first ? decay_log2(next_g) : 0.f);
-                const float total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum), 63));
-                const float in = LATER ? total - sum : sum, out = LATER ? sum : total - sum;
-                const float next_held = held + total < kLeastHeld ? 0.f : held + total;
-                sums[lane] = sum;
-                in_weight[lane] = f.scale_in * fast_exp2(in + held);
-                out_weight[lane] = f.scale_state * fast_exp2(out - next_held);
-                if (lane == 0) whole[0] = total;
-            }
-            if (OUT && (!LATER || first_head)) {
+            if (!LATER && OUT) {
                 la.put(tile_a);
                 if (DOTS) le.put(tile_e);
             }
-            if (LATER || first_head) {
+            if (LATER) {
                 lb.put(tile_b);
                 lc.put(tile_c);
             }
@@ -471,7 +481,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             }
             if (OUT && !kEarly) issue_next(n, h);
             if (LATER || last_head) {
-                if ((!LATER || first_head) && held + chunk_decay < kLeastHeld) {
+                if ((!LATER || first_head) && !can_hold(held + chunk_decay)) {
                     const float left = fast_exp2(held + chunk_decay);
 #pragma unroll
                     for (int db = 0; db < D / 32; ++db)
@@ -506,7 +516,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             __syncthreads();
         }
         all_decay += chunk_decay;
-        held = held + chunk_decay < kLeastHeld ? 0.f : held + chunk_decay;
+        held = can_hold(held + chunk_decay) ? held + chunk_decay : 0.f;
     }
     if (held != 0.f) {
         const float left = fast_exp2(held);
