@@ -4,16 +4,16 @@
 namespace hspmd {
 namespace {
 
-template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS>
+template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS, int NB>
 // (three parts of the weights leave room for one workgroup per compute unit)
 __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2) void linear_bwd_kernel(LinearParams p) {
     __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS>::bytes(true, true)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block<true>(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
-    if (role == 0) outputs_of<D, false, true, ONE, 3, WEIGHT_PARTS>(p, dq_routine(p), seg, slot, kv_head, lds);
-    else if (role == 1) outputs_of<D, true, true, ONE, 3, WEIGHT_PARTS>(p, dk_routine(p), seg, slot, kv_head, lds);
-    else outputs_of<D, true, false, ONE, V_PARTS, WEIGHT_PARTS>(p, dv_routine(p), seg, slot, kv_head, lds);
+    if (role == 0) outputs_of<D, false, true, ONE, 3, WEIGHT_PARTS, NB>(p, dq_routine(p), seg, slot, kv_head, lds);
+    else if (role == 1) outputs_of<D, true, true, ONE, 3, WEIGHT_PARTS, NB>(p, dk_routine(p), seg, slot, kv_head, lds);
+    else outputs_of<D, true, false, ONE, V_PARTS, WEIGHT_PARTS, NB>(p, dv_routine(p), seg, slot, kv_head, lds);
 }
 
 // Gradients of the log decays, a workgroup per segment and KV head, from its last chunk to its first, a chunk per wave.  g_t weighs every pair of a
@@ -95,10 +95,10 @@ __global__ __launch_bounds__(256) void linear_decay_sum_kernel(LinearParams p) {
     if (threadIdx.x == 0) p.d_log_decay[blockIdx.x] = parts[0] + parts[1] + parts[2] + parts[3];
 }
 
-template <int D, bool ONE>
+template <int D, bool ONE, int NB>
 void launch(const LinearParams& p, hipStream_t stream) {
     // dv rounded to bf16 needs two parts of the gradient of the state; that gradient itself, where it goes out, three
-    const auto kernel = p.grad_f32 ? linear_bwd_kernel<D, ONE, 3, 3> : p.d_initial ? linear_bwd_kernel<D, ONE, 2, 3> : linear_bwd_kernel<D, ONE, 2, 2>;
+    const auto kernel = p.grad_f32 ? linear_bwd_kernel<D, ONE, 3, 3, NB> : p.d_initial ? linear_bwd_kernel<D, ONE, 2, 3, NB> : linear_bwd_kernel<D, ONE, 2, 2, NB>;
     kernel<<<grid_of(p, 3), D / 32 * 64, 0, stream>>>(p);
 }
 
@@ -107,9 +107,7 @@ void launch(const LinearParams& p, hipStream_t stream) {
 hipError_t launch_linear_bwd(const LinearParams& p, hipStream_t stream) {
     if (p.shape.slots > 0) {
         launch_linear_states(p, true, 3, stream);
-        const bool one = p.shape.group == 1;
-        if (p.shape.head_dim <= 64) one ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
-        else one ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+        with_shape(p.shape, [&](auto d, auto blocks, auto one) { launch<decltype(d)::value, decltype(one)::value, decltype(blocks)::value>(p, stream); });
     }
     if (p.d_log_decay) {
         if (p.shape.slots > 0) linear_decay_kernel<<<grid_of(p, 1), kDecayWaves * 64, 0, stream>>>(p);

@@ -4,19 +4,19 @@
 namespace hspmd {
 namespace {
 
-template <int D, bool ONE, int PARTS>
+template <int D, bool ONE, int PARTS, int NB>
 __global__ __launch_bounds__(D / 32 * 64, 2) void linear_fwd_kernel(LinearParams p) {
     __shared__ __align__(16) char lds[Lds<D, 2>::bytes(true, false)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block<true>(p.shape, 1, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
-    outputs_of<D, false, false, ONE, PARTS, 2>(p, forward_routine(p), seg, slot, kv_head, lds);
+    outputs_of<D, false, false, ONE, PARTS, 2, NB>(p, forward_routine(p), seg, slot, kv_head, lds);
 }
 
-template <int D, bool ONE>
+template <int D, bool ONE, int NB>
 void launch(const LinearParams& p, hipStream_t stream) {
     // (o is rounded to bf16: two parts of the state suffice for it, a final state that is kept takes three)
-    const auto kernel = p.final.data ? linear_fwd_kernel<D, ONE, 3> : linear_fwd_kernel<D, ONE, 2>;
+    const auto kernel = p.final.data ? linear_fwd_kernel<D, ONE, 3, NB> : linear_fwd_kernel<D, ONE, 2, NB>;
     kernel<<<grid_of(p, 1), D / 32 * 64, 0, stream>>>(p);
 }
 
@@ -54,9 +54,7 @@ LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows,
 hipError_t launch_linear_fwd(const LinearParams& p, hipStream_t stream) {
     if (p.shape.slots > 0) {
         launch_linear_states(p, false, p.final.data ? 3 : 2, stream);
-        const bool one = p.shape.group == 1;
-        if (p.shape.head_dim <= 64) one ? launch<64, true>(p, stream) : launch<64, false>(p, stream);
-        else one ? launch<128, true>(p, stream) : launch<128, false>(p, stream);
+        with_shape(p.shape, [&](auto d, auto blocks, auto one) { launch<decltype(d)::value, decltype(one)::value, decltype(blocks)::value>(p, stream); });
     }
     return hipGetLastError();
 }

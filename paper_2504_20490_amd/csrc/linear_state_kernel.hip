@@ -5,7 +5,7 @@ namespace hspmd {
 namespace {
 
 // What a segment adds to the state, into the entry of the segment that it reaches next; `roles` 2: also what it adds to the gradient.
-template <int D, int PARTS>
+template <int D, int PARTS, int NB>
 __global__ __launch_bounds__(D / 32 * 64, 2) void linear_state_kernel(LinearParams p, int roles) {
     __shared__ __align__(16) char lds[Lds<D, 2>::bytes(false, false)];
     int role, kv_head, slot;
@@ -14,10 +14,10 @@ __global__ __launch_bounds__(D / 32 * 64, 2) void linear_state_kernel(LinearPara
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = p.shape.head_dim;
     const bool last = seg.index == seg.count - 1;
     if (role == 0 ? last : seg.index == 0) return;
-    State<D> S;
+    State<NB> S;
     S.clear(0.f);
-    const float decay = role == 0 ? walk<D, false, false, false, true, PARTS, 2>(p, forward_routine(p), seg, kv_head, lds, S)
-                                  : walk<D, true, false, false, false, PARTS, 2>(p, dv_routine(p), seg, kv_head, lds, S);
+    const float decay = role == 0 ? walk<D, false, false, false, true, PARTS, 2, NB>(p, forward_routine(p), seg, kv_head, lds, S)
+                                  : walk<D, true, false, false, false, PARTS, 2, NB>(p, dv_routine(p), seg, kv_head, lds, S);
     const int64_t own = (int64_t)(seg.entry + seg.index) * p.shape.kv_heads + kv_head;
     float* const to = role == 0 ? p.states + (own + p.shape.kv_heads) * d * d : p.d_states + (own - p.shape.kv_heads) * d * d;
     S.store(to, d, wave, lane);
@@ -80,9 +80,9 @@ __global__ __launch_bounds__(kPassThreads) void linear_pass_kernel(LinearParams 
     }
 }
 
-template <int D>
+template <int D, int NB>
 void launch(const LinearParams& p, int roles, int parts, hipStream_t stream) {
-    const auto kernel = parts == 3 ? linear_state_kernel<D, 3> : linear_state_kernel<D, 2>;
+    const auto kernel = parts == 3 ? linear_state_kernel<D, 3, NB> : linear_state_kernel<D, 2, NB>;
     kernel<<<grid_of(p, roles), D / 32 * 64, 0, stream>>>(p, roles);
 }
 
@@ -91,7 +91,7 @@ void launch(const LinearParams& p, int roles, int parts, hipStream_t stream) {
 void launch_linear_states(const LinearParams& p, bool backward, int parts, hipStream_t stream) {
     if (p.shape.seg_rows == 0) return;
     const int roles = backward ? 2 : 1, d = p.shape.head_dim, blocks = (d * d / 4 + kPassThreads - 1) / kPassThreads;
-    d <= 64 ? launch<64>(p, roles, parts, stream) : launch<128>(p, roles, parts, stream);
+    with_shape(p.shape, [&](auto width, auto blocks, auto) { launch<decltype(width)::value, decltype(blocks)::value>(p, roles, parts, stream); });
     linear_pass_kernel<<<dim3((unsigned)((int64_t)p.shape.windows * p.shape.kv_heads * blocks), roles), kPassThreads, 0, stream>>>(p, blocks);
 }
 

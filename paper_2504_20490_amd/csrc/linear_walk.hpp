@@ -107,14 +107,14 @@ __device__ __forceinline__ void store_rows(void* base, int64_t first, const f32x
     }
 }
 
-// The wave's part of a state: columns 32 wave .. + 31 (of c) along the lanes, all D rows (of b) in registers; register i of
+// The wave's part of a state: columns 32 wave .. + 31 (of c) along the lanes, all 32 NB rows (of b) in registers; register i of
 // block db holds row 32 db + 16 (i / 8) + 8 (lane / 32) + i % 8.
-template <int D>
+template <int NB>
 struct State {
-    f32x16 x[D / 32];
+    f32x16 x[NB];
     __device__ __forceinline__ void clear(float value) {
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < NB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[db][i] = value;
     }
@@ -122,7 +122,7 @@ struct State {
     __device__ __forceinline__ void load(const float* m, int d, bool transposed, int wave, int lane) {
         const int col = wave * 32 + (lane & 31);
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < NB; ++db)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = db * 32 + h * 16 + (lane >> 5) * 8;
@@ -144,7 +144,7 @@ struct State {
     __device__ __forceinline__ void store(float* m, int d, int wave, int lane) const {
         const int col = wave * 32 + (lane & 31);
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < NB; ++db)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = db * 32 + h * 16 + (lane >> 5) * 8;
@@ -159,7 +159,7 @@ struct State {
         const int col = wave * 32 + (lane & 31);
         float sum = 0.f;
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < NB; ++db)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int row = db * 32 + h * 16 + (lane >> 5) * 8;
@@ -248,17 +248,19 @@ __device__ __forceinline__ bool can_hold(float log2) { return __builtin_fabsf(lo
 //   DOTS    the dot products of the output with the tensor it is the gradient of, the part from the own chunk (without the token's own) and
 //           the part from the state apart
 //   ONE     a KV head has one query head
+//   NB      blocks of 32 columns that head_dim takes; steps, and waves, that would compute on columns behind them pass
 //   PARTS, WEIGHT_PARTS   bf16 values that the state and its sources, and the weights of pairs, enter products as; three of the weights go with
 //           fp32 outputs, two with bf16
 // Returns the log2 of the segment's decay.
-template <int D, bool LATER, bool OUT, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS>
-__device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, const Segment& seg, int kv_head, char* lds, State<D>& S) {
+template <int D, bool LATER, bool OUT, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS, int NB>
+__device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, const Segment& seg, int kv_head, char* lds, State<NB>& S) {
     constexpr bool OUT_F32 = WEIGHT_PARTS == 3;
     using L = Lds<D, WEIGHT_PARTS>;
     constexpr int kWaves = L::kWaves;
     constexpr bool kEarly = !DOTS || ONE;      // when the next tiles are loaded: four of them, beside outputs kept over several heads, are too many
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int d = p.shape.head_dim, group = ONE ? 1 : p.shape.group;
+    const bool mine = NB == kWaves || wave < NB;      // this wave has columns
     const int hh = lane >> 5;
     TileReads<D> reads;
     reads.init(lane);
@@ -367,11 +369,11 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                     const int sb = LATER ? (blk > 0) : blk >> 1, tb = LATER ? blk >> 1 : (blk > 0);
                     f32x16 w{};
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) w = mfma(reads.along(tile_b, sb, kk), reads.along(tile_a, tb, kk), w);
+                    for (int kk = 0; kk < 2 * NB; ++kk) w = mfma(reads.along(tile_b, sb, kk), reads.along(tile_a, tb, kk), w);
                     f32x16 y{};
                     if constexpr (DOTS) {
 #pragma unroll
-                        for (int kk = 0; kk < D / 16; ++kk) y = mfma(reads.along(tile_c, sb, kk), reads.along(tile_e, tb, kk), y);
+                        for (int kk = 0; kk < 2 * NB; ++kk) y = mfma(reads.along(tile_c, sb, kk), reads.along(tile_e, tb, kk), y);
                     }
                     const float target_sum = LATER ? sums[tb * 32 + t32] - p.scale_log2 : sums[tb * 32 + t32] + p.scale_log2;
 #pragma unroll
@@ -412,8 +414,9 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                 if (!LATER || first_head) {
                     __builtin_amdgcn_s_setprio(1);     // (products before the other workgroup's vector operations)
                     out[0] = out[1] = f32x16{};
+                    if (mine)
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk) {
+                    for (int kk = 0; kk < 2 * NB; ++kk) {
                         Parts<PARTS> parts;
                         f32x8 x;
 #pragma unroll
@@ -450,16 +453,18 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             }
 
             if constexpr (OUT) {
-                bf16x8 sources[4];     // c, 16 sources at a time down the operand's k
+                if (mine) {
+                    bf16x8 sources[4];     // c, 16 sources at a time down the operand's k
 #pragma unroll
-                for (int t = 0; t < 4; ++t) sources[t] = reads.down(tile_c, wave, t);
-                const bool finite = all_finite(sources, ops);
-                if (!finite) {
+                    for (int t = 0; t < 4; ++t) sources[t] = reads.down(tile_c, wave, t);
+                    const bool finite = all_finite(sources, ops);
+                    if (!finite) {
 #pragma unroll
-                    for (int t = 0; t < 4; ++t) sources[t] = finite_part(sources[t]);
+                        for (int t = 0; t < 4; ++t) sources[t] = finite_part(sources[t]);
+                    }
+                    add_own_chunk<D, LATER, WEIGHT_PARTS>(lds, sources, lane, out);
+                    if (!finite) add_not_finite<D, LATER, WEIGHT_PARTS>(lds, wave, lane, out);
                 }
-                add_own_chunk<D, LATER, WEIGHT_PARTS>(lds, sources, lane, out);
-                if (!finite) add_not_finite<D, LATER, WEIGHT_PARTS>(lds, wave, lane, out);
                 if (!LATER || last_head) {
                     const int64_t at = (int64_t)(seg.start + first) * target_heads + (LATER ? kv_head : kv_head * group + h);
                     store_rows<OUT_F32>(f.out, at * d, out, target_heads * d, seg.rows - first, d, wave, lane);
@@ -480,11 +485,11 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                 }
             }
             if (OUT && !kEarly) issue_next(n, h);
-            if (LATER || last_head) {
+            if (mine && (LATER || last_head)) {
                 if ((!LATER || first_head) && !can_hold(held + chunk_decay)) {
                     const float left = fast_exp2(held + chunk_decay);
 #pragma unroll
-                    for (int db = 0; db < D / 32; ++db)
+                    for (int db = 0; db < NB; ++db)
 #pragma unroll
                         for (int i = 0; i < 16; ++i) S.x[db][i] *= left;
                 }
@@ -503,13 +508,13 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                     }
                     Parts<PARTS> parts;
                     parts.of(x, ops);
-                    bf16x8 rows[D / 32];
+                    bf16x8 rows[NB];
 #pragma unroll
-                    for (int db = 0; db < D / 32; ++db) rows[db] = reads.down_ordered(tile_b, db, t);
+                    for (int db = 0; db < NB; ++db) rows[db] = reads.down_ordered(tile_b, db, t);
 #pragma unroll
                     for (int part = 0; part < PARTS; ++part)
 #pragma unroll
-                        for (int db = 0; db < D / 32; ++db) S.x[db] = mfma(rows[db], parts.part[part], S.x[db]);
+                        for (int db = 0; db < NB; ++db) S.x[db] = mfma(rows[db], parts.part[part], S.x[db]);
                 }
                 __builtin_amdgcn_s_setprio(0);
             }
@@ -521,7 +526,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
     if (held != 0.f) {
         const float left = fast_exp2(held);
 #pragma unroll
-        for (int db = 0; db < D / 32; ++db)
+        for (int db = 0; db < NB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) S.x[db][i] *= left;
     }
@@ -540,15 +545,15 @@ __device__ __forceinline__ const float* reaching_state(const LinearParams& p, co
     return m;
 }
 
-template <int D, bool LATER, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS>
+template <int D, bool LATER, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS, int NB>
 __device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine& f, const Segment& seg, int slot, int kv_head, char* lds) {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = p.shape.head_dim;
-    State<D> S;
+    State<NB> S;
     bool bad;
     const float* const from = reaching_state<LATER>(p, seg, kv_head, &bad);
     if (from) S.load(from, d, f.transposed, wave, lane);
     else S.clear(bad ? __builtin_nanf("") : 0.f);
-    walk<D, LATER, true, DOTS, ONE, PARTS, WEIGHT_PARTS>(p, f, seg, kv_head, lds, S);
+    walk<D, LATER, true, DOTS, ONE, PARTS, WEIGHT_PARTS, NB>(p, f, seg, kv_head, lds, S);
     if (!LATER && DOTS) {
         // <S, dS> behind the segment's last token: what the gradient of its decays starts from
         const float* const d_end = reaching_state<true>(p, seg, kv_head, &bad);
@@ -599,6 +604,17 @@ __device__ __forceinline__ Routine dk_routine(const LinearParams& p) {
 }
 __device__ __forceinline__ Routine dv_routine(const LinearParams& p) {
     return Routine{p.k, p.q, p.d_o, nullptr, p.kv_stride, p.q_stride, p.do_stride, 0, 1.f, p.scale, p.dv, false, nullptr, nullptr};
+}
+
+// calls f(tile width, blocks of 32 columns, one query head per KV head) as constants
+template <typename F>
+void with_shape(const LinearShape& shape, F&& f) {
+    using std::integral_constant;
+    const auto heads = [&](auto d, auto blocks) { shape.group == 1 ? f(d, blocks, std::true_type{}) : f(d, blocks, std::false_type{}); };
+    if (shape.head_dim <= 32) heads(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    else if (shape.head_dim <= 64) heads(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    else if (shape.head_dim <= 96) heads(integral_constant<int, 128>{}, integral_constant<int, 3>{});
+    else heads(integral_constant<int, 128>{}, integral_constant<int, 4>{});
 }
 
 unsigned grid_of(const LinearParams& p, int roles) { return (unsigned)linear_grid((int64_t)p.shape.slots * p.shape.kv_heads * roles, 4 * roles); }
