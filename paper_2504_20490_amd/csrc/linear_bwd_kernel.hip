@@ -5,9 +5,8 @@ namespace hspmd {
 namespace {
 
 template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS, int NB>
-// (three parts of the weights leave room for one workgroup per compute unit)
-__global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 ? 1 : 2) void linear_bwd_kernel(LinearParams p) {
-    __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS>::bytes(true, true)];
+__global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 && !ONE ? 1 : 2) void linear_bwd_kernel(LinearParams p) {
+    __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS, ONE>::bytes(true, true)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block<true>(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;

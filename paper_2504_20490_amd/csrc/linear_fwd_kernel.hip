@@ -6,7 +6,7 @@ namespace {
 
 template <int D, bool ONE, int PARTS, int NB>
 __global__ __launch_bounds__(D / 32 * 64, 2) void linear_fwd_kernel(LinearParams p) {
-    __shared__ __align__(16) char lds[Lds<D, 2>::bytes(true, false)];
+    __shared__ __align__(16) char lds[Lds<D, 2, ONE>::bytes(true, false)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block<true>(p.shape, 1, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;

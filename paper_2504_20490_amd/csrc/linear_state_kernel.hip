@@ -7,7 +7,7 @@ namespace {
 // What a segment adds to the state, into the entry of the segment that it reaches next; `roles` 2: also what it adds to the gradient.
 template <int D, int PARTS, int NB>
 __global__ __launch_bounds__(D / 32 * 64, 2) void linear_state_kernel(LinearParams p, int roles) {
-    __shared__ __align__(16) char lds[Lds<D, 2>::bytes(false, false)];
+    __shared__ __align__(16) char lds[Lds<D, 2, true>::bytes(false, false)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block(p.shape, roles, role, kv_head, slot) || !find_segment(p.shape, slot, seg) || seg.count == 1) return;

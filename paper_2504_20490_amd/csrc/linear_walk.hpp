@@ -29,8 +29,8 @@ struct Routine {
     float* far;
 };
 
-// What a workgroup keeps in LDS.  WEIGHT_PARTS: bf16 values per weight of a pair
-template <int D, int WEIGHT_PARTS>
+// What a workgroup keeps in LDS.  WEIGHT_PARTS: bf16 values per weight of a pair; ONE: a KV head has one query head
+template <int D, int WEIGHT_PARTS, bool ONE>
 struct Lds {
     static constexpr int kWaves = D / 32;
     static constexpr int kTile = kLinearChunk * D * 2;
@@ -38,12 +38,18 @@ struct Lds {
     static constexpr int kSums = 2 * kTile;                   // running sums of the log decays, weights of targets and of sources, the chunk's decay
     static constexpr int kA = kSums + (3 * kLinearChunk + 4) * 4;
     static constexpr int kWeights = kA + kTile;               // of pairs: [block][step of 16 sources][part][lane]
-    static constexpr int kNear = kWeights + 3 * 2 * WEIGHT_PARTS * 1024;
+    // D = 128: with a third part the area would leave room for one workgroup per compute unit.  It goes where the tile of e was, behind the last use of
+    // that (with several heads, which share the tile of a KV head, there is no such time)
+    static constexpr bool kLate = D == 128 && WEIGHT_PARTS == 3 && ONE;
+    static constexpr int kAreaParts = kLate ? 2 : WEIGHT_PARTS;
+    static constexpr int kNear = kWeights + 3 * 2 * kAreaParts * 1024;
     static constexpr int kFar = kNear + 3 * 32 * 4;
     static constexpr int kE = kFar + kWaves * kLinearChunk * 4;
     static constexpr int bytes(bool out, bool dots) { return dots ? kE + kTile : out ? kNear : kA; }
     // where the weights of a block's step are, for lane 0
-    static constexpr int weights(int blk, int step, int part) { return kWeights + ((blk * 2 + step) * WEIGHT_PARTS + part) * 1024; }
+    static constexpr int weights(int blk, int step, int part) {
+        return part < kAreaParts ? kWeights + ((blk * 2 + step) * kAreaParts + part) * 1024 : kE + (blk * 2 + step) * 1024;
+    }
 };
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -196,12 +202,12 @@ __device__ __forceinline__ bf16x8 finite_part(bf16x8 x) {
     return c.v;
 }
 
-// What the sources of the own chunk give: weights times c, (source block, target block) of 32 x 32 pairs by their number, see walk
-template <int D, bool LATER, int WEIGHT_PARTS>
+// What the sources of the own chunk give: parts FIRST .. LAST of the weights times c, (source block, target block) of 32 x 32 pairs by their number, see walk
+template <int D, bool LATER, bool ONE, int WEIGHT_PARTS, int FIRST, int LAST>
 __device__ __forceinline__ void add_own_chunk(const char* lds, const bf16x8 (&sources)[4], int lane, f32x16 (&out)[2]) {
-    using L = Lds<D, WEIGHT_PARTS>;
+    using L = Lds<D, WEIGHT_PARTS, ONE>;
 #pragma unroll
-    for (int part = 0; part < WEIGHT_PARTS; ++part)
+    for (int part = FIRST; part <= LAST; ++part)
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
@@ -210,9 +216,9 @@ __device__ __forceinline__ void add_own_chunk(const char* lds, const bf16x8 (&so
                 out[tb] = mfma(sources[2 * sb + tt], *reinterpret_cast<const bf16x8*>(lds + L::weights(blk, tt, part) + lane * 16), out[tb]);
             }
 }
-template <int D, bool LATER, int WEIGHT_PARTS>
+template <int D, bool LATER, bool ONE, int WEIGHT_PARTS>
 __device__ __forceinline__ void add_not_finite(const char* lds, int wave, int lane, f32x16 (&out)[2]) {
-    using L = Lds<D, WEIGHT_PARTS>;
+    using L = Lds<D, WEIGHT_PARTS, ONE>;
     const char* const tile = lds + L::kC;
     const int t32 = lane & 31, hh = lane >> 5;
 #pragma unroll 1
@@ -255,7 +261,7 @@ __device__ __forceinline__ bool can_hold(float log2) { return __builtin_fabsf(lo
 template <int D, bool LATER, bool OUT, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS, int NB>
 __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, const Segment& seg, int kv_head, char* lds, State<NB>& S) {
     constexpr bool OUT_F32 = WEIGHT_PARTS == 3;
-    using L = Lds<D, WEIGHT_PARTS>;
+    using L = Lds<D, WEIGHT_PARTS, ONE>;
     constexpr int kWaves = L::kWaves;
     constexpr bool kEarly = !DOTS || ONE;      // when the next tiles are loaded: four of them, beside outputs kept over several heads, are too many
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -363,6 +369,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
 
             if (!OUT) issue_next(n, h);
             if constexpr (OUT) {
+                bf16x8 late[2];        // (kLate: a wave has one block at most)
                 // pairs of sources (along the rows) and targets (along the lanes): of the four blocks of 32 x 32, the three that are not all hidden
 #pragma unroll 1
                 for (int blk = wave; blk < 3; blk += kWaves) {
@@ -405,8 +412,9 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                         for (int i = 0; i < 8; ++i) x[i] = w[8 * tt + i];
                         parts.of(x, ops);
 #pragma unroll
-                        for (int part = 0; part < WEIGHT_PARTS; ++part)
-                            *reinterpret_cast<bf16x8*>(lds + L::weights(0, tt, part) + blk * (2 * WEIGHT_PARTS * 1024) + lane * 16) = parts.part[part];
+                        for (int part = 0; part < L::kAreaParts; ++part)
+                            *reinterpret_cast<bf16x8*>(lds + L::weights(0, tt, part) + blk * (2 * L::kAreaParts * 1024) + lane * 16) = parts.part[part];
+                        if constexpr (L::kLate) late[tt] = parts.part[2];
                     }
                 }
                 if (kEarly) issue_next(n, h);      // (in front of the pairs they would take registers that these need)
@@ -450,21 +458,31 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                     }
                 }
                 __syncthreads();
+                if constexpr (L::kLate) {
+                    if (wave < 3) {
+#pragma unroll
+                        for (int tt = 0; tt < 2; ++tt) *reinterpret_cast<bf16x8*>(lds + L::weights(0, tt, 2) + wave * 2048 + lane * 16) = late[tt];
+                    }
+                }
             }
-
             if constexpr (OUT) {
+                bf16x8 sources[4];     // c, 16 sources at a time down the operand's k
+                bool finite = true;
                 if (mine) {
-                    bf16x8 sources[4];     // c, 16 sources at a time down the operand's k
 #pragma unroll
                     for (int t = 0; t < 4; ++t) sources[t] = reads.down(tile_c, wave, t);
-                    const bool finite = all_finite(sources, ops);
+                    finite = all_finite(sources, ops);
                     if (!finite) {
 #pragma unroll
                         for (int t = 0; t < 4; ++t) sources[t] = finite_part(sources[t]);
                     }
-                    add_own_chunk<D, LATER, WEIGHT_PARTS>(lds, sources, lane, out);
-                    if (!finite) add_not_finite<D, LATER, WEIGHT_PARTS>(lds, wave, lane, out);
+                    add_own_chunk<D, LATER, ONE, WEIGHT_PARTS, 0, L::kAreaParts - 1>(lds, sources, lane, out);
                 }
+                if constexpr (L::kLate) {
+                    __syncthreads();
+                    if (mine) add_own_chunk<D, LATER, ONE, WEIGHT_PARTS, 2, 2>(lds, sources, lane, out);
+                }
+                if (!finite) add_not_finite<D, LATER, ONE, WEIGHT_PARTS>(lds, wave, lane, out);
                 if (!LATER || last_head) {
                     const int64_t at = (int64_t)(seg.start + first) * target_heads + (LATER ? kv_head : kv_head * group + h);
                     store_rows<OUT_F32>(f.out, at * d, out, target_heads * d, seg.rows - first, d, wave, lane);
