@@ -1,0 +1,140 @@
+"""Linear attention, calls that the documentation allows and that hardly anyone makes: offsets beyond 32 bits, many query heads on one KV head, two host threads,
+row offsets that make no sense, gradients that are not wanted, accuracy of what goes out in fp32."""
+import threading
+
+import numpy as np
+import pytest
+
+from linear_util import BF16_HALF_STEP, Case, check, check_backward, check_forward, host
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def A():
+    import paper_2504_20490_amd as A
+    A.load_library()
+    return A
+
+
+def test_rows_beyond_4_gib(A):
+    """70000 rows, 32768 elements apart: the last ones start at 4.6e9 bytes."""
+    import torch
+    T, d, far = 70000, 64, 32768
+    wide = torch.zeros(T * far, dtype=torch.bfloat16, device="cuda").view(T, far)
+    wide[:, :3 * d] = torch.randn(T, 3 * d, device="cuda")
+    q, k, v = (wide[:, i * d:(i + 1) * d].view(T, 1, d) for i in range(3))
+    g = -torch.rand(T, 1, device="cuda") * 0.2
+    batch = A.LinearBatch(torch.tensor([0, 5, T], dtype=torch.int32, device="cuda"), max_rows=T)
+    outs = []
+    for x in ((q, k, v), tuple(y.contiguous() for y in (q, k, v))):
+        o, final = torch.full((T, 1, d), float("nan"), dtype=torch.bfloat16, device="cuda"), torch.zeros(2, 1, d, d, device="cuda")
+        ws = torch.empty(A.linear_attn_workspace_bytes(batch, T, 1, 1, d, backward=True), dtype=torch.uint8, device="cuda")
+        A.linear_attn_fwd(batch, *x, g, o, ws, final=final)
+        grads = [torch.empty(T, 1, d, device="cuda") for _ in range(3)]
+        dg = torch.empty_like(g)
+        A.linear_attn_bwd(batch, *x, g, o, *grads, ws, d_log_decay=dg)
+        outs.append([o, final, *grads, dg])
+    assert torch.isfinite(outs[0][0].float()).all()
+    for a, b in zip(*outs):
+        assert torch.equal(a, b)
+
+
+def test_states_beyond_4_gib(A):
+    """Slots of a pool of 70000 states of 64 KB."""
+    import torch
+    d, slots = 128, [69999, 3, 66000]
+    pool = torch.empty(70000, 1, d, d, device="cuda")
+    case = Case([1, 1, 1], 2, 1, d, 40, False, True).to_device()
+    for i, s in enumerate(slots):
+        pool[s] = case.tinitial[i]
+    guard = pool[slots[0] - 1].clone()
+    where = torch.tensor(slots, dtype=torch.int32, device="cuda")
+    o = torch.empty_like(case.tq)
+    A.linear_attn_step(A.LinearBatch(initial_slots=where, final_slots=where), case.tq, case.tk, case.tv, case.tg, o, initial=pool, final=pool)
+    check_forward(case, o, pool[slots])
+    assert torch.equal(torch.nan_to_num(pool[slots[0] - 1]), torch.nan_to_num(guard))
+    for i, s in enumerate(slots):
+        pool[s] = case.tinitial[i]
+    A.linear_attn_fwd(A.LinearBatch(case.tcu, 1, where, where), case.tq, case.tk, case.tv, case.tg, o, None, initial=pool, final=pool)
+    check_forward(case, o, pool[slots])
+
+
+@pytest.mark.parametrize("hq,hkv,d", [(33, 1, 32), (34, 2, 128), (24, 24, 16)])
+def test_many_heads(A, hq, hkv, d):
+    case = Case([90, 400], hq, hkv, d, 41, False, True).to_device()
+    check_forward(case, *case.run_forward(A))
+    check_backward(case, case.run_backward(A))
+
+
+def test_two_host_threads(A):
+    import torch
+    cases = [Case([700, 33], 2, 2, 64, 42, False, True).to_device(), Case([64, 300, 5], 4, 2, 104, 43, False, True).to_device()]
+    want = [(c.run_forward(A), c.run_backward(A)) for c in cases]
+    torch.cuda.synchronize()
+    got, errors = [None, None], []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(20):
+                    got[i] = (cases[i].run_forward(A), cases[i].run_backward(A))
+                stream.synchronize()
+        except Exception as e:          # (a thread's exception would be lost)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors
+    for (f0, b0), (f1, b1) in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(f0, f1)) and all(torch.equal(b0[n], b1[n]) for n in b0)
+
+
+@pytest.mark.parametrize("cu", [[0, 500, 100000, 700], [0, -5, 300, 2 ** 31 - 1], [800, 400, 0, 0], [-2 ** 31, 900, 100, 950]])
+def test_row_offsets_that_make_no_sense_stay_inside_the_tensors(A, cu):
+    """Results are undefined; what lies around the tensors, and the rows that no sequence can reach, are not touched."""
+    import torch
+    T, d, H = 1000, 64, 2
+    q, k, v, do = (torch.randn(T, H, d, device="cuda").bfloat16() for _ in range(4))
+    g = -torch.rand(T, H, device="cuda")
+    batch = A.LinearBatch(torch.tensor(cu, dtype=torch.int32, device="cuda"))
+    guarded = lambda *shape, t=torch.float32: torch.full((shape[0] + 2, *shape[1:]), 7.0, dtype=t, device="cuda")
+    o, dq, dk, dv = (guarded(T, H, d, t=torch.bfloat16) for _ in range(4))
+    dg, final, first = guarded(T, H), guarded(3, H, d, d), guarded(3, H, d, d)
+    need = A.linear_attn_workspace_bytes(batch, T, H, H, d, backward=True)
+    ws = torch.full((need + 4096,), 90, dtype=torch.uint8, device="cuda")
+    A.linear_attn_fwd(batch, q, k, v, g, o[1:-1], ws[:A.linear_attn_workspace_bytes(batch, T, H, H, d)], final=final[1:-1])
+    A.linear_attn_bwd(batch, q, k, v, g, do, dq[1:-1], dk[1:-1], dv[1:-1], ws[:need], d_log_decay=dg[1:-1], d_initial=first[1:-1])
+    torch.cuda.synchronize()
+    for x in (o, dq, dk, dv, dg, final, first):
+        assert (x[0] == 7).all() and (x[-1] == 7).all()
+    assert (ws[need:] == 90).all()
+
+
+def test_without_the_decays_gradient_the_others_are_the_same(A):
+    import torch
+    for fixed in (False, True):
+        case = Case([700, 33], 4, 2, 64, 44, fixed, True).to_device()
+        want, got = case.run_backward(A, f32=False), case.run_backward(A, f32=False, decays=False)
+        assert all(torch.equal(want[n], got[n]) for n in got)
+
+
+@pytest.mark.parametrize("hq,hkv,d,fixed", [(4, 4, 128, False), (8, 2, 64, False), (3, 3, 80, True)])
+def test_what_goes_out_in_fp32_is_of_fp32(A, hq, hkv, d, fixed):
+    """Relative to the result's 2-norm.  Terms have random signs, so errors and results grow with the same root of their number: an error of e per term leaves e of the
+    result.  Per term: three roundings at 2^-24 (weight, product, part), the decays' exponents of up to 7 roundings of sums below 2^4 (7 * 2^-20 at worst, their root
+    mean square an eighth of that), and chains of 64 + 128 sums, whose roundings at 2^-25 of the running sum add up as sqrt(192) of one: 2^-21.  Decay gradients cancel
+    by up to four of these, a fixed decay's, the sum of all rows, by the root of their number more."""
+    case = Case([900, 300, 70], hq, hkv, d, 45, fixed, True, rate=0.05).to_device()
+    out, want = case.run_backward(A), case.backward()
+    _, final = case.run_forward(A)
+    out["final"], want["final"] = final, case.forward()[1]
+    for name, x in out.items():
+        got, ref = host(x), want[name]
+        off = np.linalg.norm(got - ref) / np.linalg.norm(ref)
+        most = 2.0 ** -20 * (4 if name == "dg" else 1) * (np.sqrt(case.T) if name == "dg" and fixed else 1)
+        assert off <= most, (name, off, most)
