@@ -602,9 +602,12 @@ typedef struct {
  *              write the slot that it read; one that another sequence of the call reads must not be written.  A sequence without rows passes its state on
  *   o          bf16 [total_rows, local_q_heads, head_dim], contiguous, written
  *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 0) bytes, 16-byte aligned; nothing in it outlives the call
- * States are fp32 throughout; where they, and the weights of pairs, enter a product on the matrix cores they do so in two bf16 parts, which leaves an error of
- * 2^-17 of each factor.  No atomics: results are run-to-run bit-identical.  Rows are not changed by later ones of their sequence, whatever
- * those hold; an infinity or NaN in a row of k or v is in the state from there on and may make all of it NaN.
+ * Sequences longer than some hundred to thousand rows are cut and computed by several workgroups, where there are few (how follows from the batch's counts and
+ * max_rows, and so does the workspace: ask with the counts of the call).
+ * States, sums and outputs are fp32 until the one rounding of o.  Where states, and the weights of pairs, enter a product on the matrix cores they do
+ * so as sums of two bf16 values (2^-17 of each factor, far below o's rounding), the state's sources of three, all 24 bits, if final states are kept.  They may
+ * pass through 2^16 times their values.  No atomics: results are run-to-run bit-identical.  A row of o is not changed by later rows of its sequence,
+ * whatever those hold; an infinity or NaN in a row of k, v or log_decay is in the state from there on and may make all of it NaN.
  */
 size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward);   /* 0 on bad arguments, and where none is needed */
 hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
@@ -613,7 +616,9 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
                                    size_t workspace_bytes, void* stream);
 
 /*
- * The gradients, from the forward's inputs alone (the states are computed again).  final_slots are not looked at.
+ * The gradients, from the forward's inputs alone (the states are computed again).  final_slots are not looked at.  Products as in the forward, the
+ * state's in three parts (dv, rounded to bf16, without d_initial: in two), the weights' in three where gradients are fp32.  Gradients of a row depend on
+ * rows that it is not seen by, or does not see, as little as o does.
  *   d_o        bf16 [total_rows, local_q_heads, head_dim], contiguous
  *   initial    as in the forward
  *   d_final    fp32 [num_seqs, local_kv_heads, head_dim, head_dim], 16-byte aligned: the gradient of the sequences' final states; NULL: zeros

@@ -26,7 +26,7 @@ LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows,
                          bool backward) {
     LinearSizes s{};
     // As many segments as make one round of workgroups, 512 (a sequence ends in half a segment on average); fewer leave the device idle, more cost states
-    // and a second round's end.  (The headline pack, 24 heads: 345 us in segments of 1024, 328 of 1856, 417 of 3072; ten prompts, 16 heads: 158 of 1024,
+    // and a second round's end.  (The headline pack, 24 heads: 345 us in segments of 1024, 328 of 1856; ten prompts, 16 heads: 158 of 1024,
     // 131 of 640, 168 of 384.)  The backward, three workgroups for each, takes some more.  Sequences of up to two segments stay whole: that takes less
     // than a second reading of their keys and values.
     const int64_t longest = max_rows > 0 && max_rows < total_rows ? max_rows : total_rows;
