@@ -28,6 +28,8 @@ __device__ __forceinline__ float sum_up_to(float x) {
     x += moved(x, integral_constant<int, 0x143>{}, integral_constant<int, 0xc>{});      // row_bcast 31: lane 31 to rows 2, 3
     return x;
 }
+// the value of the lane before, 0 in lane 0 (all lanes active): wave_shr 1
+__device__ __forceinline__ float lane_before(float x) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x138, 0xf, 0xf, true)); }
 // over the lanes lane .. 63
 __device__ __forceinline__ float sum_from(float x, int lane) {
 #pragma unroll

@@ -273,7 +273,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int d = p.shape.head_dim, group = ONE ? 1 : p.shape.group;
     const bool mine = NB == kWaves || wave < NB;      // this wave has columns
-    const int hh = lane >> 5;
+    const int hh = lane >> 5, token = LATER ? 63 - lane : lane;      // whose decay the lane has
     TileReads<D> reads;
     reads.init(lane);
     PairOps ops;
@@ -324,7 +324,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
         next_g = 0.f;
         if (ONE || h == 0)
             next_g = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(whole_memory(base_g + first * p.decay_stride),
-                                                                          lane < rows ? (uint32_t)(lane * (int)p.decay_stride * 4) : kNowhere, 0, 0));
+                                                                          token < rows ? (uint32_t)(token * (int)p.decay_stride * 4) : kNowhere, 0, 0));
     };
     auto issue_next = [&](int n, int h) {
         if (h + 1 < group) issue(n, h + 1);
@@ -335,13 +335,15 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
         const int chunk = LATER ? chunks - 1 - n : n;
         const int first = chunk * kLinearChunk;
         if (wave == kWaves - 1) {        // (the wave without a block of pairs)
-            const float sum = sum_up_to(lane < seg.rows - first ? decay_log2(next_g) : 0.f);
-            const float total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum), 63));
-            const float in = LATER ? total - sum : sum, out = LATER ? sum : total - sum;
+            // LATER: the sums are those of the tokens behind each, from the chunk's end on, so that a decay that is NaN reaches the tokens it decays alone
+            const float upto = sum_up_to(token < seg.rows - first ? decay_log2(next_g) : 0.f);
+            const float total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto), 63));
+            const float sum = LATER ? -lane_before(upto) : upto;
+            const float in = LATER ? -sum : sum, out = LATER ? total + sum : total - sum;
             const float next_held = can_hold(held + total) ? held + total : 0.f;
-            sums[lane] = sum;
-            in_weight[lane] = f.scale_in * fast_exp2(in + held);
-            out_weight[lane] = f.scale_state * fast_exp2(out - next_held);
+            sums[token] = sum;
+            in_weight[token] = f.scale_in * fast_exp2(in + held);
+            out_weight[token] = f.scale_state * fast_exp2(out - next_held);
             if (lane == 0) whole[0] = total;
         }
         // tiles of the chunk; those of a head follow in the loop over them

@@ -138,3 +138,26 @@ def test_what_goes_out_in_fp32_is_of_fp32(A, hq, hkv, d, fixed):
         off = np.linalg.norm(got - ref) / np.linalg.norm(ref)
         most = 2.0 ** -20 * (4 if name == "dg" else 1) * (np.sqrt(case.T) if name == "dg" and fixed else 1)
         assert off <= most, (name, off, most)
+
+
+@pytest.mark.parametrize("d,f32", [(64, True), (128, False), (128, True)])
+def test_gradients_of_rows_that_a_bad_value_does_not_reach(A, d, f32):
+    """From the formulas: dk_j and dv_j hold decays behind row j, q and d_o from it on, v_j and k_j; dq_i holds decays, k and v up to row i."""
+    import torch
+    case = Case([50, 400, 90], 4, 2, d, 46, False, True).to_device()
+    clean = case.run_backward(A, f32=f32)
+    bad, rows = 50 + 77, torch.arange(case.T, device="cuda")
+    before, behind, inside = rows < bad, rows > bad, (rows >= 50) & (rows < 450)
+    everywhere, own = torch.ones_like(before), rows != bad
+    # what a bad value in each input leaves as it is: of dq, dk, dv
+    for name, value, keeps in (("tg", float("nan"), (before, ~before, ~before)), ("tq", float("inf"), (everywhere, behind, behind)),
+                               ("tdo", float("nan"), (own, behind, behind)), ("tk", float("-inf"), (before, everywhere, own)),
+                               ("tv", float("nan"), (before, own, everywhere))):
+        x = getattr(case, name)
+        old = x.clone()
+        x[bad] = value
+        got = case.run_backward(A, f32=f32)
+        x.copy_(old)
+        for out, keep in zip(("dq", "dk", "dv"), keeps):
+            assert torch.equal(got[out][keep | ~inside], clean[out][keep | ~inside]), (name, out)
+        assert torch.equal(got["d_initial"][[0, 2]], clean["d_initial"][[0, 2]]), name
