@@ -604,10 +604,12 @@ typedef struct {
  *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 0) bytes, 16-byte aligned; nothing in it outlives the call
  * Sequences longer than some hundred to thousand rows are cut and computed by several workgroups, where there are few (how follows from the batch's counts and
  * max_rows, and so does the workspace: ask with the counts of the call).
- * States, sums and outputs are fp32 until the one rounding of o.  Where states, and the weights of pairs, enter a product on the matrix cores they do
- * so as sums of two bf16 values (2^-17 of each factor, far below o's rounding), the state's sources of three, all 24 bits, if final states are kept.  They may
- * pass through 2^16 times their values.  No atomics: results are run-to-run bit-identical.  A row of o is not changed by later rows of its sequence,
- * whatever those hold; an infinity or NaN in a row of k, v or log_decay is in the state from there on and may make all of it NaN.
+ * States, sums and outputs are fp32 until the one rounding of o.  Where states, and the weights of pairs, enter a product on the matrix cores they do so as
+ * sums of two bf16 values (2^-17 of each factor, far below o's rounding), the state's sources of three, all 24 bits, if final states are kept.  They may pass
+ * through 2^16 times their values.  The weight of a pair is the exponential of a difference of sums of up to 64 decays, and is off by the rounding of these:
+ * 2^-24 of their size (decays of e^-5 in every row: 2^-16 of the weight; in o that is lost in its rounding).  No atomics: results are run-to-run bit-identical.
+ * A row of o is not changed by later rows of its sequence, whatever those hold; an infinity or NaN in a row of k, v or log_decay is in the state from there on
+ * and may make all of it NaN.
  */
 size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward);   /* 0 on bad arguments, and where none is needed */
 hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
@@ -617,8 +619,8 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
 
 /*
  * The gradients, from the forward's inputs alone (the states are computed again).  final_slots are not looked at.  Products as in the forward, the
- * state's in three parts (dv, rounded to bf16, without d_initial: in two), the weights' in three where gradients are fp32.  Gradients of a row depend on
- * rows that it is not seen by, or does not see, as little as o does.
+ * state's in three parts (dv, rounded to bf16, without d_initial: in two), the weights' in three where gradients are fp32.  Rows of dq are not changed by
+ * later rows of their sequence, rows of dk and dv not by earlier ones, whatever those hold.
  *   d_o        bf16 [total_rows, local_q_heads, head_dim], contiguous
  *   initial    as in the forward
  *   d_final    fp32 [num_seqs, local_kv_heads, head_dim, head_dim], 16-byte aligned: the gradient of the sequences' final states; NULL: zeros

@@ -1487,6 +1487,7 @@ hspmd_status hspmd_linear_attn_bwd(const hspmd_linear_batch* batch, const void* 
     if (hspmd_status rc = resolve_scale(scale, batch->head_dim, &p.scale)) return rc;
     if (hspmd_status rc = check_linear_states(batch, initial, batch->initial_slots, "initial", &p.initial)) return rc;
     if (!aligned16(d_final) || !aligned16(d_initial)) return fail(HSPMD_ERR_INVALID_ARG, "d_final and d_initial must be 16-byte aligned");
+    if (d_initial && d_initial == d_final) return fail(HSPMD_ERR_INVALID_ARG, "d_initial must not be d_final");
     if (reinterpret_cast<uintptr_t>(d_log_decay) & 3u) return fail(HSPMD_ERR_INVALID_ARG, "d_log_decay must be 4-byte aligned");
     const bool fixed_sum = d_log_decay && decay_token_stride == 0;     // written whether there are rows or not
     if (batch->num_seqs > 0) {
