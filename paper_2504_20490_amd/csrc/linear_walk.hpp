@@ -235,10 +235,10 @@ __device__ __forceinline__ void add_not_finite(const char* lds, int wave, int la
             if (LATER ? sb < tb : sb > tb) continue;
             const bool sees = sb != tb || (LATER ? r >= t32 : r <= t32);
             // the weight of (s, t32) as it was laid out for the products: lane 32 (r / 4 % 2) + t32, element 4 (r / 8 % 2) + r % 4 of step r / 16
-            const char* const at = lds + L::weights(sb + tb, r / 16, 0) + (32 * (r / 4 % 2) + t32) * 16 + (4 * (r / 8 % 2) + r % 4) * 2;
+            const int at = (32 * (r / 4 % 2) + t32) * 16 + (4 * (r / 8 % 2) + r % 4) * 2;
             float weight = 0.f;
 #pragma unroll
-            for (int part = 0; part < WEIGHT_PARTS; ++part) weight += (float)*reinterpret_cast<const __bf16*>(at + part * 1024);
+            for (int part = 0; part < WEIGHT_PARTS; ++part) weight += (float)*reinterpret_cast<const __bf16*>(lds + L::weights(sb + tb, r / 16, part) + at);
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int col = wave * 32 + 8 * (i / 4) + 4 * hh + i % 4;

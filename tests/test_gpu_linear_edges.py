@@ -161,3 +161,35 @@ def test_gradients_of_rows_that_a_bad_value_does_not_reach(A, d, f32):
         for out, keep in zip(("dq", "dk", "dv"), keeps):
             assert torch.equal(got[out][keep | ~inside], clean[out][keep | ~inside]), (name, out)
         assert torch.equal(got["d_initial"][[0, 2]], clean["d_initial"][[0, 2]]), name
+
+
+@pytest.mark.parametrize("hq,hkv", [(2, 2), (4, 2)])
+@pytest.mark.parametrize("d,f32", [(128, True), (128, False), (64, True), (104, True)])
+def test_infinite_sources_keep_the_sign_of_their_weights(A, hq, hkv, d, f32):
+    """One sequence of one group of 64 rows, an infinite value in one row of a tensor that sources are taken from: the formulas' signed infinities."""
+    import torch
+    case = Case([64], hq, hkv, d, 47, False, False).to_device()
+    q, k, v, do = (host(getattr(case, n)) for n in ("tq", "tk", "tv", "tdo"))
+    group = hq // hkv
+    row, col, head = 45, 3, 1
+    def column(name, out):
+        x = getattr(case, name)
+        old = x.clone()
+        x[row, head, col] = float("inf")
+        if out == "o":
+            got = host(case.run_forward(A, final=False)[0])
+        else:
+            got = host(case.run_backward(A, f32=f32)[out])
+        x.copy_(old)
+        return got[:, :, col]
+    def expect(got, sign, sees):          # (weights whose sign a rounding of 128 terms could turn are let be)
+        clear = sees & (abs(sign) > 2.0 ** -10)
+        assert clear.any() and (np.isposinf(got[clear]) == (sign[clear] > 0)).all() and np.isinf(got[clear]).all()
+        assert np.isfinite(got[~sees]).all()
+    rows = np.arange(64)
+    for h in range(head * group, (head + 1) * group):      # o_i[col] = <q_i, k_row> v_row[col], dq_i[col] = <dO_i, v_row> k_row[col]
+        expect(column("tv", "o")[:, h], q[:, h] @ k[row, head], rows >= row)
+        expect(column("tk", "dq")[:, h], do[:, h] @ v[row, head], rows >= row)
+    head = 1                                               # (a query head, whose KV head is head // group)
+    expect(column("tq", "dk")[:, head // group], v[:, head // group] @ do[row, head], rows <= row)
+    expect(column("tdo", "dv")[:, head // group], k[:, head // group] @ q[row, head], rows <= row)
