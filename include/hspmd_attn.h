@@ -625,7 +625,8 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
  *   initial    as in the forward
  *   d_final    fp32 [num_seqs, local_kv_heads, head_dim, head_dim], 16-byte aligned: the gradient of the sequences' final states; NULL: zeros
  *   dq, dk, dv as in hspmd_attn_varlen_bwd: contiguous, bf16 or fp32; dk, dv summed over the group
- *   d_log_decay  fp32, written; NULL: not wanted.  [total_rows, local_kv_heads], or, with decay_token_stride 0, [local_kv_heads]: the sum over all rows
+ *   d_log_decay  fp32, written; NULL: not wanted, the call then takes a tenth to a fifth less.  [total_rows, local_kv_heads], or, with
+ *              decay_token_stride 0, [local_kv_heads]: the sum over all rows
  *   d_initial  like d_final, written: the gradient of the sequences' initial states (by sequence: where several share a slot the caller adds
  *              them up); NULL: not wanted.  Not d_final itself: other workgroups still read it
  *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 1) bytes, 16-byte aligned

@@ -4,14 +4,16 @@
 namespace hspmd {
 namespace {
 
-template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS, int NB>
+// DECAYS: their gradients are wanted, and with them the dot products, which cost a sixth (headline pack, 24 heads: 955 us with, 855 without; fp32 gradients 1065 and 960,
+// on 32 query heads of 8 KV heads 1460 and 1190).  The other gradients are the same bits.
+template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS, int NB, bool DECAYS>
 __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 && !ONE ? 1 : 2) void linear_bwd_kernel(LinearParams p) {
-    __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS, ONE>::bytes(true, true)];
+    __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS, ONE>::bytes(true, DECAYS || Lds<D, WEIGHT_PARTS, ONE>::kLate)];
     int role, kv_head, slot;
     Segment seg;
     if (!item_of_block<true>(p.shape, 3, role, kv_head, slot) || !find_segment(p.shape, slot, seg)) return;
-    if (role == 0) outputs_of<D, false, true, ONE, 3, WEIGHT_PARTS, NB>(p, dq_routine(p), seg, slot, kv_head, lds);
-    else if (role == 1) outputs_of<D, true, true, ONE, 3, WEIGHT_PARTS, NB>(p, dk_routine(p), seg, slot, kv_head, lds);
+    if (role == 0) outputs_of<D, false, DECAYS, ONE, 3, WEIGHT_PARTS, NB>(p, dq_routine(p), seg, slot, kv_head, lds);
+    else if (role == 1) outputs_of<D, true, DECAYS, ONE, 3, WEIGHT_PARTS, NB>(p, dk_routine(p), seg, slot, kv_head, lds);
     else outputs_of<D, true, false, ONE, V_PARTS, WEIGHT_PARTS, NB>(p, dv_routine(p), seg, slot, kv_head, lds);
 }
 
@@ -94,10 +96,11 @@ __global__ __launch_bounds__(256) void linear_decay_sum_kernel(LinearParams p) {
     if (threadIdx.x == 0) p.d_log_decay[blockIdx.x] = parts[0] + parts[1] + parts[2] + parts[3];
 }
 
-template <int D, bool ONE, int NB>
+template <int D, bool ONE, int NB, bool DECAYS>
 void launch(const LinearParams& p, hipStream_t stream) {
     // dv rounded to bf16 needs two parts of the gradient of the state; that gradient itself, where it goes out, three
-    const auto kernel = p.grad_f32 ? linear_bwd_kernel<D, ONE, 3, 3, NB> : p.d_initial ? linear_bwd_kernel<D, ONE, 2, 3, NB> : linear_bwd_kernel<D, ONE, 2, 2, NB>;
+    const auto kernel = p.grad_f32 ? linear_bwd_kernel<D, ONE, 3, 3, NB, DECAYS>
+                      : p.d_initial ? linear_bwd_kernel<D, ONE, 2, 3, NB, DECAYS> : linear_bwd_kernel<D, ONE, 2, 2, NB, DECAYS>;
     kernel<<<grid_of(p, 3), D / 32 * 64, 0, stream>>>(p);
 }
 
@@ -106,7 +109,11 @@ void launch(const LinearParams& p, hipStream_t stream) {
 hipError_t launch_linear_bwd(const LinearParams& p, hipStream_t stream) {
     if (p.shape.slots > 0) {
         launch_linear_states(p, true, 3, stream);
-        with_shape(p.shape, [&](auto d, auto blocks, auto one) { launch<decltype(d)::value, decltype(one)::value, decltype(blocks)::value>(p, stream); });
+        with_shape(p.shape, [&](auto d, auto blocks, auto one) {
+            const auto with = p.d_log_decay ? launch<decltype(d)::value, decltype(one)::value, decltype(blocks)::value, true>
+                                            : launch<decltype(d)::value, decltype(one)::value, decltype(blocks)::value, false>;
+            with(p, stream);
+        });
     }
     if (p.d_log_decay) {
         if (p.shape.slots > 0) linear_decay_kernel<<<grid_of(p, 1), kDecayWaves * 64, 0, stream>>>(p);

@@ -5,7 +5,7 @@ import threading
 import numpy as np
 import pytest
 
-from linear_util import BF16_HALF_STEP, Case, check, check_backward, check_forward, host
+from linear_util import Case, check, check_backward, check_forward, host
 
 pytestmark = pytest.mark.gpu
 
@@ -193,3 +193,15 @@ def test_infinite_sources_keep_the_sign_of_their_weights(A, hq, hkv, d, f32):
     head = 1                                               # (a query head, whose KV head is head // group)
     expect(column("tq", "dk")[:, head // group], v[:, head // group] @ do[row, head], rows <= row)
     expect(column("tdo", "dv")[:, head // group], k[:, head // group] @ q[row, head], rows <= row)
+
+
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("hq,hkv,d,fixed,states", [(2, 2, 128, False, False), (2, 2, 104, True, True), (8, 2, 128, False, True), (3, 1, 80, True, False),
+                                                   (2, 2, 40, False, True), (6, 2, 24, True, False)])
+def test_gradients_without_the_decays(A, hq, hkv, d, fixed, states, f32):
+    import torch
+    case = Case([700, 33, 0, 129], hq, hkv, d, 48, fixed, states).to_device()
+    want, got = case.run_backward(A, f32=f32), case.run_backward(A, f32=f32, decays=False)
+    assert "dg" not in got
+    assert all(torch.equal(want[n], got[n]) for n in got)
+    check_backward(case, want, f32)
