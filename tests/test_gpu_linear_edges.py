@@ -205,3 +205,50 @@ def test_gradients_without_the_decays(A, hq, hkv, d, fixed, states, f32):
     assert "dg" not in got
     assert all(torch.equal(want[n], got[n]) for n in got)
     check_backward(case, want, f32)
+
+
+def test_the_most_rows(A):
+    """2^25 rows of one head; the last 3000, from a decay that forgets all on, are as they are alone."""
+    import torch
+    T, n, d = 1 << 25, 3000, 8
+    case = Case([n], 1, 1, d, 49, False, False)
+    case.g[0] = -np.inf
+    case.to_device()
+    q, k, v, do = (torch.zeros(T, 1, d, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    g = torch.full((T, 1), -0.01, device="cuda")
+    for whole, part in ((q, case.tq), (k, case.tk), (v, case.tv), (do, case.tdo), (g, case.tg)):
+        if whole is not g:
+            whole[:T - n] = 1.0
+        whole[T - n:] = part
+    batch = A.LinearBatch(torch.tensor([0, 7, T], dtype=torch.int32, device="cuda"))
+    ws = torch.empty(A.linear_attn_workspace_bytes(batch, T, 1, 1, d, backward=True), dtype=torch.uint8, device="cuda")
+    out = {"o": torch.empty_like(q), "dg": torch.empty_like(g), **{x: torch.empty(T, 1, d, device="cuda") for x in ("dq", "dk", "dv")}}
+    A.linear_attn_fwd(batch, q, k, v, g, out["o"], ws)
+    A.linear_attn_bwd(batch, q, k, v, g, do, out["dq"], out["dk"], out["dv"], ws, d_log_decay=out["dg"])
+    # (a constant's steady state: 8 * 1 / (1 - e^-0.01) / sqrt(8); sums of 64 decays and states in fp32: as many roundings as rows are remembered)
+    assert abs(out["o"][T - n - 1].float().mean().item() / (np.sqrt(8) / (1 - np.exp(-0.01))) - 1) < 2.0 ** -8
+    check_forward(case, out["o"][T - n:], None)
+    check_backward(case, {x: out[x][T - n:] for x in ("dq", "dk", "dv", "dg")})
+
+
+@pytest.mark.parametrize("d", [8, 72])
+def test_the_most_sequences(A, d):
+    """2^22 sequences of one row: o = s <q, k> v and its gradients, row by row."""
+    import torch
+    T = 1 << 22
+    q, k, v, do = (torch.randint(-2, 3, (T, 1, d), device="cuda").bfloat16() for _ in range(4))      # (sums of small whole numbers: exact in fp32)
+    g = torch.full((T, 1), -0.5, device="cuda")
+    batch = A.LinearBatch(torch.arange(T + 1, dtype=torch.int32, device="cuda"))
+    ws = torch.empty(A.linear_attn_workspace_bytes(batch, T, 1, 1, d, backward=True), dtype=torch.uint8, device="cuda")
+    o, step = torch.empty_like(q), torch.empty_like(q)
+    A.linear_attn_fwd(batch, q, k, v, g, o, ws, scale=0.5)
+    A.linear_attn_step(A.LinearBatch(), q, k, v, g, step, scale=0.5)
+    want = 0.5 * (q.float() * k.float()).sum(-1, keepdim=True) * v.float()
+    assert torch.equal(o, want.bfloat16()) and torch.equal(step, o)
+    dq, dk, dv = (torch.empty(T, 1, d, device="cuda") for _ in range(3))
+    dg = torch.empty_like(g)
+    A.linear_attn_bwd(batch, q, k, v, g, do, dq, dk, dv, ws, d_log_decay=dg, scale=0.5)
+    pair = 0.5 * (do.float() * v.float()).sum(-1, keepdim=True)
+    assert torch.equal(dq, pair * k.float()) and torch.equal(dk, pair * q.float())
+    assert torch.equal(dv, 0.5 * (q.float() * k.float()).sum(-1, keepdim=True) * do.float())
+    assert (dg == 0).all()
