@@ -606,10 +606,9 @@ typedef struct {
  * max_rows, and so does the workspace: ask with the counts of the call).
  * States, sums and outputs are fp32 until the one rounding of o.  Where states, and the weights of pairs, enter a product on the matrix cores they do so as
  * sums of two bf16 values (2^-17 of each factor, far below o's rounding), the state's sources of three, all 24 bits, if final states are kept.  They may pass
- * through 2^16 times their values.  The weight of a pair is the exponential of a difference of sums of up to 64 decays, and is off by the rounding of these:
- * 2^-24 of their size (decays of e^-5 in every row: 2^-16 of the weight; in o that is lost in its rounding).  No atomics: results are run-to-run bit-identical.
- * A row of o is not changed by later rows of its sequence, whatever those hold; an infinity or NaN in a row of k, v or log_decay is in the state from there on
- * and may make all of it NaN.
+ * through 2^16 times their values.  The exponents of weights are differences of sums held as whole numbers and rests: off by some 2^-21, however strong the
+ * decays. No atomics: results are run-to-run bit-identical. A row of o is not changed by later rows of its sequence, whatever those hold; an infinity or NaN in
+ * a row of k, v or log_decay is in the state from there on and may make all of it NaN.
  */
 size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward);   /* 0 on bad arguments, and where none is needed */
 hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,

@@ -14,6 +14,18 @@ __device__ __forceinline__ float decay_log2(float log_decay) {
     return g < kForgetLog2 ? kForgetLog2 : g;      // (NaN stays)
 }
 
+// The same as a whole number and the rest: sums of the former are exact, those of the latter small, and so is what a difference of two sums is off by, however
+// strong the decays between.  (One sum: decays of e^-5 in every row left errors of 6e-5 in their gradients.)
+struct DecayLog2 {
+    float whole, rest;
+};
+__device__ __forceinline__ DecayLog2 split_decay_log2(float log_decay) {
+    constexpr float kLog2eRest = 1.9259629e-8f;       // log2(e) - kLog2e
+    const float whole = __builtin_rintf(log_decay * kLog2e);
+    if (whole < kForgetLog2) return {kForgetLog2, 0.f};
+    return {whole, __builtin_fmaf(log_decay, kLog2eRest, __builtin_fmaf(log_decay, kLog2e, -whole))};
+}
+
 // inclusive sum over the lanes 0 .. lane of a wave (all lanes active): rows of 16 lanes, then their last lanes to the rows behind
 __device__ __forceinline__ float sum_up_to(float x) {
     const auto moved = [](float v, auto ctrl, auto rows) {

@@ -41,8 +41,8 @@ struct Lds {
     static constexpr int kWaves = D / 32;
     static constexpr int kTile = kLinearChunk * D * 2;
     static constexpr int kB = 0, kC = kTile;
-    static constexpr int kSums = 2 * kTile;                   // running sums of the log decays, weights of targets and of sources, the chunk's decay
-    static constexpr int kA = kSums + (3 * kLinearChunk + 4) * 4;
+    static constexpr int kSums = 2 * kTile;                   // running sums of the log decays in two parts, weights of targets and of sources, the chunk's decay
+    static constexpr int kA = kSums + (4 * kLinearChunk + 4) * 4;
     static constexpr int kWeights = kA + kTile;               // of pairs: [block][step of 16 sources][part][lane]
     // D = 128: with a third part the area would leave room for one workgroup per compute unit.  It goes where the tile of e was, behind the last use of
     // that (with several heads, which share the tile of a KV head, there is no such time)
@@ -283,7 +283,8 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
     char* const tile_c = lds + L::kC;
     char* const tile_e = lds + L::kE;
     float* const sums = reinterpret_cast<float*>(lds + L::kSums);
-    float* const in_weight = sums + kLinearChunk;
+    float* const rests = sums + kLinearChunk;
+    float* const in_weight = rests + kLinearChunk;
     float* const out_weight = in_weight + kLinearChunk;
     float* const whole = out_weight + kLinearChunk;
     float* const near = reinterpret_cast<float*>(lds + L::kNear);
@@ -336,14 +337,19 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
         const int first = chunk * kLinearChunk;
         if (wave == kWaves - 1) {        // (the wave without a block of pairs)
             // LATER: the sums are those of the tokens behind each, from the chunk's end on, so that a decay that is NaN reaches the tokens it decays alone
-            const float upto = sum_up_to(token < seg.rows - first ? decay_log2(next_g) : 0.f);
-            const float total = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto), 63));
-            const float sum = LATER ? -lane_before(upto) : upto;
-            const float in = LATER ? -sum : sum, out = LATER ? total + sum : total - sum;
+            const bool there = token < seg.rows - first;
+            const DecayLog2 g = split_decay_log2(next_g);
+            const float upto = sum_up_to(there ? g.whole : 0.f), upto_rest = sum_up_to(there ? g.rest : 0.f);
+            const float all = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto), 63));
+            const float all_rest = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto_rest), 63)), total = all + all_rest;
+            const float sum = LATER ? -lane_before(upto) : upto, rest = LATER ? -lane_before(upto_rest) : upto_rest;
             const float next_held = can_hold(held + total) ? held + total : 0.f;
+            const float in = LATER ? -sum + (held - rest) : sum + (held + rest);
+            const float out = LATER ? (all + sum) + (all_rest + rest - next_held) : (all - sum) + (all_rest - rest - next_held);
             sums[token] = sum;
-            in_weight[token] = f.scale_in * fast_exp2(in + held);
-            out_weight[token] = f.scale_state * fast_exp2(out - next_held);
+            rests[token] = rest;
+            in_weight[token] = f.scale_in * fast_exp2(in);
+            out_weight[token] = f.scale_state * fast_exp2(out);
             if (lane == 0) whole[0] = total;
         }
         // tiles of the chunk; those of a head follow in the loop over them
@@ -390,12 +396,17 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
 #pragma unroll
                         for (int kk = 0; kk < 2 * NB; ++kk) y = mfma(reads.along(tile_c, sb, kk), reads.along(tile_e, tb, kk), y);
                     }
-                    const float target_sum = LATER ? sums[tb * 32 + t32] - p.scale_log2 : sums[tb * 32 + t32] + p.scale_log2;
+                    const float target_sum = sums[tb * 32 + t32], target_rest = LATER ? rests[tb * 32 + t32] - p.scale_log2 : rests[tb * 32 + t32] + p.scale_log2;
 #pragma unroll
                     for (int i4 = 0; i4 < 4; ++i4) {
                         const f32x4 source_sum = *reinterpret_cast<const f32x4*>(sums + sb * 32 + 8 * i4 + 4 * hh);
+                        const f32x4 source_rest = *reinterpret_cast<const f32x4*>(rests + sb * 32 + 8 * i4 + 4 * hh);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) w[4 * i4 + j] *= fast_exp2(LATER ? source_sum[j] - target_sum : target_sum - source_sum[j]);
+                        for (int j = 0; j < 4; ++j) {
+                            const float between = LATER ? source_sum[j] - target_sum : target_sum - source_sum[j];
+                            w[4 * i4 + j] *= fast_exp2(between + (LATER ? source_rest[j] - target_rest : target_rest - source_rest[j]));
+                        }
+                        if (!kEarly) __builtin_amdgcn_sched_barrier(0);     // (or the sums of all sources are read at once, into registers that are not there)
                     }
                     if (sb == tb) {
 #pragma unroll

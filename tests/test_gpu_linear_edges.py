@@ -252,3 +252,21 @@ def test_the_most_sequences(A, d):
     assert torch.equal(dq, pair * k.float()) and torch.equal(dk, pair * q.float())
     assert torch.equal(dv, 0.5 * (q.float() * k.float()).sum(-1, keepdim=True) * do.float())
     assert (dg == 0).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("rate", [0.5, 2.0, 20.0, "in half of the rows all", "in half of the rows e^-80"])
+def test_strong_decays_keep_fp32(A, rate, d):
+    """As above: a weight's exponent is off by the roundings of sums of 64 rests of at most a half, 2^-20 each at worst."""
+    case = Case([900, 300, 70], 2, 2, d, 50, False, True)
+    rng = np.random.default_rng(51)
+    shape = case.g.shape
+    strong = {"in half of the rows all": -np.inf, "in half of the rows e^-80": -80.0}
+    g = np.where(rng.random(shape) < 0.5, strong[rate], -0.05 * rng.random(shape)) if rate in strong else -rate * rng.exponential(1.0, shape)
+    case.g = g.astype(np.float32).astype(np.float64)
+    case.to_device()
+    out, want = case.run_backward(A), case.backward()
+    out["final"], want["final"] = case.run_forward(A)[1], case.forward()[1]
+    for name, x in out.items():
+        off = np.linalg.norm(host(x) - want[name]) / np.linalg.norm(want[name])
+        assert off <= 2.0 ** -20 * (4 if name == "dg" else 1), (name, off)
