@@ -4,7 +4,7 @@
 namespace hspmd {
 namespace {
 
-// DECAYS: their gradients are wanted, and with them the dot products, which cost a sixth (headline pack, 24 heads: 955 us with, 855 without; fp32 gradients 1065 and 960,
+// DECAYS: their gradients are wanted, and with them the dot products, which cost a sixth (headline pack, 24 heads: 965 us with, 860 without; fp32 gradients 1065 and 960,
 // on 32 query heads of 8 KV heads 1460 and 1190).  The other gradients are the same bits.
 template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS, int NB, bool DECAYS>
 __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 && !ONE ? 1 : 2) void linear_bwd_kernel(LinearParams p) {

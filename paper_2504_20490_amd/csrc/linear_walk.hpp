@@ -11,7 +11,7 @@
 // element, its parts) is shared by 64 targets; with two workgroups per compute unit their tiles fit LDS (62 KB forward, 80 KB backward).
 // The state stays in registers: a wave holds 32 of its columns, 64 registers at head_dim 128, and everything it multiplies comes from LDS.
 // What bounds it: memory in the forward (512 sequences of 1024 tokens, head_dim 128: 130 us, 4.1 TB/s; loads and stores alone 113 us, products
-// alone 92), the chip's power in the backward (24 heads, 32768 tokens: 866 us, 0.6 PFLOP/s of products in their parts at 1.5 GHz).
+// alone 92), the chip's power in the backward (24 heads, 32768 tokens: 907 us, 0.6 PFLOP/s of products in their parts at 1.5 GHz).
 #pragma once
 #include "linear_device.hpp"
 
