@@ -1429,7 +1429,9 @@ static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward,
         p->k_near = take(sizes.k_row_bytes);
         p->k_far = take(sizes.k_row_bytes);
         p->across = take(sizes.slot_bytes);
-        p->decay_sums = take(sizes.slot_bytes);
+        p->decay_sums = reinterpret_cast<double*>(take(sizes.slot_bytes));
+        p->anchors = take(sizes.anchor_bytes);
+        p->d_anchors = take(sizes.anchor_bytes);
     }
     return HSPMD_OK;
 }

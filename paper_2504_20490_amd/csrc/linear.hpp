@@ -50,16 +50,18 @@ struct LinearParams {
     float* q_far;                  // ... and from before the chunk
     float* k_near;                 // [kv_heads][total_rows], likewise
     float* k_far;
-    float* across;                 // [slots][kv_heads]: <S, dS> at a segment's end
-    float* decay_sums;             // [slots][kv_heads]: a segment's share of a fixed decay's gradient
+    float* across;                 // [2][slots][kv_heads]: <S, dS> at a segment's end, and at its start
+    double* decay_sums;            // [slots][kv_heads]: a segment's share of a fixed decay's gradient
+    float* anchors;                // [linear_anchors][kv_heads][linear_anchor_elements]: S at an anchor's start, as the waves hold it ...
+    float* d_anchors;              // ... and dS at its end
 };
 
 struct LinearSizes {
     int32_t seg_rows;              // as in LinearShape
     int64_t slots, entries, windows;
-    size_t state_bytes, decay_bytes, q_row_bytes, k_row_bytes, slot_bytes;
+    size_t state_bytes, decay_bytes, q_row_bytes, k_row_bytes, slot_bytes, anchor_bytes;
     size_t total_bytes(bool backward) const {
-        return backward ? 2 * state_bytes + decay_bytes + 2 * q_row_bytes + 2 * k_row_bytes + 2 * slot_bytes : state_bytes + decay_bytes;
+        return backward ? 2 * state_bytes + decay_bytes + 2 * q_row_bytes + 2 * k_row_bytes + 2 * slot_bytes + 2 * anchor_bytes : state_bytes + decay_bytes;
     }
 };
 LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,

@@ -18,11 +18,54 @@ __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 && !ONE 
 }
 
 // Gradients of the log decays, a workgroup per segment and KV head, from its last chunk to its first, a chunk per wave.  g_t weighs every pair of a
-// token from t on and one before t.  Of these pairs, a chunk's own and those with a token on one side of the chunk come from the dot products;
-// those across the whole chunk, <e^{G_L} S, R>, are what is left of <S, dS> at its end without its own keys.
-constexpr int kDecayWaves = 8;
+// token from t on and one before t.  Of these pairs, a chunk's own and those with a token on one side of the chunk come from the dot products.
+// Those across the whole chunk are <e^{G_L} S, R>, S in front of it and R behind it.  Between two chunks <S, R> is
+//   what lies across the left one + its keys' = what lies across the right one + its queries',
+// so from a place where <S, R> is known, what lies across the chunks next to it follows by differences.  These keep the rounding errors of all terms on the way, where
+// the value itself shrinks with the decays: carried along a segment of 8192 tokens they came to 1e-3 of a fixed decay's gradient, and to as much of rows near others
+// with 10^4 times their gradients.  So <S, R> is known at the segment's ends and at every fourth chunk (its anchors), and a chunk in between takes the
+// difference from the side where the terms on the way are smaller.  (Per row as accurate as <S, R> of every chunk, which would move four times as much.)
+constexpr int kDecayWaves = 8, kDecayBlocks = kDecayWaves / kLinearAnchor;
+static_assert(kLinearAnchor == 4 && kDecayWaves % kLinearAnchor == 0, "the waves of an anchor's chunks share its sum");
+
+struct ChunkSums {
+    float keys, queries;         // pairs of its keys with what is behind it, of its queries with what is in front
+    float most_keys, most_queries;     // by their magnitudes
+    float decay;                 // 0: it leaves nothing
+};
+
+// What lies across each chunk of a block, from the right (its last chunk) to the left, into whole[]; n chunks; *across: <S, R> at the block's right end, then at its left one.
+// `left`: what lies across the leftmost chunk (anchored), or <S, R> at the left end
+__device__ __forceinline__ void across_chunks(const ChunkSums* sums, int n, bool anchored, float left, float* across, float (&whole)[kLinearAnchor]) {
+    float noise[kLinearAnchor], from = *across, most = fabsf(from);      // (noise: the largest term on the way)
+#pragma unroll
+    for (int i = 0; i < kLinearAnchor; ++i) {
+        if (i >= n) break;
+        // a decay that leaves nothing leaves no pairs across it either, not even rounding errors
+        const bool none = sums[i].decay == 0.f;
+        whole[i] = none ? 0.f : from - sums[i].keys;
+        noise[i] = none ? 0.f : fmaxf(most, sums[i].most_keys);
+        from = whole[i] + sums[i].queries;
+        most = fmaxf(noise[i], sums[i].most_queries);
+    }
+    from = left, most = fabsf(left);
+#pragma unroll
+    for (int i = kLinearAnchor - 1; i >= 0; --i) {
+        if (i >= n) continue;
+        const bool known = anchored && i == kLinearAnchor - 1;
+        const float x = known ? left : from - sums[i].queries, noise_x = known ? 0.f : fmaxf(most, sums[i].most_queries);
+        // (a side that a NaN reaches is not taken while there is another)
+        if (x == x && (whole[i] != whole[i] || noise_x < noise[i])) whole[i] = x, noise[i] = noise_x;
+        from = whole[i] + sums[i].keys;
+        most = fmaxf(noise[i], sums[i].most_keys);
+    }
+    *across = whole[kLinearAnchor - 1] + sums[kLinearAnchor - 1].queries;
+}
+
 __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearParams p) {
-    __shared__ float keys[kDecayWaves], queries[kDecayWaves], dead[kDecayWaves], totals[kDecayWaves];
+    __shared__ ChunkSums sums[kDecayWaves];
+    __shared__ float products[kDecayWaves];
+    __shared__ double totals[kDecayWaves];
     const LinearShape& sh = p.shape;
     int role, kv_head, slot;
     if (!item_of_block(sh, 1, role, kv_head, slot)) return;
@@ -31,17 +74,31 @@ __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearPa
     const bool fixed = p.decay_stride == 0;
     Segment seg;
     if (!find_segment(sh, slot, seg)) {
-        if (fixed && threadIdx.x == 0) p.decay_sums[item] = 0.f;
+        if (fixed && threadIdx.x == 0) p.decay_sums[item] = 0.;
         return;
     }
-    float across = p.across[item], total = 0.f;
-    for (int last = (seg.rows + kLinearChunk - 1) / kLinearChunk - 1; last >= 0; last -= kDecayWaves) {
+    const int chunks = (seg.rows + kLinearChunk - 1) / kLinearChunk, elements = linear_anchor_elements(sh.head_dim);
+    float across = p.across[item];
+    const float at_start = p.across[(int64_t)sh.slots * sh.kv_heads + item];
+    double total = 0.;
+    for (int last = chunks - 1; last >= 0; last -= kDecayWaves) {
         const int chunk = last - wave;
         const int64_t row = seg.start + chunk * kLinearChunk + lane;
         const bool there = chunk >= 0 && chunk * kLinearChunk + lane < seg.rows;
-        float near = 0.f, far_q = 0.f, far_k = 0.f, g = 0.f;
+        // <S, R> of the anchor among the wave's four chunks, a quarter of the products
+        const int anchor = last - (wave | (kLinearAnchor - 1));
+        float product = 0.f;
+        if (anchor > 0) {
+            const int64_t from = ((int64_t)linear_anchor(seg.start, anchor, chunks) * sh.kv_heads + kv_head) * elements;
+            f32x4 sum{};
+            for (int i = (wave % kLinearAnchor) * 64 + lane; i < elements / 4; i += kLinearAnchor * 64)
+                sum += reinterpret_cast<const f32x4*>(p.anchors + from)[i] * reinterpret_cast<const f32x4*>(p.d_anchors + from)[i];
+            product = sum[0] + sum[1] + sum[2] + sum[3];
+        }
+        float near = 0.f, far_q = 0.f, far_k = 0.f;
+        DecayLog2 g{0.f, 0.f};
         if (there) {
-            g = decay_log2(p.log_decay[row * p.decay_stride + kv_head]);
+            g = split_decay_log2(p.log_decay[row * p.decay_stride + kv_head]);
             far_k = p.k_far[(int64_t)kv_head * sh.total_rows + row];
             for (int h = 0; h < sh.group; ++h) {
                 const int64_t at = (int64_t)(kv_head * sh.group + h) * sh.total_rows + row;
@@ -50,23 +107,32 @@ __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearPa
             }
             near -= p.k_near[(int64_t)kv_head * sh.total_rows + row];
         }
-        const float all_k = wave_sum(far_k), all_q = wave_sum(far_q), all_g = wave_sum(g);
+        const ChunkSums mine = {wave_sum(far_k), wave_sum(far_q), wave_sum(fabsf(far_k)), wave_sum(fabsf(far_q)), fast_exp2(wave_sum(g.whole) + wave_sum(g.rest))};
+        product = wave_sum(product);
         __syncthreads();                       // (the others have read the round before)
         if (lane == 0) {
-            keys[wave] = all_k;
-            queries[wave] = all_q;
-            // a decay that leaves nothing leaves no pairs across it either, not even rounding errors
-            dead[wave] = fast_exp2(all_g) == 0.f ? 1.f : 0.f;
+            sums[wave] = mine;
+            products[wave] = product;
         }
         __syncthreads();
-        float whole = 0.f, mine = 0.f;
+        float whole_here = 0.f;
 #pragma unroll
-        for (int w = 0; w < kDecayWaves; ++w) {
-            whole = dead[w] != 0.f ? 0.f : across - keys[w];
-            if (w == wave) mine = whole;
-            across = whole + queries[w];
+        for (int b = 0; b < kDecayBlocks; ++b) {
+            const int first = b * kLinearAnchor, n = min(last - first + 1, kLinearAnchor);
+            if (n <= 0) break;
+            float left = at_start, whole[kLinearAnchor] = {};
+            const bool anchored = last - first - (kLinearAnchor - 1) > 0;
+            if (anchored) {
+                left = 0.f;
+#pragma unroll
+                for (int i = 0; i < kLinearAnchor; ++i) left += products[first + i];
+                left *= sums[first + kLinearAnchor - 1].decay;
+            }
+            across_chunks(sums + first, n, anchored, left, &across, whole);
+#pragma unroll
+            for (int i = 0; i < kLinearAnchor; ++i) whole_here = first + i == wave ? whole[i] : whole_here;
         }
-        const float grad = sum_from(near + far_q, lane) + (sum_up_to(far_k) - far_k) + mine;
+        const float grad = sum_from(near + far_q, lane) + (sum_up_to(far_k) - far_k) + whole_here;
         if (there) {
             if (fixed) total += grad;
             else p.d_log_decay[row * sh.kv_heads + kv_head] = grad;
@@ -77,7 +143,7 @@ __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearPa
         if (lane == 0) totals[wave] = total;
         __syncthreads();
         if (threadIdx.x == 0) {
-            total = 0.f;
+            total = 0.;
 #pragma unroll
             for (int w = 0; w < kDecayWaves; ++w) total += totals[w];
             p.decay_sums[item] = total;
@@ -87,13 +153,13 @@ __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearPa
 
 // A fixed decay's gradient is the sum over all tokens: one workgroup per KV head, in a fixed order.
 __global__ __launch_bounds__(256) void linear_decay_sum_kernel(LinearParams p) {
-    __shared__ float parts[4];
-    float sum = 0.f;
+    __shared__ double parts[4];
+    double sum = 0.;
     for (int64_t i = threadIdx.x; i < p.shape.slots; i += 256) sum += p.decay_sums[i * p.shape.kv_heads + blockIdx.x];
     sum = wave_sum(sum);
     if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = sum;
     __syncthreads();
-    if (threadIdx.x == 0) p.d_log_decay[blockIdx.x] = parts[0] + parts[1] + parts[2] + parts[3];
+    if (threadIdx.x == 0) p.d_log_decay[blockIdx.x] = (float)(parts[0] + parts[1] + parts[2] + parts[3]);
 }
 
 template <int D, bool ONE, int NB, bool DECAYS>

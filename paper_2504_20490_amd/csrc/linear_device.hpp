@@ -51,7 +51,8 @@ __device__ __forceinline__ float sum_from(float x, int lane) {
     }
     return x;
 }
-__device__ __forceinline__ float wave_sum(float x) {
+template <typename T>
+__device__ __forceinline__ T wave_sum(T x) {
 #pragma unroll
     for (int step = 1; step < 64; step *= 2) x += __shfl_xor(x, step, 64);
     return x;

@@ -47,7 +47,8 @@ LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows,
     s.decay_bytes = rounded(s.entries * kv_heads * 4);
     s.q_row_bytes = rounded((int64_t)total_rows * q_heads * 4);
     s.k_row_bytes = rounded((int64_t)total_rows * kv_heads * 4);
-    s.slot_bytes = rounded(s.slots * kv_heads * 4);
+    s.slot_bytes = rounded(s.slots * kv_heads * 8);
+    s.anchor_bytes = rounded(linear_anchors(total_rows) * kv_heads * linear_anchor_elements(head_dim) * 4);
     return s;
 }
 

@@ -39,6 +39,16 @@ HSPMD_LINEAR_INDEX int64_t linear_slots(int64_t total_rows, int64_t num_seqs, in
 HSPMD_LINEAR_INDEX int linear_first_entry(int start, int seg_rows) { return (int)(2 * (int64_t)start / seg_rows); }
 HSPMD_LINEAR_INDEX int64_t linear_entries(int64_t total_rows, int64_t seg_rows) { return 2 * total_rows / seg_rows + 1; }
 
+// Anchors: chunks of a segment whose states are kept for the decays' gradients, the fourth from its end and every fourth in front of that, without the segment's first.
+// A segment's number of them is at most (rows - 1) / 256, so they have entries of their own from start / 256 on.
+constexpr int kLinearAnchor = 4;     // chunks
+HSPMD_LINEAR_INDEX int linear_first_anchor(int start) { return start / (kLinearAnchor * kLinearChunk); }
+HSPMD_LINEAR_INDEX int64_t linear_anchors(int64_t total_rows) { return total_rows / (kLinearAnchor * kLinearChunk); }
+HSPMD_LINEAR_INDEX bool linear_is_anchor(int chunk, int chunks) { return chunk > 0 && (chunks - chunk) % kLinearAnchor == 0; }
+HSPMD_LINEAR_INDEX int linear_anchor(int start, int chunk, int chunks) { return linear_first_anchor(start) + (chunks - chunk) / kLinearAnchor - 1; }
+// What an anchor keeps: a state's rows and columns that head_dim takes, in whole groups of 16 and 32
+HSPMD_LINEAR_INDEX int linear_anchor_elements(int head_dim) { return (head_dim + 15) / 16 * 16 * ((head_dim + 31) / 32 * 32); }
+
 // The sequence of several segments that starts in window w (tokens w * seg_rows .. + seg_rows - 1), if there is one, is the last that
 // starts there; windows are what the launch that passes states from segment to segment goes by.
 HSPMD_LINEAR_INDEX int64_t linear_windows(int64_t total_rows, int64_t seg_rows) { return total_rows / seg_rows + 1; }

@@ -33,6 +33,7 @@ struct Routine {
     bool transposed;         // the state is b c^T transposed to how it lies in memory
     float* near;             // DOTS: [heads][total_rows], see LinearParams
     float* far;
+    float* anchors;          // DOTS: where the states of anchors go
 };
 
 // What a workgroup keeps in LDS.  WEIGHT_PARTS: bf16 values per weight of a pair; ONE: a KV head has one query head
@@ -164,6 +165,20 @@ struct State {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) m[(row + i) * d + col] = x[db][8 * h + i];
                 }
+            }
+    }
+    // 2^log2 times it as it lies in the registers, without the rows that nothing of head_dim is in
+    __device__ __forceinline__ void keep(float* m, int d, float log2, int wave, int lane) const {
+        const float by = fast_exp2(log2);
+        const __amdgpu_buffer_rsrc_t rsrc = whole_memory(m + wave * ((d + 15) / 16 * 16 * 32));
+#pragma unroll
+        for (int db = 0; db < NB; ++db)
+#pragma unroll
+            for (int i = 0; i < 16; i += 4) {
+                union { f32x4 f; u32x4 u; } y;
+                y.f = f32x4{x[db][i] * by, x[db][i + 1] * by, x[db][i + 2] * by, x[db][i + 3] * by};
+                if (db * 32 + i / 8 * 16 < d) __builtin_amdgcn_raw_buffer_store_b128(y.u, rsrc, lane * 16, (db * 16 + i) * 256, 0);
+                __builtin_amdgcn_sched_barrier(0);      // (one at a time: else the products take registers that are not there)
             }
     }
     // this lane's share of the sum over all elements of this state times the one in memory
@@ -381,6 +396,11 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             __syncthreads();
             if (first_head) chunk_decay = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(whole[0])));
 
+            if constexpr (DOTS) {
+                // the state in front of this chunk (LATER: behind it), for the gradients of the decays
+                if (first_head && mine && linear_is_anchor(chunk, chunks))
+                    S.keep(f.anchors + ((int64_t)linear_anchor(seg.start, chunk, chunks) * p.shape.kv_heads + kv_head) * linear_anchor_elements(d), d, held, wave, lane);
+            }
             if (!OUT) issue_next(n, h);
             if constexpr (OUT) {
                 bf16x8 late[2];        // (kLate: a wave has one block at most)
@@ -592,17 +612,17 @@ __device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine&
     if (from) S.load(from, d, f.transposed, wave, lane);
     else S.clear(bad ? __builtin_nanf("") : 0.f);
     walk<D, LATER, true, DOTS, ONE, PARTS, WEIGHT_PARTS, NB>(p, f, seg, kv_head, lds, S);
-    if (!LATER && DOTS) {
-        // <S, dS> behind the segment's last token: what the gradient of its decays starts from
-        const float* const d_end = reaching_state<true>(p, seg, kv_head, &bad);
-        float sum = d_end ? wave_sum(S.dot(d_end, d, f.transposed, wave, lane)) : 0.f;
+    if (DOTS) {
+        // <S, dS> behind the segment's last token, or (LATER) in front of its first: what the gradients of its decays start from
+        const float* const other = reaching_state<!LATER>(p, seg, kv_head, &bad);
+        float sum = other ? wave_sum(S.dot(other, d, f.transposed, wave, lane)) : bad ? __builtin_nanf("") : 0.f;
         float* const parts = reinterpret_cast<float*>(lds);
         if (lane == 0) parts[wave] = sum;
         __syncthreads();
         if (threadIdx.x == 0) {
             sum = 0.f;
             for (int w = 0; w < D / 32; ++w) sum += parts[w];
-            p.across[(int64_t)slot * p.shape.kv_heads + kv_head] = sum;
+            p.across[((LATER ? p.shape.slots : 0) + (int64_t)slot) * p.shape.kv_heads + kv_head] = sum;
         }
     }
     if (!DOTS && !f.transposed) {
@@ -632,16 +652,16 @@ __device__ __forceinline__ bool item_of_block(const LinearShape& shape, int role
 }
 
 __device__ __forceinline__ Routine forward_routine(const LinearParams& p) {
-    return Routine{p.q, p.k, p.v, nullptr, p.q_stride, p.kv_stride, p.kv_stride, 0, p.scale, 1.f, p.o, false, nullptr, nullptr};
+    return Routine{p.q, p.k, p.v, nullptr, p.q_stride, p.kv_stride, p.kv_stride, 0, p.scale, 1.f, p.o, false, nullptr, nullptr, nullptr};
 }
 __device__ __forceinline__ Routine dq_routine(const LinearParams& p) {
-    return Routine{p.d_o, p.v, p.k, p.q, p.do_stride, p.kv_stride, p.kv_stride, p.q_stride, p.scale, 1.f, p.dq, true, p.q_near, p.q_far};
+    return Routine{p.d_o, p.v, p.k, p.q, p.do_stride, p.kv_stride, p.kv_stride, p.q_stride, p.scale, 1.f, p.dq, true, p.q_near, p.q_far, p.anchors};
 }
 __device__ __forceinline__ Routine dk_routine(const LinearParams& p) {
-    return Routine{p.v, p.d_o, p.q, p.k, p.kv_stride, p.do_stride, p.q_stride, p.kv_stride, 1.f, p.scale, p.dk, true, p.k_near, p.k_far};
+    return Routine{p.v, p.d_o, p.q, p.k, p.kv_stride, p.do_stride, p.q_stride, p.kv_stride, 1.f, p.scale, p.dk, true, p.k_near, p.k_far, p.d_anchors};
 }
 __device__ __forceinline__ Routine dv_routine(const LinearParams& p) {
-    return Routine{p.k, p.q, p.d_o, nullptr, p.kv_stride, p.q_stride, p.do_stride, 0, 1.f, p.scale, p.dv, false, nullptr, nullptr};
+    return Routine{p.k, p.q, p.d_o, nullptr, p.kv_stride, p.q_stride, p.do_stride, 0, 1.f, p.scale, p.dv, false, nullptr, nullptr, nullptr};
 }
 
 // calls f(tile width, blocks of 32 columns, one query head per KV head) as constants
