@@ -606,7 +606,7 @@ typedef struct {
  * max_rows, and so does the workspace: ask with the counts of the call).
  * States, sums and outputs are fp32 until the one rounding of o.  Where states, and the weights of pairs, enter a product on the matrix cores they do so as
  * sums of two bf16 values (2^-17 of each factor, far below o's rounding), the state's sources of three, all 24 bits, if final states are kept.  They may pass
- * through 2^16 times their values.  The exponents of weights are differences of sums held as whole numbers and rests: off by some 2^-21, however strong the
+ * through 2^16 times their values.  The exponents of weights are differences of sums held as multiples of 2^-10 and rests: rounded once, however strong the
  * decays. No atomics: results are run-to-run bit-identical. A row of o is not changed by later rows of its sequence, whatever those hold; an infinity or NaN in
  * a row of k, v or log_decay is in the state from there on and may make all of it NaN.
  */
@@ -625,7 +625,8 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
  *   d_final    fp32 [num_seqs, local_kv_heads, head_dim, head_dim], 16-byte aligned: the gradient of the sequences' final states; NULL: zeros
  *   dq, dk, dv as in hspmd_attn_varlen_bwd: contiguous, bf16 or fp32; dk, dv summed over the group
  *   d_log_decay  fp32, written; NULL: not wanted, the call then takes a tenth to a fifth less.  [total_rows, local_kv_heads], or, with
- *              decay_token_stride 0, [local_kv_heads]: the sum over all rows
+ *              decay_token_stride 0, [local_kv_heads]: the sum over all rows, in 64 bits.  A row's is off by roundings of the terms that its own 64 rows
+ *              take part in (some 2^-18 of them at worst, all in fp32), however large those elsewhere in the sequence are
  *   d_initial  like d_final, written: the gradient of the sequences' initial states (by sequence: where several share a slot the caller adds
  *              them up); NULL: not wanted.  Not d_final itself: other workgroups still read it
  *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 1) bytes, 16-byte aligned

@@ -1419,7 +1419,9 @@ static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward,
         at += bytes;
         return r;
     };
-    p->scale_log2 = std::log2(p->scale);
+    const double scale_log2 = std::log2((double)p->scale);
+    p->scale_log2.whole = (float)(std::rint(scale_log2 * 1024) / 1024);
+    p->scale_log2.rest = (float)(scale_log2 - p->scale_log2.whole);
     p->states = take(sizes.state_bytes);
     p->seg_decay = take(sizes.decay_bytes);
     if (backward) {

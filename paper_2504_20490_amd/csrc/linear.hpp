@@ -25,6 +25,11 @@ struct LinearStates {
     int32_t num_slots;
 };
 
+// A log2 as a multiple of 2^-10 and the rest
+struct DecayLog2 {
+    float whole, rest;
+};
+
 struct LinearParams {
     LinearShape shape;
     const uint16_t* q;
@@ -33,7 +38,8 @@ struct LinearParams {
     const uint16_t* d_o;           // backward only
     const float* log_decay;
     int64_t q_stride, kv_stride, do_stride, decay_stride;
-    float scale, scale_log2;       // and its log2
+    float scale;
+    DecayLog2 scale_log2;          // its log2
     LinearStates initial, final;   // backward: `final` is the gradient that comes in (read)
     void* o;                       // forward: bf16
     void* dq;
@@ -50,7 +56,7 @@ struct LinearParams {
     float* q_far;                  // ... and from before the chunk
     float* k_near;                 // [kv_heads][total_rows], likewise
     float* k_far;
-    float* across;                 // [2][slots][kv_heads]: <S, dS> at a segment's end, and at its start
+    float* across;                 // [2][slots][kv_heads]: <S, dS> at a segment's end, and at a sequence's start (its first slot)
     double* decay_sums;            // [slots][kv_heads]: a segment's share of a fixed decay's gradient
     float* anchors;                // [linear_anchors][kv_heads][linear_anchor_elements]: S at an anchor's start, as the waves hold it ...
     float* d_anchors;              // ... and dS at its end

@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kDecayWaves * 64) void linear_decay_kernel(LinearPa
     }
     const int chunks = (seg.rows + kLinearChunk - 1) / kLinearChunk, elements = linear_anchor_elements(sh.head_dim);
     float across = p.across[item];
-    const float at_start = p.across[(int64_t)sh.slots * sh.kv_heads + item];
+    const float at_start = seg.index > 0 ? p.across[item - sh.kv_heads] : p.across[(int64_t)sh.slots * sh.kv_heads + item];
     double total = 0.;
     for (int last = chunks - 1; last >= 0; last -= kDecayWaves) {
         const int chunk = last - wave;

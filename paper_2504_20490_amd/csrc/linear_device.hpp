@@ -14,14 +14,14 @@ __device__ __forceinline__ float decay_log2(float log_decay) {
     return g < kForgetLog2 ? kForgetLog2 : g;      // (NaN stays)
 }
 
-// The same as a whole number and the rest: sums of the former are exact, those of the latter small, and so is what a difference of two sums is off by, however
-// strong the decays between.  (One sum: decays of e^-5 in every row left errors of 6e-5 in their gradients.)
-struct DecayLog2 {
-    float whole, rest;
-};
+// The same as a multiple of 2^-10 and the rest: sums of 64 of the former, at most 10240, are exact, those of the latter below 2^-5 and off by 2^-30, and so is what a
+// difference of two sums is off by, however strong the decays between.  All that compute the weight of a pair, from either end of a chunk, then come to the same
+// bits, but for a rounding here and there: the decays' gradients are differences between sums of such weights.  (One sum: decays of e^-5 in every row left errors of 6e-5
+// in their gradients; whole numbers and rests: a fixed decay of e^-1 5e-5 in the gradient over 8192 rows.)
+constexpr float kDecayStep = 0x1p-10f;
 __device__ __forceinline__ DecayLog2 split_decay_log2(float log_decay) {
     constexpr float kLog2eRest = 1.9259629e-8f;       // log2(e) - kLog2e
-    const float whole = __builtin_rintf(log_decay * kLog2e);
+    const float whole = __builtin_rintf(log_decay * (kLog2e / kDecayStep)) * kDecayStep;
     if (whole < kForgetLog2) return {kForgetLog2, 0.f};
     return {whole, __builtin_fmaf(log_decay, kLog2eRest, __builtin_fmaf(log_decay, kLog2e, -whole))};
 }

@@ -21,7 +21,7 @@ __global__ __launch_bounds__(D / 32 * 64, 2) void linear_state_kernel(LinearPara
     const int64_t own = (int64_t)(seg.entry + seg.index) * p.shape.kv_heads + kv_head;
     float* const to = role == 0 ? p.states + (own + p.shape.kv_heads) * d * d : p.d_states + (own - p.shape.kv_heads) * d * d;
     S.store(to, d, wave, lane);
-    if (threadIdx.x == 0 && (role == 0 || last)) p.seg_decay[own] = decay;
+    if (wave == D / 32 - 1 && lane == 0 && (role == 0 || last)) p.seg_decay[own] = decay;
 }
 
 // Passes states from segment to segment, elementwise: entry b holds what segment b - 1 adds and receives the state at the start of segment b.

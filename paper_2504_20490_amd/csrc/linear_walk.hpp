@@ -42,8 +42,9 @@ struct Lds {
     static constexpr int kWaves = D / 32;
     static constexpr int kTile = kLinearChunk * D * 2;
     static constexpr int kB = 0, kC = kTile;
-    static constexpr int kSums = 2 * kTile;                   // running sums of the log decays in two parts, weights of targets and of sources, the chunk's decay
-    static constexpr int kA = kSums + (4 * kLinearChunk + 4) * 4;
+    static constexpr int kSums = 2 * kTile;                   // running sums of the log decays in two parts, weights of targets and of sources, `passing`, two addresses
+    static constexpr int kLater = kSums + (4 * kLinearChunk + 8) * 4;
+    static constexpr int kA = kSums + (4 * kLinearChunk + 8) * 4 + 16;
     static constexpr int kWeights = kA + kTile;               // of pairs: [block][step of 16 sources][part][lane]
     // D = 128: with a third part the area would leave room for one workgroup per compute unit.  It goes where the tile of e was, behind the last use of
     // that (with several heads, which share the tile of a KV head, there is no such time)
@@ -181,19 +182,21 @@ struct State {
                 __builtin_amdgcn_sched_barrier(0);      // (one at a time: else the products take registers that are not there)
             }
     }
-    // this lane's share of the sum over all elements of this state times the one in memory
-    __device__ __forceinline__ float dot(const float* m, int d, bool transposed, int wave, int lane) const {
-        const int col = wave * 32 + (lane & 31);
+    // this lane's share of the sum over all elements of this state times the one in memory, which is its transpose
+    __device__ __forceinline__ float dot_transposed(const float* m, int d, int wave, int lane) const {
+        const __amdgpu_buffer_rsrc_t rsrc = whole_memory(m);
+        const int col = wave * 32 + (lane & 31), row = (lane >> 5) * 8;
         float sum = 0.f;
 #pragma unroll
         for (int db = 0; db < NB; ++db)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int row = db * 32 + h * 16 + (lane >> 5) * 8;
-                if (row < d && col < d) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sum += x[db][8 * h + i] * (transposed ? m[(int64_t)col * d + row + i] : m[(row + i) * d + col]);
-                }
+            for (int i = 0; i < 16; i += 4) {
+                const int at = row + db * 32 + i / 8 * 16 + i % 8;
+                union { u32x4 u; f32x4 f; } y;
+                y.u = __builtin_amdgcn_raw_buffer_load_b128(rsrc, at < d && col < d ? (uint32_t)(col * d + at) * 4u : kNowhere, 0, 0);
+                // (a state's columns behind head_dim may hold NaN, of weights that are)
+                const float part = x[db][i] * y.f[0] + x[db][i + 1] * y.f[1] + x[db][i + 2] * y.f[2] + x[db][i + 3] * y.f[3];
+                sum += at < d && col < d ? part : 0.f;
             }
         return sum;
     }
@@ -278,7 +281,7 @@ __device__ __forceinline__ bool can_hold(float log2) { return __builtin_fabsf(lo
 //   NB      blocks of 32 columns that head_dim takes; steps, and waves, that would compute on columns behind them pass
 //   PARTS, WEIGHT_PARTS   bf16 values that the state and its sources, and the weights of pairs, enter products as; three of the weights go with
 //           fp32 outputs, two with bf16
-// Returns the log2 of the segment's decay.
+// Returns the log2 of the segment's decay, to the last wave and without OUT.
 template <int D, bool LATER, bool OUT, bool DOTS, bool ONE, int PARTS, int WEIGHT_PARTS, int NB>
 __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, const Segment& seg, int kv_head, char* lds, State<NB>& S) {
     constexpr bool OUT_F32 = WEIGHT_PARTS == 3;
@@ -301,13 +304,15 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
     float* const rests = sums + kLinearChunk;
     float* const in_weight = rests + kLinearChunk;
     float* const out_weight = in_weight + kLinearChunk;
-    float* const whole = out_weight + kLinearChunk;
+    // What goes with the state from chunk to chunk, here so that it takes no registers in the loop.  0, 1: log2 of what the state is held as behind the chunk, in two parts;
+    // 2: the same in front of it; 3: what the state's registers are multiplied by; 4: the sum of 0 and 1
+    float* const passing = out_weight + kLinearChunk;
     float* const near = reinterpret_cast<float*>(lds + L::kNear);
     float* const far = reinterpret_cast<float*>(lds + L::kFar);
 
     const int chunks = (seg.rows + kLinearChunk - 1) / kLinearChunk;
     const int target_heads = LATER ? p.shape.kv_heads : p.shape.q_heads;
-    float all_decay = 0.f, held = 0.f;
+    float all_decay = 0.f, all_decay_rest = 0.f;
 
     TileLoad<D> la, lb, lc, le;
     float next_g = 0.f;
@@ -356,16 +361,22 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             const DecayLog2 g = split_decay_log2(next_g);
             const float upto = sum_up_to(there ? g.whole : 0.f), upto_rest = sum_up_to(there ? g.rest : 0.f);
             const float all = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto), 63));
-            const float all_rest = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto_rest), 63)), total = all + all_rest;
+            const float all_rest = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(upto_rest), 63));
             const float sum = LATER ? -lane_before(upto) : upto, rest = LATER ? -lane_before(upto_rest) : upto_rest;
-            const float next_held = can_hold(held + total) ? held + total : 0.f;
-            const float in = LATER ? -sum + (held - rest) : sum + (held + rest);
-            const float out = LATER ? (all + sum) + (all_rest + rest - next_held) : (all - sum) + (all_rest - rest - next_held);
+            const float held = n > 0 ? passing[0] : 0.f, held_rest = n > 0 ? passing[1] : 0.f;
+            const bool holds = can_hold(held + all);
+            const float left = holds ? held + all : 0.f, left_rest = holds ? held_rest + all_rest : 0.f;
+            const float in = LATER ? (held - sum) + (held_rest - rest) : (held + sum) + (held_rest + rest);
+            const float out = LATER ? (all + sum - left) + (all_rest + rest - left_rest) : (all - sum - left) + (all_rest - rest - left_rest);
             sums[token] = sum;
             rests[token] = rest;
             in_weight[token] = f.scale_in * fast_exp2(in);
             out_weight[token] = f.scale_state * fast_exp2(out);
-            if (lane == 0) whole[0] = total;
+            if (lane == 0) {
+                passing[0] = left, passing[1] = left_rest, passing[2] = held + held_rest, passing[4] = left + left_rest;
+                passing[3] = holds ? 1.f : fast_exp2((held + all) + (held_rest + all_rest));
+            }
+            if (!OUT) all_decay += all, all_decay_rest += all_rest;
         }
         // tiles of the chunk; those of a head follow in the loop over them
         if (LATER && OUT) {
@@ -377,7 +388,6 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             lc.put(tile_c);
         }
         f32x16 out_of_heads[2];            // LATER: summed over the heads
-        float chunk_decay = 0.f;
         for (int h = 0; h < group; ++h) {
             f32x16 out_of_head[2];
             f32x16 (&out)[2] = LATER ? out_of_heads : out_of_head;
@@ -394,12 +404,10 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
                 lc.put(tile_c);
             }
             __syncthreads();
-            if (first_head) chunk_decay = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(whole[0])));
-
             if constexpr (DOTS) {
                 // the state in front of this chunk (LATER: behind it), for the gradients of the decays
                 if (first_head && mine && linear_is_anchor(chunk, chunks))
-                    S.keep(f.anchors + ((int64_t)linear_anchor(seg.start, chunk, chunks) * p.shape.kv_heads + kv_head) * linear_anchor_elements(d), d, held, wave, lane);
+                    S.keep(f.anchors + ((int64_t)linear_anchor(seg.start, chunk, chunks) * p.shape.kv_heads + kv_head) * linear_anchor_elements(d), d, passing[2], wave, lane);
             }
             if (!OUT) issue_next(n, h);
             if constexpr (OUT) {
@@ -416,7 +424,8 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
 #pragma unroll
                         for (int kk = 0; kk < 2 * NB; ++kk) y = mfma(reads.along(tile_c, sb, kk), reads.along(tile_e, tb, kk), y);
                     }
-                    const float target_sum = sums[tb * 32 + t32], target_rest = LATER ? rests[tb * 32 + t32] - p.scale_log2 : rests[tb * 32 + t32] + p.scale_log2;
+                    const float target_sum = LATER ? sums[tb * 32 + t32] - p.scale_log2.whole : sums[tb * 32 + t32] + p.scale_log2.whole;
+                    const float target_rest = LATER ? rests[tb * 32 + t32] - p.scale_log2.rest : rests[tb * 32 + t32] + p.scale_log2.rest;
 #pragma unroll
                     for (int i4 = 0; i4 < 4; ++i4) {
                         const f32x4 source_sum = *reinterpret_cast<const f32x4*>(sums + sb * 32 + 8 * i4 + 4 * hh);
@@ -544,8 +553,8 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             }
             if (OUT && !kEarly) issue_next(n, h);
             if (mine && (LATER || last_head)) {
-                if ((!LATER || first_head) && !can_hold(held + chunk_decay)) {
-                    const float left = fast_exp2(held + chunk_decay);
+                const float left = __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(passing[3])));
+                if ((!LATER || first_head) && left != 1.f) {
 #pragma unroll
                     for (int db = 0; db < NB; ++db)
 #pragma unroll
@@ -578,17 +587,15 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
             }
             __syncthreads();
         }
-        all_decay += chunk_decay;
-        held = can_hold(held + chunk_decay) ? held + chunk_decay : 0.f;
     }
-    if (held != 0.f) {
-        const float left = fast_exp2(held);
+    if (chunks > 0 && passing[4] != 0.f) {
+        const float left = fast_exp2(passing[4]);
 #pragma unroll
         for (int db = 0; db < NB; ++db)
 #pragma unroll
             for (int i = 0; i < 16; ++i) S.x[db][i] *= left;
     }
-    return all_decay;
+    return all_decay + all_decay_rest;
 }
 
 // the state at a segment's start (LATER: the gradient at its end) as it lies in memory; NULL: zeros.  *bad: it is one that does not exist
@@ -608,21 +615,36 @@ __device__ __forceinline__ void outputs_of(const LinearParams& p, const Routine&
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = p.shape.head_dim;
     State<NB> S;
     bool bad;
+    // <S, dS> behind the segment's last token, or (LATER) in front of the sequence's first: what the gradients of its decays start from.  Where the other state is and the
+    // sum goes waits in LDS: in registers, it would cost the walk some
+    uint64_t* const later = reinterpret_cast<uint64_t*>(lds + Lds<D, WEIGHT_PARTS, ONE>::kLater);
+    if (DOTS && threadIdx.x == 0) {
+        const float* other = nullptr;
+        bad = false;
+        if (!LATER || seg.index == 0) other = reaching_state<!LATER>(p, seg, kv_head, &bad);
+        float* const to = p.across + ((LATER ? p.shape.slots : 0) + (int64_t)slot) * p.shape.kv_heads + kv_head;
+        if (!other) *to = bad ? __builtin_nanf("") : 0.f;
+        later[0] = reinterpret_cast<uint64_t>(other);
+        later[1] = reinterpret_cast<uint64_t>(to);
+    }
     const float* const from = reaching_state<LATER>(p, seg, kv_head, &bad);
     if (from) S.load(from, d, f.transposed, wave, lane);
     else S.clear(bad ? __builtin_nanf("") : 0.f);
     walk<D, LATER, true, DOTS, ONE, PARTS, WEIGHT_PARTS, NB>(p, f, seg, kv_head, lds, S);
     if (DOTS) {
-        // <S, dS> behind the segment's last token, or (LATER) in front of its first: what the gradients of its decays start from
-        const float* const other = reaching_state<!LATER>(p, seg, kv_head, &bad);
-        float sum = other ? wave_sum(S.dot(other, d, f.transposed, wave, lane)) : bad ? __builtin_nanf("") : 0.f;
-        float* const parts = reinterpret_cast<float*>(lds);
-        if (lane == 0) parts[wave] = sum;
         __syncthreads();
-        if (threadIdx.x == 0) {
-            sum = 0.f;
-            for (int w = 0; w < D / 32; ++w) sum += parts[w];
-            p.across[((LATER ? p.shape.slots : 0) + (int64_t)slot) * p.shape.kv_heads + kv_head] = sum;
+        const uint32_t low = __builtin_amdgcn_readfirstlane((uint32_t)later[0]), high = __builtin_amdgcn_readfirstlane((uint32_t)(later[0] >> 32));
+        const float* const other = reinterpret_cast<const float*>((uint64_t)high << 32 | low);
+        if (other) {
+            float* const parts = reinterpret_cast<float*>(lds);
+            const float sum = wave_sum(S.dot_transposed(other, d, wave, lane));
+            if (lane == 0) parts[wave] = sum;
+            __syncthreads();
+            if (threadIdx.x == 0) {
+                float all = 0.f;
+                for (int w = 0; w < D / 32; ++w) all += parts[w];
+                *reinterpret_cast<float*>(later[1]) = all;
+            }
         }
     }
     if (!DOTS && !f.transposed) {

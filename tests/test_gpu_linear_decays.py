@@ -68,3 +68,19 @@ def test_a_fixed_decays_gradient_over_a_long_sequence(A, n, hq, hkv, d, states, 
     rows = case.backward()["dg"]
     off, may = np.abs(got - rows.sum(0)), 16 * 2.0 ** -18 * np.linalg.norm(rows, axis=0)
     assert (off <= may).all(), (off / may).tolist()
+
+
+@pytest.mark.parametrize("rate", [0.3, 0.6, 1.0, 2.5])
+@pytest.mark.parametrize("n,hq,hkv,d", [(8192, 2, 2, 32), (4000, 2, 1, 64), (2500, 1, 1, 128)])
+def test_a_fixed_strong_decays_gradient(A, n, hq, hkv, d, rate):
+    """With the same decay in every row, a weight's error is the same for all pairs as far apart, and pairs are counted into a row's gradient and out of it again: both
+    times with one weight's bits, so that its error counts no more than the pair does.  What is left are the roundings of sums, 2^-21 (chains of 64 + 128),
+    of four of them: 2^-20 of the rows' 2-norm, and sqrt(256) times that of their sum, as above."""
+    case = Case([n], hq, hkv, d, 62, True, False)
+    case.g = np.full(hkv, -np.float32(rate)).astype(np.float64)
+    case.to_device()
+    got = host(case.run_backward(A, uncut(case, A))["dg"])
+    case.fixed = False
+    rows = case.backward()["dg"]
+    off, may = np.abs(got - rows.sum(0)), 16 * 2.0 ** -20 * np.linalg.norm(rows, axis=0)
+    assert (off <= may).all(), (off / may).tolist()
