@@ -628,7 +628,7 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
  *              decay_token_stride 0, [local_kv_heads]: the sum over all rows, in 64 bits.  A row's is off by roundings of the terms that its own 64 rows
  *              take part in (some 2^-18 of them at worst, all in fp32), however large those elsewhere in the sequence are
  *   d_initial  like d_final, written: the gradient of the sequences' initial states (by sequence: where several share a slot the caller adds
- *              them up); NULL: not wanted.  Not d_final itself: other workgroups still read it
+ *              them up); NULL: not wanted.  It shares no memory with d_final or with a slot of the initial pool: other workgroups still read them
  *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 1) bytes, 16-byte aligned
  */
 hspmd_status hspmd_linear_attn_bwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,

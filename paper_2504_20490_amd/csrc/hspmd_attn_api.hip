@@ -1403,6 +1403,23 @@ static hspmd_status check_linear_states(const hspmd_linear_batch* batch, const h
     return HSPMD_OK;
 }
 
+// d_initial is written while other workgroups still read d_final and the initial states
+static hspmd_status check_linear_d_initial(const hspmd_linear_batch* batch, const float* d_initial, const float* d_final, const hspmd::LinearStates& initial) {
+    if (!d_initial) return HSPMD_OK;
+    // (all of them 16-byte aligned: in elements)
+    const auto place = [](const float* x) { return (int64_t)(reinterpret_cast<uintptr_t>(x) / 4); };
+    const int64_t state = (int64_t)batch->local_kv_heads * batch->head_dim * batch->head_dim, size = state * batch->num_seqs;
+    const int64_t apart = place(d_initial) - place(d_final);
+    if (d_initial == d_final || (d_final && apart < size && -apart < size))
+        return fail(HSPMD_ERR_INVALID_ARG, "d_initial must not share memory with d_final");
+    if (!initial.data) return HSPMD_OK;
+    // the first slot that ends behind d_initial's start is the only one that can begin before its end without a later one doing so too
+    const int64_t from = place(d_initial) - place(initial.data), slot = from < state ? 0 : (from - state) / initial.slot_stride + 1;
+    const int64_t begin = slot == 0 ? -from : initial.slot_stride - (from - (slot - 1) * initial.slot_stride);      // of that slot, from d_initial's start on
+    if (slot < initial.num_slots && begin < size) return fail(HSPMD_ERR_INVALID_ARG, "d_initial must not share memory with the initial states");
+    return HSPMD_OK;
+}
+
 // shape and workspace of a chunked call
 static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward, void* workspace, size_t workspace_bytes, hspmd::LinearParams* p) {
     const hspmd::LinearSizes sizes = hspmd::linear_sizes(batch->total_rows, batch->num_seqs, batch->max_rows, batch->local_q_heads, batch->local_kv_heads,
@@ -1491,7 +1508,7 @@ hspmd_status hspmd_linear_attn_bwd(const hspmd_linear_batch* batch, const void* 
     if (hspmd_status rc = resolve_scale(scale, batch->head_dim, &p.scale)) return rc;
     if (hspmd_status rc = check_linear_states(batch, initial, batch->initial_slots, "initial", &p.initial)) return rc;
     if (!aligned16(d_final) || !aligned16(d_initial)) return fail(HSPMD_ERR_INVALID_ARG, "d_final and d_initial must be 16-byte aligned");
-    if (d_initial && d_initial == d_final) return fail(HSPMD_ERR_INVALID_ARG, "d_initial must not be d_final");
+    if (hspmd_status rc = check_linear_d_initial(batch, d_initial, d_final, p.initial)) return rc;
     if (reinterpret_cast<uintptr_t>(d_log_decay) & 3u) return fail(HSPMD_ERR_INVALID_ARG, "d_log_decay must be 4-byte aligned");
     const bool fixed_sum = d_log_decay && decay_token_stride == 0;     // written whether there are rows or not
     if (batch->num_seqs > 0) {
