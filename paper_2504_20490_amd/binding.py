@@ -900,8 +900,8 @@ def _linear_workspace(workspace, devices: list):
 
 def linear_attn_bwd(batch: LinearBatch, q, k, v, log_decay, d_o, dq, dk, dv, workspace, initial=None, d_final=None, d_log_decay=None,
                     d_initial=None, scale: float = 0.0, stream=None) -> None:
-    """dq, dk, dv (all bf16 or all fp32, contiguous), d_log_decay (fp32, log_decay's shape; [kv_heads] where its token stride is 0) and d_initial
-    (fp32 [num_seqs, kv_heads, d, d]) from d_o and d_final (like d_initial); the last three may be None."""
+    """dq, dk, dv (all bf16 or all fp32, contiguous), d_log_decay (fp32, log_decay's shape; [kv_heads] where its token stride is 0, and, if that is wanted,
+    where there is at most one row) and d_initial (fp32 [num_seqs, kv_heads, d, d]) from d_o and d_final (like d_initial); the last three may be None."""
     import torch
     if not batch.has_cu:
         raise _bad("the batch has no cu_rows")
@@ -913,6 +913,8 @@ def linear_attn_bwd(batch: LinearBatch, q, k, v, log_decay, d_o, dq, dk, dv, wor
     if t is not torch.bfloat16 and t is not f32:
         raise _bad("the gradients have to be bf16 or fp32")
     grads = [_linear_dense(x, (T, h, d), t, name, devices) for x, h, name in ((dq, hq, "dq"), (dk, hkv, "dk"), (dv, hkv, "dv"))]
+    if T <= 1 and d_log_decay is not None and d_log_decay.dim() == 1:      # (the stride of one row says nothing)
+        strides = (*strides[:2], 0)
     dg_ptr = _linear_dense(d_log_decay, (T, hkv) if strides[2] else (hkv,), f32, "d_log_decay", devices)
     end_ptr, start_ptr = (_linear_dense(x, (n, hkv, d, d), f32, name, devices) for x, name in ((d_final, "d_final"), (d_initial, "d_initial")))
     ws, size = _linear_workspace(workspace, devices)
