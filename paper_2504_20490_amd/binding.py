@@ -869,9 +869,13 @@ def linear_attn_workspace_bytes(batch: LinearBatch, total_rows: int, q_heads: in
     """Bytes of workspace that linear_attn_fwd (or, backward, linear_attn_bwd) takes; 0 where none is needed."""
     lib, counts = load_library(), [_count(x, "a count") for x in (total_rows, q_heads, kv_heads, head_dim)]
     # (the library answers 0 to what it refuses as well: its backward takes some wherever there is a sequence)
-    if int(lib.hspmd_linear_attn_workspace_bytes(batch._args(*counts), 1)) == 0 and (batch.num_seqs or counts[0]):
+    args = batch._args(*counts)
+    asked = args._obj.num_seqs
+    args._obj.num_seqs = max(asked, 1)
+    if int(lib.hspmd_linear_attn_workspace_bytes(args, 1)) == 0:
         raise HspmdError(1, lib.hspmd_last_error().decode())
-    return int(lib.hspmd_linear_attn_workspace_bytes(batch._args(*counts), 1 if backward else 0))
+    args._obj.num_seqs = asked
+    return int(lib.hspmd_linear_attn_workspace_bytes(args, 1 if backward else 0))
 
 
 def linear_attn_fwd(batch: LinearBatch, q, k, v, log_decay, o, workspace, initial=None, final=None, scale: float = 0.0, stream=None) -> None:
