@@ -53,6 +53,20 @@ HSPMD_LINEAR_INDEX int linear_anchor_elements(int head_dim) { return (head_dim +
 // starts there; windows are what the launch that passes states from segment to segment goes by.
 HSPMD_LINEAR_INDEX int64_t linear_windows(int64_t total_rows, int64_t seg_rows) { return total_rows / seg_rows + 1; }
 
+// Columns of a state that a workgroup of the single step takes; `states` of the launch.  Narrow pieces of rows are read and written in more places at once, but a line of 128
+// bytes that two of them share moves twice.  us at 4 query heads each (d = 104, 120: one, 96: four), pieces in the order 32, 64 columns, whole rows:
+//   d = 128: 64 states 7.6, 8.3, 11.1; 512 states 16.0, 16.6, 18.7; 640 states 24.2, 21.3, 22.9; 4096 states 112, 111, 125: 32 to 2^23 elements, 64 from there on
+//   d = 96: 64 states 6.7, 7.0, 8.6; 768 states 19.5, 19.7, 17.9; 4096 states 70, 72, 79: likewise
+//   d = 104: 64 states 9.9, 7.0, 7.5; 128 states 10.9, 8.3, 8.3; 512 states 17.6, 15.2, 14.1; 8192 states 224, 198, 144: 64 for few
+//   d = 120: 64 states 7.9, 7.7, 8.4; 192 states 11.9, 11.2, 10.9; 8192 states 296, 264, 180: likewise
+//   up to 88 and at 64: whole rows throughout (d = 64: 512 states 11.6, whole 8.3; d = 72: 128 states 11.1, 7.0, d = 40: 256 states 10.2, 5.0)
+HSPMD_LINEAR_INDEX int linear_step_columns(int head_dim, int64_t states) {
+    const int64_t elements = states * head_dim * head_dim;
+    if (head_dim <= 64) return head_dim;
+    if (head_dim % 32 == 0) return elements <= (1 << 23) ? 32 : 64;
+    return head_dim > 96 && elements <= (1 << 20) ? 64 : head_dim;
+}
+
 // Workgroups go to the 8 XCDs in turn.  Items do so four heads at a time (`granule` items: four heads, all that is computed for them): neighbouring heads share
 // lines of the decays and the edges of rows, which then meet in one L2, and every XCD has as many items as another but for one granule.  (All heads of a slot
 // on one XCD, ranges of slots, left some with a round of workgroups more.)  The grid is 8 * granule * rounds; items from `items` on are none.

@@ -1,7 +1,7 @@
 // Linear attention with a decay for each head, recurrent form: one token per sequence over a pool of states.
 //   S' = e^g S + k v^T,   o_h = s S'^T q_h for each query head h of the group.
 // Bound by reading and writing the states: 8 d^2 bytes for 3 d^2 + 2 d^2 group operations.  A workgroup takes a (sequence, KV head), or some
-// of its columns where there are few; a thread owns four columns of every R-th row and keeps them in registers, so a state is read once and
+// of its columns (linear_step_columns); a thread owns four columns of every R-th row and keeps them in registers, so a state is read once and
 // written once however many query heads share it, and all of a thread's reads are in flight at once.
 #include "linear_device.hpp"
 
@@ -81,12 +81,7 @@ hipError_t launch_linear_step(const LinearStepParams& p, hipStream_t stream) {
     const int d = p.head_dim;
     const int64_t states = (int64_t)p.num_seqs * p.kv_heads;
     if (states == 0) return hipSuccess;
-    // Few states: their columns go to four workgroups, or to two, which read and write in more places at once (d = 128, 4 query heads each: 128 states 7.4 us in
-    // four parts, 7.9 in two, 10.5 whole; 512 states 15.3, 15.7, 17.2).  Narrow pieces of rows cost where there are enough workgroups without
-    // (8000 states, d = 104: 140 us whole, 191 in two parts; 1024, d = 64: 8.1, 9.9).
-    const int64_t elements = states * d * d;
-    const int split = d > 32 && elements <= (1 << 21) ? 4 : d > 64 && elements <= (1 << 23) ? 2 : 1;
-    const int columns = split == 1 ? d : (d / split + 7) / 8 * 8, parts = (d + columns - 1) / columns;
+    const int columns = linear_step_columns(d, states), parts = (d + columns - 1) / columns;
     const unsigned grid = (unsigned)(states * parts);
     const int rows_per_pass = kStepThreads / (columns / 4), passes = (d + rows_per_pass - 1) / rows_per_pass;
     if (passes <= 4) linear_step_kernel<4><<<grid, kStepThreads, 0, stream>>>(p, columns, parts);

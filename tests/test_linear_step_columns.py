@@ -1,0 +1,43 @@
+"""What a workgroup of the linear attention's single step takes of a state, from the kernels' own rule on the host: all columns are taken once, pieces of rows are whole
+lines of memory wherever rows are, and rows that are not are cut for few states of many columns only."""
+import ctypes
+import subprocess
+
+import pytest
+
+from paper_2504_20490_amd import build as lib_build
+
+SHIM = """
+#include "linear_index.hpp"
+extern "C" int columns(int head_dim, long states) { return hspmd::linear_step_columns(head_dim, states); }
+"""
+
+
+@pytest.fixture(scope="module")
+def columns(tmp_path_factory):
+    d = tmp_path_factory.mktemp("linear_step")
+    (d / "shim.cpp").write_text(SHIM)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-shared", "-fPIC", "-Wall", "-Werror", f"-I{lib_build.CSRC}", "-o", str(d / "shim.so"), str(d / "shim.cpp")], check=True)
+    f = ctypes.CDLL(str(d / "shim.so")).columns
+    f.argtypes = [ctypes.c_int, ctypes.c_long]
+    return f
+
+
+@pytest.mark.parametrize("d", range(8, 129, 8))
+def test_pieces(columns, d):
+    for states in (1, 2, 7, 63, 64, 65, 500, 512, 513, 640, 4096, 8000, 1 << 22):
+        c = columns(d, states)
+        assert 0 < c <= d and c % 8 == 0
+        assert states * -(-d // c) * 256 < 1 << 32                   # threads of the launch
+        if d <= 64 or d % 32 and d <= 96:
+            assert c == d
+        elif d % 32 == 0:
+            assert c % 32 == 0 and c < d
+        else:
+            assert c % 32 == 0 if states * d * d <= 1 << 20 else c == d
+
+
+def test_more_states_never_take_narrower_pieces(columns):
+    for d in range(8, 129, 8):
+        seen = [columns(d, n) for n in (1, 10, 64, 100, 512, 513, 1000, 10000, 1 << 22)]
+        assert seen == sorted(seen)
