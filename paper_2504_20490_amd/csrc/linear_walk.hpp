@@ -178,7 +178,8 @@ struct State {
             for (int i = 0; i < 16; i += 4) {
                 union { f32x4 f; u32x4 u; } y;
                 y.f = f32x4{x[db][i] * by, x[db][i + 1] * by, x[db][i + 2] * by, x[db][i + 3] * by};
-                if (db * 32 + i / 8 * 16 < d) __builtin_amdgcn_raw_buffer_store_b128(y.u, rsrc, lane * 16, (db * 16 + i) * 256, 0);
+                // (with its offset in a scalar register the store would read what the next instructions leave in y's registers: the compiler takes it to need no room)
+                if (db * 32 + i / 8 * 16 < d) __builtin_amdgcn_raw_buffer_store_b128(y.u, rsrc, lane * 16 + (db * 16 + i) * 256, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);      // (one at a time: else the products take registers that are not there)
             }
     }

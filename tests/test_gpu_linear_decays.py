@@ -84,3 +84,38 @@ def test_a_fixed_strong_decays_gradient(A, n, hq, hkv, d, rate):
     rows = case.backward()["dg"]
     off, may = np.abs(got - rows.sum(0)), 16 * 2.0 ** -20 * np.linalg.norm(rows, axis=0)
     assert (off <= may).all(), (off / may).tolist()
+
+
+@pytest.mark.parametrize("f32", [True, False])
+@pytest.mark.parametrize("hq,hkv,d", [(24, 24, 128), (24, 24, 64), (16, 4, 128), (12, 12, 104), (20, 20, 80)])
+def test_packs_that_fill_the_device_are_run_to_run_the_same(A, hq, hkv, d, f32):
+    """Many heads on segments of many groups of 64 rows: the same bits three times, and as uncut sequences.  Each of the two is off by 2^-20 of
+    its terms, which cancel by up to four, 2^-18 of the norm of 64 rows' and their neighbours', in its own way, as states pass in other roundings: the two differ by
+    up to twice that."""
+    import torch
+    torch.manual_seed(63)
+    lengths = [1851, 4713, 898, 8207, 450]
+    n = sum(lengths)
+    q, do = (torch.randn(n, hq, d, device="cuda").bfloat16() for _ in range(2))
+    k, v = (torch.randn(n, hkv, d, device="cuda").bfloat16() for _ in range(2))
+    rate = 0.5 * 2.0 ** (-8.0 * torch.arange(hkv, device="cuda") / hkv)
+    g = -rate * torch.exp(0.5 * torch.randn(n, hkv, device="cuda"))
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(lengths)]), dtype=torch.int32, device="cuda")
+
+    def run(hint):
+        batch = A.LinearBatch(cu, max_rows=hint)
+        ws = torch.full((A.linear_attn_workspace_bytes(batch, n, hq, hkv, d, backward=True),), 255, dtype=torch.uint8, device="cuda")
+        t = torch.float32 if f32 else torch.bfloat16
+        out = [torch.empty(n, h, d, dtype=t, device="cuda") for h in (hq, hkv, hkv)] + [torch.empty(n, hkv, device="cuda")]
+        A.linear_attn_bwd(batch, q, k, v, g, do, *out[:3], ws, d_log_decay=out[3])
+        return out
+
+    first = run(max(lengths))
+    for _ in range(2):
+        assert all(torch.equal(a, b) for a, b in zip(first, run(max(lengths))))
+    uncut = run(1)[3].double()
+    off = (first[3].double() - uncut)
+    groups = lambda x: torch.nn.functional.pad(x * x, (0, 0, 0, -n % 64)).view(-1, 64, hkv).sum(1)
+    size = groups(uncut)
+    near = torch.stack([size, size.roll(1, 0), size.roll(-1, 0)]).max(0).values      # (groups of the packed rows, not of the sequences)
+    assert (groups(off) <= (2 * 2.0 ** -18) ** 2 * near).all(), (groups(off) / near).max().sqrt().item()
