@@ -610,7 +610,8 @@ typedef struct {
  * decays. No atomics: results are run-to-run bit-identical. A row of o is not changed by later rows of its sequence, whatever those hold; an infinity or NaN in
  * a row of k, v or log_decay is in the state from there on and may make all of it NaN.
  */
-size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward);   /* 0 on bad arguments, and where none is needed */
+/* backward: 0 the forward's, 1 the backward's, 2 the backward's without d_log_decay.  0 on bad arguments, and where none is needed */
+size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward);
 hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
                                    int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,
                                    const hspmd_linear_states* initial, const hspmd_linear_states* final, void* o, void* workspace,
@@ -629,7 +630,8 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
  *              take part in (some 2^-18 of them at worst, all in fp32), however large those elsewhere in the sequence are
  *   d_initial  like d_final, written: the gradient of the sequences' initial states (by sequence: where several share a slot the caller adds
  *              them up); NULL: not wanted.  It shares no memory with d_final or with a slot of the initial pool: other workgroups still read them
- *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 1) bytes, 16-byte aligned
+ *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 1) bytes, 16-byte aligned; without d_log_decay (batch, 2) bytes suffice, which spares
+ *              two fp32 states for every 256 rows and KV head
  */
 hspmd_status hspmd_linear_attn_bwd(const hspmd_linear_batch* batch, const void* q, const void* k, const void* v, const float* log_decay,
                                    const void* d_o, int64_t q_token_stride, int64_t kv_token_stride, int64_t decay_token_stride, float scale,

@@ -865,8 +865,9 @@ def _linear_rows(batch: LinearBatch, q, k, v, log_decay):
     return (T, hq, hkv, d), (q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr()), (qs, ks, gs), devices
 
 
-def linear_attn_workspace_bytes(batch: LinearBatch, total_rows: int, q_heads: int, kv_heads: int, head_dim: int, backward: bool = False) -> int:
-    """Bytes of workspace that linear_attn_fwd (or, backward, linear_attn_bwd) takes; 0 where none is needed."""
+def linear_attn_workspace_bytes(batch: LinearBatch, total_rows: int, q_heads: int, kv_heads: int, head_dim: int, backward: bool = False,
+                                decays: bool = True) -> int:
+    """Bytes of workspace that linear_attn_fwd (or, backward, linear_attn_bwd, without decays: without d_log_decay) takes; 0 where none is needed."""
     lib, counts = load_library(), [_count(x, "a count") for x in (total_rows, q_heads, kv_heads, head_dim)]
     # (the library answers 0 to what it refuses as well: its backward takes some wherever there is a sequence)
     args = batch._args(*counts)
@@ -875,7 +876,7 @@ def linear_attn_workspace_bytes(batch: LinearBatch, total_rows: int, q_heads: in
     if int(lib.hspmd_linear_attn_workspace_bytes(args, 1)) == 0:
         raise HspmdError(1, lib.hspmd_last_error().decode())
     args._obj.num_seqs = asked
-    return int(lib.hspmd_linear_attn_workspace_bytes(args, 1 if backward else 0))
+    return int(lib.hspmd_linear_attn_workspace_bytes(args, (1 if decays else 2) if backward else 0))
 
 
 def linear_attn_fwd(batch: LinearBatch, q, k, v, log_decay, o, workspace, initial=None, final=None, scale: float = 0.0, stream=None) -> None:

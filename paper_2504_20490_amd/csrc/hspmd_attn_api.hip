@@ -1421,9 +1421,9 @@ static hspmd_status check_linear_d_initial(const hspmd_linear_batch* batch, cons
 }
 
 // shape and workspace of a chunked call
-static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward, void* workspace, size_t workspace_bytes, hspmd::LinearParams* p) {
+static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward, bool decays, void* workspace, size_t workspace_bytes, hspmd::LinearParams* p) {
     const hspmd::LinearSizes sizes = hspmd::linear_sizes(batch->total_rows, batch->num_seqs, batch->max_rows, batch->local_q_heads, batch->local_kv_heads,
-                                                         batch->head_dim, backward);
+                                                         batch->head_dim, backward, decays);
     const size_t need = sizes.total_bytes(backward);
     if (need > 0 && (!workspace || !aligned16(workspace))) return fail(HSPMD_ERR_INVALID_ARG, "workspace must be non-NULL and 16-byte aligned");
     if (workspace_bytes < need) return fail(HSPMD_ERR_WORKSPACE_TOO_SMALL, "workspace smaller than hspmd_linear_attn_workspace_bytes");
@@ -1458,7 +1458,7 @@ static hspmd_status linear_shape(const hspmd_linear_batch* batch, bool backward,
 size_t hspmd_linear_attn_workspace_bytes(const hspmd_linear_batch* batch, int32_t backward) {
     if (check_linear_batch(batch) || batch->num_seqs == 0) return 0;
     return hspmd::linear_sizes(batch->total_rows, batch->num_seqs, batch->max_rows, batch->local_q_heads, batch->local_kv_heads, batch->head_dim,
-                               backward != 0).total_bytes(backward != 0);
+                               backward != 0, backward != 2).total_bytes(backward != 0);
 }
 
 static hspmd_status check_linear_cu(const hspmd_linear_batch* batch) {
@@ -1483,7 +1483,7 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
     } else if (!final) {
         return HSPMD_OK;
     }
-    if (hspmd_status rc = linear_shape(batch, false, workspace, workspace_bytes, &p)) return rc;
+    if (hspmd_status rc = linear_shape(batch, false, false, workspace, workspace_bytes, &p)) return rc;
     p.q = static_cast<const uint16_t*>(q);
     p.k = static_cast<const uint16_t*>(k);
     p.v = static_cast<const uint16_t*>(v);
@@ -1520,7 +1520,7 @@ hspmd_status hspmd_linear_attn_bwd(const hspmd_linear_batch* batch, const void* 
                 return fail(HSPMD_ERR_INVALID_ARG, "d_o, dq, dk, dv must be 16-byte aligned");
         }
         if (batch->total_rows > 0 || d_initial || fixed_sum) {
-            if (hspmd_status rc = linear_shape(batch, true, workspace, workspace_bytes, &p)) return rc;
+            if (hspmd_status rc = linear_shape(batch, true, d_log_decay != nullptr, workspace, workspace_bytes, &p)) return rc;
         }
     }
     if (!fixed_sum && (batch->num_seqs == 0 || (batch->total_rows == 0 && !d_initial))) return HSPMD_OK;

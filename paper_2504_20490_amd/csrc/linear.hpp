@@ -66,12 +66,12 @@ struct LinearSizes {
     int32_t seg_rows;              // as in LinearShape
     int64_t slots, entries, windows;
     size_t state_bytes, decay_bytes, q_row_bytes, k_row_bytes, slot_bytes, anchor_bytes;
-    size_t total_bytes(bool backward) const {
+    size_t total_bytes(bool backward) const {      // (without anchors where decay gradients are not wanted: anchor_bytes is 0 then)
         return backward ? 2 * state_bytes + decay_bytes + 2 * q_row_bytes + 2 * k_row_bytes + 2 * slot_bytes + 2 * anchor_bytes : state_bytes + decay_bytes;
     }
 };
 LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
-                         bool backward);
+                         bool backward, bool decays);
 // states of sequences that are cut into segments; parts: of a source's bf16 values, 2 or 3
 void launch_linear_states(const LinearParams& p, bool backward, int parts, hipStream_t stream);
 hipError_t launch_linear_fwd(const LinearParams& p, hipStream_t stream);

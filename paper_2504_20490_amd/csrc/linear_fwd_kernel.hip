@@ -23,7 +23,7 @@ void launch(const LinearParams& p, hipStream_t stream) {
 }  // namespace
 
 LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows, int32_t q_heads, int32_t kv_heads, int32_t head_dim,
-                         bool backward) {
+                         bool backward, bool decays) {
     LinearSizes s{};
     // As many segments as make one round of workgroups, 512 (a sequence ends in half a segment on average); fewer leave the device idle, more cost states
     // and a second round's end.  (The headline pack, 24 heads: 345 us in segments of 1024, 328 of 1856; ten prompts, 16 heads: 158 of 1024,
@@ -48,7 +48,7 @@ LinearSizes linear_sizes(int32_t total_rows, int32_t num_seqs, int32_t max_rows,
     s.q_row_bytes = rounded((int64_t)total_rows * q_heads * 4);
     s.k_row_bytes = rounded((int64_t)total_rows * kv_heads * 4);
     s.slot_bytes = rounded(s.slots * kv_heads * 8);
-    s.anchor_bytes = rounded(linear_anchors(total_rows) * kv_heads * linear_anchor_elements(head_dim) * 4);
+    s.anchor_bytes = rounded(decays ? linear_anchors(total_rows) * kv_heads * linear_anchor_elements(head_dim) * 4 : 0);
     return s;
 }
 

@@ -41,3 +41,20 @@ def test_more_states_never_take_narrower_pieces(columns):
     for d in range(8, 129, 8):
         seen = [columns(d, n) for n in (1, 10, 64, 100, 512, 513, 1000, 10000, 1 << 22)]
         assert seen == sorted(seen)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,group", [(3, 5), (30, 1), (600, 2)])
+@pytest.mark.parametrize("d", [8, 40, 64, 72, 88, 96, 104, 112, 120, 128])
+def test_steps_in_pieces(d, n, group):
+    import numpy as np
+    import torch
+    import paper_2504_20490_amd as A
+    from linear_util import Case, check_forward, host
+    case = Case([1] * n, 2 * group, 2, d, 80 + d, False, True).to_device()
+    o = torch.full((n, 2 * group, d), float("nan"), dtype=torch.bfloat16, device="cuda")
+    final = torch.full_like(case.tinitial, float("nan"))
+    A.linear_attn_step(A.LinearBatch(), case.tq, case.tk, case.tv, case.tg, o, initial=case.tinitial, final=final)
+    check_forward(case, o, final)
+    want, most = case.forward()[1], case.forward(absolute=True)[1]
+    assert (np.abs(host(final) - want) <= 2.0 ** -22 * most).all()      # a product and a sum, the decay's exponent and exponential
