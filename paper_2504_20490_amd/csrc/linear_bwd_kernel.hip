@@ -4,8 +4,8 @@
 namespace hspmd {
 namespace {
 
-// DECAYS: their gradients are wanted, and with them the dot products, which cost a sixth (headline pack, 24 heads: 965 us with, 860 without; fp32 gradients 1065 and 960,
-// on 32 query heads of 8 KV heads 1460 and 1190).  The other gradients are the same bits.
+// DECAYS: their gradients are wanted, and with them the dot products and the anchors, which cost a quarter on one query head per KV head (headline pack, 24 heads: 1095 us with, 865
+// without; fp32 gradients 1200 and 965; 32 query heads on 8 KV heads: 1130 and 940, fp32 1680 and 1340).  The other gradients are the same bits.
 template <int D, bool ONE, int WEIGHT_PARTS, int V_PARTS, int NB, bool DECAYS>
 __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 && !ONE ? 1 : 2) void linear_bwd_kernel(LinearParams p) {
     __shared__ __align__(16) char lds[Lds<D, WEIGHT_PARTS, ONE>::bytes(true, DECAYS || Lds<D, WEIGHT_PARTS, ONE>::kLate)];
@@ -24,7 +24,9 @@ __global__ __launch_bounds__(D / 32 * 64, D == 128 && WEIGHT_PARTS == 3 && !ONE 
 // so from a place where <S, R> is known, what lies across the chunks next to it follows by differences.  These keep the rounding errors of all terms on the way, where
 // the value itself shrinks with the decays: carried along a segment of 8192 tokens they came to 1e-3 of a fixed decay's gradient, and to as much of rows near others
 // with 10^4 times their gradients.  So <S, R> is known at the segment's ends and at every fourth chunk (its anchors), and a chunk in between takes the
-// difference from the side where the terms on the way are smaller.  (Per row as accurate as <S, R> of every chunk, which would move four times as much.)
+// difference from the side where the terms on the way are smaller.  What this launch takes is reading them: 101 us for the headline pack, 4 TB/s.  (Against the definition in 64
+// bits over 8192 rows: every 64 rows' gradients off by 1e-6 to 3e-6 of their norm, a fixed decay's by up to 8e-6 of its rows' norm.  Anchors at every second
+// chunk: 5e-6 and 15 % more time for the backward, at every eighth 2e-5 and 6 % less.)
 constexpr int kDecayWaves = 8, kDecayBlocks = kDecayWaves / kLinearAnchor;
 static_assert(kLinearAnchor == 4 && kDecayWaves % kLinearAnchor == 0, "the waves of an anchor's chunks share its sum");
 

@@ -11,7 +11,7 @@
 // element, its parts) is shared by 64 targets; with two workgroups per compute unit their tiles fit LDS (62 KB forward, 80 KB backward).
 // The state stays in registers: a wave holds 32 of its columns, 64 registers at head_dim 128, and everything it multiplies comes from LDS.
 // What bounds it: memory in the forward (512 sequences of 1024 tokens, head_dim 128: 130 us, 4.1 TB/s; loads and stores alone 113 us, products
-// alone 92), the chip's power in the backward (24 heads, 32768 tokens: 907 us, 0.6 PFLOP/s of products in their parts at 1.5 GHz).
+// alone 92), the chip's power in the backward (24 heads, 32768 tokens: 934 us, 0.56 PFLOP/s of products in their parts at 1.5 to 1.75 GHz).
 #pragma once
 #include "linear_device.hpp"
 
@@ -356,7 +356,7 @@ __device__ __forceinline__ float walk(const LinearParams& p, const Routine& f, c
     for (int n = 0; n < chunks; ++n) {
         const int chunk = LATER ? chunks - 1 - n : n;
         const int first = chunk * kLinearChunk;
-        if (wave == kWaves - 1) {        // (the wave without a block of pairs)
+        if (wave == kWaves - 1) {        // (of four waves the one without a block of pairs)
             // LATER: the sums are those of the tokens behind each, from the chunk's end on, so that a decay that is NaN reaches the tokens it decays alone
             const bool there = token < seg.rows - first;
             const DecayLog2 g = split_decay_log2(next_g);
