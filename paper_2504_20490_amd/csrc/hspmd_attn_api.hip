@@ -1412,7 +1412,7 @@ static hspmd_status check_linear_d_initial(const hspmd_linear_batch* batch, cons
     const int64_t apart = place(d_initial) - place(d_final);
     if (d_initial == d_final || (d_final && apart < size && -apart < size))
         return fail(HSPMD_ERR_INVALID_ARG, "d_initial must not share memory with d_final");
-    if (!initial.data) return HSPMD_OK;
+    if (!initial.data || size == 0) return HSPMD_OK;
     // the first slot that ends behind d_initial's start is the only one that can begin before its end without a later one doing so too
     const int64_t from = place(d_initial) - place(initial.data), slot = from < state ? 0 : (from - state) / initial.slot_stride + 1;
     const int64_t begin = slot == 0 ? -from : initial.slot_stride - (from - (slot - 1) * initial.slot_stride);      // of that slot, from d_initial's start on

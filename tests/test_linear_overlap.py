@@ -59,3 +59,10 @@ def test_no_memory_in_common_where_there_is_none():
 def test_slots_as_far_apart_as_can_be(stride):
     far = P + (1 << 26)
     assert call(None, far, far, stride=stride) == 1 and call(None, far + 4 * STATE, far, stride=stride) == 3 and call(None, far - 16, far, stride=stride) == 1
+
+
+def test_no_sequence_has_no_gradient():
+    """Nothing is written then, whatever the pointers are."""
+    far = P + (1 << 26)
+    for d_initial in (far, far + 16, far + 4 * STATE):
+        assert call(None, d_initial, far, n=0, rows=0) == 0 and call(far + 32, d_initial, n=0, rows=0) == 0, d_initial - far
