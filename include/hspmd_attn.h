@@ -627,7 +627,8 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
  *   dq, dk, dv as in hspmd_attn_varlen_bwd: contiguous, bf16 or fp32; dk, dv summed over the group
  *   d_log_decay  fp32, written; NULL: not wanted, the call then takes a tenth to a fifth less.  [total_rows, local_kv_heads], or, with
  *              decay_token_stride 0, [local_kv_heads]: the sum over all rows, in 64 bits.  A row's is off by fp32 roundings of the terms that its own 64 rows
- *              take part in (1e-6 to 3e-6 of the norm of 64 rows' gradients), however large those elsewhere in the sequence are
+ *              take part in (1e-6 to 3e-6 of the norm of 64 rows' gradients), however large those elsewhere in the sequence are, but
+ *              for ones within 256 rows on both sides
  *   d_initial  like d_final, written: the gradient of the sequences' initial states (by sequence: where several share a slot the caller adds
  *              them up); NULL: not wanted.  It shares no memory with d_final or with a slot of the initial pool: other workgroups still read them
  *   workspace  device, hspmd_linear_attn_workspace_bytes(batch, 1) bytes, 16-byte aligned; without d_log_decay (batch, 2) bytes suffice, which spares
