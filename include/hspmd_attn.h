@@ -625,7 +625,7 @@ hspmd_status hspmd_linear_attn_fwd(const hspmd_linear_batch* batch, const void* 
  *   initial    as in the forward
  *   d_final    fp32 [num_seqs, local_kv_heads, head_dim, head_dim], 16-byte aligned: the gradient of the sequences' final states; NULL: zeros
  *   dq, dk, dv as in hspmd_attn_varlen_bwd: contiguous, bf16 or fp32; dk, dv summed over the group
- *   d_log_decay  fp32, written; NULL: not wanted, the call then takes a tenth to a fifth less.  [total_rows, local_kv_heads], or, with
+ *   d_log_decay  fp32, written; NULL: not wanted, the call then takes a sixth to a third less.  [total_rows, local_kv_heads], or, with
  *              decay_token_stride 0, [local_kv_heads]: the sum over all rows, in 64 bits.  A row's is off by fp32 roundings of the terms that its own 64 rows
  *              take part in (1e-6 to 3e-6 of the norm of 64 rows' gradients), however large those elsewhere in the sequence are, but
  *              for ones within 256 rows on both sides
